@@ -301,6 +301,112 @@ drf_status drf_noise_count(const drf_sched_config* sched, drf_mode mode, int n, 
 drf_status drf_plan_build(const drf_sched_config* sched, drf_mode mode, int n, int32_t* rows, size_t cap,
                           size_t* n_rows);
 
+/* ---- operators of the denoiser's attention --------------------------------------------------------
+ * What a transformer denoiser does between its qkv Linear and its attention's output: rotary positions,
+ * norms of queries and keys, the choice of key blocks, attention over the chosen ones.  A denoiser made
+ * by drf_denoiser_create_attn runs them in every block; a caller with a predictor of its own calls them
+ * on its own tensors.  They allocate nothing, keep nothing between calls and need no handle; every call
+ * may be captured into a HIP graph.  All arithmetic is fp32 or wider; results are rounded once, to the
+ * tensors' type (the attention's probabilities are rounded to the type of the values too).
+ */
+
+/*
+ * A tensor [slots][tokens][heads][head_dim], DEVICE: element (s, n, h, c) at
+ * data + s * slot_stride + n * token_stride + h * head_stride + c, strides in elements.  A column range
+ * of a qkv Linear's rows (token_stride = row width, head_stride = head_dim) and planes stored head by
+ * head (head_stride = tokens * head_dim, token_stride = head_dim) are both such tensors.
+ */
+typedef struct { void* data; int64_t slot_stride, token_stride, head_stride; } drf_heads;
+
+/* Sizes of an attention; lengths behind which a slot's tokens do not exist, DEVICE int32 [slots], or NULL:
+ * all tokens do.  A length is taken as 0 below 0 and as the number of tokens above it. */
+typedef struct {
+    drf_dtype dtype;
+    int slots, q_tokens, kv_tokens, q_heads, kv_heads, head_dim;   /* q_heads a multiple of kv_heads: query head h reads kv head h / (q_heads / kv_heads) */
+    const int32_t *q_lens, *kv_lens;
+} drf_attn_shape;
+
+/*
+ * Rotary positions with up to three axes (time, row, column of a latent).  Columns of a head are sections
+ * of dim[0], dim[1], .. columns from column 0 on, the rest is left as it is.  Pair i of an axis with dim
+ * columns turns by phi = position * theta^(-2 i / dim):
+ *   (x, y) -> (x cos phi - y sin phi, x sin phi + y cos phi)
+ * DRF_ROPE_PAIRS: x and y are columns 2i and 2i + 1 of the section; DRF_ROPE_HALVES: i and i + dim / 2.
+ * Position of token n on axis a: origin[a] + step[a] * (its coordinate in the row-major grid of extent[0] x
+ * extent[1] x .., the first axis slowest and not limited by its extent), or table entry [n][a] where a call gives a table.
+ * Angles are formed in double precision.  Negated origins and steps turn back.
+ */
+#define DRF_ROPE_AXES 3
+typedef enum { DRF_ROPE_PAIRS = 0, DRF_ROPE_HALVES = 1 } drf_rope_layout;
+typedef struct {
+    int n_axes;                     /* 1 .. DRF_ROPE_AXES */
+    int dim[DRF_ROPE_AXES];         /* even, >= 0; together at most head_dim */
+    int extent[DRF_ROPE_AXES];      /* >= 1 */
+    double origin[DRF_ROPE_AXES], step[DRF_ROPE_AXES];
+    double theta;                   /* > 0 */
+    drf_rope_layout layout;
+} drf_rope_config;
+
+/*
+ * out = rotated x, for one tensor of queries or keys.
+ *   lens        DEVICE int32 [slots] or NULL; rows behind a slot's length are neither read nor written
+ *   positions   DEVICE fp32 or NULL: element (slot s, token n, axis a) at positions[s * positions_slot_stride +
+ *               n * n_axes + a] (stride 0: one table for all slots); replaces the grid, origin and step
+ *   out         may be x itself (the same address and strides); otherwise the two do not overlap
+ * head_dim <= 128.  16-byte aligned tensors whose strides and head_dim are multiples of 16 bytes take 16-byte
+ * accesses; all others one element at a time.
+ */
+drf_status drf_rope(const drf_rope_config* rope, drf_dtype dtype, int slots, int tokens, int heads, int head_dim,
+                    const int32_t* lens, const float* positions, size_t positions_slot_stride, const drf_heads* x,
+                    const drf_heads* out, void* hip_stream);
+
+/*
+ * Norm of every head of q and k, then the rotation (rope NULL: none), in one pass:
+ *   DRF_QK_RMS     y = x / sqrt(mean(x^2) + eps) * gain
+ *   DRF_QK_LAYER   y = (x - mean(x)) / sqrt(var(x) + eps) * gain + bias
+ *   DRF_QK_NONE    y = x                                             (gains and biases NULL)
+ * and the queries times q_scale (a softmax scale, or 1).  Gains and biases: DEVICE fp32 [head_dim], or NULL:
+ * ones and zeros; biases only with DRF_QK_LAYER.  q and k have the same tokens (shape->kv_tokens == q_tokens) and lengths
+ * (shape->q_lens; kv_lens is NULL or the same address).  q_out may be q itself, k_out k itself; otherwise as in drf_rope.
+ */
+typedef enum { DRF_QK_NONE = 0, DRF_QK_RMS = 1, DRF_QK_LAYER = 2 } drf_qk_norm;
+typedef struct {
+    drf_qk_norm norm;
+    double eps;                     /* >= 0 */
+    float q_scale;
+    const float *q_gain, *q_bias, *k_gain, *k_bias;
+} drf_qk_config;
+drf_status drf_qk_norm_rope(const drf_qk_config* cfg, const drf_rope_config* rope, const drf_attn_shape* shape,
+                            const float* positions, size_t positions_slot_stride, const drf_heads* q, const drf_heads* k,
+                            const drf_heads* q_out, const drf_heads* k_out, void* hip_stream);
+
+/*
+ * The key blocks that each block of queries attends to.  Queries are taken q_block at a time, keys kv_block at a time
+ * (each 32, 64 or 128), and
+ *   score(i, j) = (mean of the queries of block i) . (mean of the keys of block j)       in double precision,
+ * means over the rows inside a slot's length.  Of the key blocks that hold a key the topk of largest score are chosen, the
+ * lower j of equal ones, one that is not a number after all others.
+ *   blocks   DEVICE uint32 [slots][q_heads][nq][words], nq = ceil(q_tokens / q_block), words = drf_block_words():
+ *            bit j % 32 of word j / 32 of row i: query block i attends to key block j.  A query block with no query
+ *            inside its slot's length has none.
+ *   scratch  DEVICE, 16-byte aligned, drf_block_select_scratch_bytes() bytes of any content
+ * head_dim <= 128, at most 1024 key blocks.  drf_block_words and .._scratch_bytes give 0 for sizes that are refused.
+ */
+size_t drf_block_words(int kv_tokens, int kv_block);
+size_t drf_block_select_scratch_bytes(const drf_attn_shape* shape, int q_block, int kv_block);
+drf_status drf_block_select(const drf_attn_shape* shape, int q_block, int kv_block, int topk, const drf_heads* q,
+                            const drf_heads* k, void* scratch, size_t scratch_bytes, uint32_t* blocks, void* hip_stream);
+
+/*
+ * out = softmax(scale q k^T) v over the keys of the blocks that `blocks` gives each query block (its layout as above; the
+ * caller's own choice as well as drf_block_select's; bits of blocks beyond the keys do not count).  A query with no key gives
+ * zeros.  Rows of out behind a slot's q length are left as they were; keys and values behind its kv length, and of blocks
+ * not chosen, are not looked at.  out overlaps no input.
+ * head_dim <= 128; DRF_BF16: head_dim % 8 == 0, 16-byte aligned tensors, strides % 8 == 0.  token strides below 2^24.
+ */
+drf_status drf_block_attention(const drf_attn_shape* shape, int q_block, int kv_block, float scale, const uint32_t* blocks,
+                               const drf_heads* q, const drf_heads* k, const drf_heads* v, const drf_heads* out, void* hip_stream);
+
 /* HOST, thread-local, valid until the next failing call on this thread. */
 const char* drf_last_error(void);
 

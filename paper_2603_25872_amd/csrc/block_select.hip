@@ -1,0 +1,273 @@
+// The key blocks that each block of queries attends to: sums of the rows of every block in double precision, their products, and the topk
+// largest of each row of products.
+//
+// Which blocks are chosen must not depend on the order of a sum, so nothing before the comparison is narrower than 64 bits (a sum of
+// bf16 rows is then exact unless their exponents lie 37 apart), and equal scores go to the lower block.
+// The first launch reads q and k once and is bound by that; the sums, 1 / block of it, stay in the L2s for the second.
+#include <type_traits>
+
+#include "common.h"
+
+namespace drf {
+
+namespace {
+
+typedef double f64x4 __attribute__((ext_vector_type(4)));
+
+constexpr int kMaxD = 128, kThreads = 256, kWaves = kThreads / 64;
+constexpr int kMaxBlocks = 1024;            // key blocks: 16 rows of scores fill 128 of a CU's 160 KB of LDS
+
+struct PoolSide {
+    const void* x;
+    int64_t xs, xt, xh;
+    int tokens, heads, block, blocks;
+    const int32_t* lens;
+    double* out;        // [slot][head][block / 16][k-step][64]: operand fragments of the 16 x 16 x 4 product, lane 16 (c % 4) + block % 16 of k-step c / 4
+};
+
+__device__ inline int slot_len(const int32_t* lens, int slot, int tokens)
+{
+    if (!lens) return tokens;
+    const int n = lens[slot];
+    return n < 0 ? 0 : n < tokens ? n : tokens;
+}
+
+__device__ inline size_t fragment(int block, int c, int ksteps)
+{
+    return ((size_t)(block >> 4) * ksteps + (c >> 2)) * 64 + 16 * (c & 3) + (block & 15);
+}
+
+// A wave takes a head of a block: 64 / P rows at a time in pieces of 16 bytes (VEC), or a row at a time, a column or two a lane.
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(kThreads) pool_kernel(const PoolSide q, const PoolSide k, int d, int q_groups, int parts)
+{
+    constexpr int E = VEC ? 16 / (int)sizeof(T) : 2;
+    typedef T piece __attribute__((ext_vector_type(16 / sizeof(T))));
+    __shared__ double part_sums[kWaves][64 * (16 / sizeof(T))];
+    int id = blockIdx.x;
+    const bool is_k = id >= q_groups;
+    const PoolSide& s = is_k ? k : q;
+    if (is_k) id -= q_groups;
+    const int part = id % parts;
+    id /= parts;
+    const int slot = id / s.blocks, block = id - slot * s.blocks, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int len = slot_len(s.lens, slot, s.tokens), n0 = block * s.block, end = n0 + s.block < len ? n0 + s.block : len;
+    const int ksteps = (d + 3) / 4, tiles = (s.blocks + 15) / 16;
+    for (int h = part * kWaves + wave; h < s.heads; h += parts * kWaves) {
+        const T* x = (const T*)s.x + slot * s.xs + h * s.xh;
+        double* out = s.out + ((size_t)slot * s.heads + h) * tiles * ksteps * 64;
+        double sum[E];
+#pragma unroll
+        for (int j = 0; j < E; ++j) sum[j] = 0.0;
+        if constexpr (VEC) {
+            const int P = d / E, rpw = 64 / P, lr = lane / P, lp = lane - lr * P;
+            if (lr < rpw)
+                for (int n = n0 + lr; n < end; n += rpw) {
+                    const piece v = *reinterpret_cast<const piece*>(x + (int64_t)n * s.xt + lp * E);
+#pragma unroll
+                    for (int j = 0; j < E; ++j) sum[j] += (double)(float)v[j];
+                }
+            double* mine = part_sums[wave];                     // (a wave's LDS operations complete in order)
+#pragma unroll
+            for (int j = 0; j < E; ++j) mine[lane * E + j] = sum[j];
+            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+            for (int c = lane; c < 4 * ksteps; c += 64) {
+                double t = 0.0;
+                if (c < d)
+                    for (int r = 0; r < rpw; ++r) t += mine[r * d + c];
+                out[fragment(block, c, ksteps)] = t;
+            }
+            __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+        } else {
+            for (int n = n0; n < end; ++n)
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+                    if (lane + 64 * j < d) sum[j] += (double)(float)x[(int64_t)n * s.xt + lane + 64 * j];
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+                if (lane + 64 * j < 4 * ksteps) out[fragment(block, lane + 64 * j, ksteps)] = sum[j];
+        }
+    }
+}
+
+// Unsigned keys in the order of the scores, none of them 0; one that is not a number below all.
+__device__ inline uint64_t key_of(double v)
+{
+    if (v != v) return 1;
+    v += 0.0;                                                   // -0 and 0 are equal
+    const uint64_t u = __builtin_bit_cast(uint64_t, v);
+    return u >> 63 ? ~u : u | 0x8000000000000000ull;
+}
+
+struct SelectArgs {
+    const double *q, *k;
+    int q_tokens, kv_tokens, q_heads, group, q_block, kv_block, nq, nk, ksteps, topk, words;
+    const int32_t *q_lens, *kv_lens;
+    uint32_t* blocks;
+};
+
+// A workgroup takes 16 query blocks of a (slot, head): their scores against all key blocks on the 16 x 16 x 4 matrix instruction into LDS,
+// then a wave a row: the topk-th largest key by bisection over its bits (counting by ballots, until a bound splits off exactly topk), the
+// keys above it and of those equal to it the lowest blocks.  NK: keys a lane holds.
+template <int NK>
+__global__ void __launch_bounds__(kThreads) select_kernel(const SelectArgs a)
+{
+    extern __shared__ __attribute__((aligned(16))) double score[];          // [16][nk padded]
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int qtiles = (a.nq + 15) / 16, ktiles = (a.nk + 15) / 16, ld = ktiles * 16 + 2;
+    const int qt = blockIdx.x % qtiles, sh = blockIdx.x / qtiles, slot = sh / a.q_heads, h = sh - slot * a.q_heads;
+    const int q_len = slot_len(a.q_lens, slot, a.q_tokens), kv_len = slot_len(a.kv_lens, slot, a.kv_tokens);
+    const int n_valid = (kv_len + a.kv_block - 1) / a.kv_block;             // key blocks that hold a key
+    const double* q = a.q + ((size_t)sh * qtiles + qt) * a.ksteps * 64 + lane;
+    const double* k = a.k + ((size_t)slot * (a.q_heads / a.group) + h / a.group) * ktiles * a.ksteps * 64 + lane;
+    for (int t = wave; t < ktiles; t += kWaves) {
+        const double* kt = k + (size_t)t * a.ksteps * 64;
+        f64x4 acc = { 0.0, 0.0, 0.0, 0.0 };
+        for (int s = 0; s < a.ksteps; ++s) acc = __builtin_amdgcn_mfma_f64_16x16x4f64(q[s * 64], kt[s * 64], acc, 0, 0, 0);
+        // lane l holds column l % 16 of rows l / 16 + 4 r
+        const int j = t * 16 + (lane & 15), left = kv_len - j * a.kv_block, count = left < a.kv_block ? left : a.kv_block;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) score[((lane >> 4) + 4 * r) * ld + j] = count > 0 ? acc[r] / (double)count : 0.0;
+    }
+    __syncthreads();
+    for (int r = wave; r < 16; r += kWaves) {
+        const int i = qt * 16 + r;
+        if (i >= a.nq) break;
+        const int want = i * a.q_block >= q_len ? 0 : a.topk < n_valid ? a.topk : n_valid;
+        uint64_t key[NK];
+#pragma unroll
+        for (int c = 0; c < NK; ++c) key[c] = c * 64 + lane < n_valid ? key_of(score[r * ld + c * 64 + lane]) : 0;
+        uint64_t least = 0;
+        int above = n_valid;                                                // keys >= least
+        if (want > 0 && want < n_valid) {
+            for (int b = 63; b >= 0 && above != want; --b) {
+                const uint64_t bound = least | 1ull << b;
+                int n = 0;
+#pragma unroll
+                for (int c = 0; c < NK; ++c) n += __popcll(__ballot(key[c] >= bound));
+                if (n >= want) { least = bound; above = n; }
+            }
+        }
+        // keys > least are all chosen; of those equal to it the first that are still wanted
+        int equal = 0;
+        if (above != want) {
+            int more = 0;
+#pragma unroll
+            for (int c = 0; c < NK; ++c) more += __popcll(__ballot(key[c] > least));
+            equal = want - more;
+        }
+        uint32_t* out = a.blocks + ((size_t)sh * a.nq + i) * a.words;
+#pragma unroll
+        for (int c = 0; c < NK; ++c) {
+            bool in = key[c] != 0 && key[c] >= least;
+            if (above != want) {
+                const uint64_t same = __ballot(key[c] == least && key[c] != 0);
+                const int before = __popcll(same & ((1ull << lane) - 1));
+                in = key[c] > least || (key[c] == least && key[c] != 0 && before < equal);
+                const int here = __popcll(same);
+                equal = equal > here ? equal - here : 0;
+            }
+            const uint64_t word = want > 0 ? __ballot(in) : 0;
+            if (lane < 2 && 2 * c + lane < a.words) out[2 * c + lane] = (uint32_t)(word >> (32 * lane));
+        }
+    }
+}
+
+bool block_size(int b) { return b == 32 || b == 64 || b == 128; }
+
+drf_status check_select(const drf_attn_shape* s, int q_block, int kv_block)
+{
+    if (!s) DRF_FAIL(DRF_EINVAL, "shape is NULL");
+    if (s->dtype != DRF_F32 && s->dtype != DRF_BF16) DRF_FAIL(DRF_EINVAL, "unknown dtype");
+    if (s->slots < 0 || s->q_tokens < 0 || s->kv_tokens < 0 || s->q_heads < 1 || s->kv_heads < 1 || s->head_dim < 1)
+        DRF_FAIL(DRF_EINVAL, "slots and tokens must be >= 0, heads and head_dim >= 1");
+    if (s->q_heads % s->kv_heads) DRF_FAIL(DRF_ESHAPE, "%d query heads are no multiple of %d kv heads", s->q_heads, s->kv_heads);
+    if (s->head_dim > kMaxD) DRF_FAIL(DRF_ESHAPE, "head_dim must be <= %d (got %d)", kMaxD, s->head_dim);
+    if (!block_size(q_block) || !block_size(kv_block)) DRF_FAIL(DRF_EINVAL, "blocks of %d queries and %d keys: each must be 32, 64 or 128", q_block, kv_block);
+    return DRF_OK;
+}
+
+size_t side_bytes(int slots, int heads, int blocks, int d)
+{
+    return (size_t)slots * heads * ((blocks + 15) / 16) * ((d + 3) / 4) * 64 * sizeof(double);
+}
+
+template <int NK> drf_status launch_select(const SelectArgs& a, unsigned grid, size_t lds, hipStream_t st)
+{
+    auto kern = select_kernel<NK>;
+    static bool attr_set = false;
+    if (!attr_set) {
+        DRF_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, 16 * (64 * NK + 2) * (int)sizeof(double)));
+        attr_set = true;
+    }
+    hipLaunchKernelGGL(kern, dim3(grid), dim3(kThreads), lds, st, a);
+    DRF_HIP(hipGetLastError());
+    return DRF_OK;
+}
+
+}  // namespace
+
+}  // namespace drf
+
+using namespace drf;
+
+extern "C" size_t drf_block_words(int kv_tokens, int kv_block)
+{
+    if (kv_tokens < 0 || !block_size(kv_block)) return 0;
+    const long long blocks = ((long long)kv_tokens + kv_block - 1) / kv_block;
+    return (size_t)((blocks + 31) / 32);
+}
+
+extern "C" size_t drf_block_select_scratch_bytes(const drf_attn_shape* shape, int q_block, int kv_block)
+{
+    if (check_select(shape, q_block, kv_block) != DRF_OK) return 0;
+    const int nq = (int)(((long long)shape->q_tokens + q_block - 1) / q_block), nk = (int)(((long long)shape->kv_tokens + kv_block - 1) / kv_block);
+    return side_bytes(shape->slots, shape->q_heads, nq, shape->head_dim) + side_bytes(shape->slots, shape->kv_heads, nk, shape->head_dim);
+}
+
+extern "C" drf_status drf_block_select(const drf_attn_shape* shape, int q_block, int kv_block, int topk, const drf_heads* q,
+                                       const drf_heads* k, void* scratch, size_t scratch_bytes, uint32_t* blocks, void* hip_stream)
+{
+    drf_status rc = check_select(shape, q_block, kv_block);
+    if (rc != DRF_OK) return rc;
+    const drf_attn_shape& s = *shape;
+    if (topk < 1) DRF_FAIL(DRF_EINVAL, "topk must be >= 1 (got %d)", topk);
+    const int nq = (int)(((long long)s.q_tokens + q_block - 1) / q_block), nk = (int)(((long long)s.kv_tokens + kv_block - 1) / kv_block);
+    if (nk > kMaxBlocks) DRF_FAIL(DRF_ESHAPE, "%d key blocks exceed the %d that are compared", nk, kMaxBlocks);
+    if (s.slots == 0 || s.q_tokens == 0 || s.kv_tokens == 0) return DRF_OK;         // no row, or rows of no words
+    if (!q || !k || !q->data || !k->data || !blocks || !scratch) DRF_FAIL(DRF_EINVAL, "NULL buffer");
+    if ((reinterpret_cast<uintptr_t>(scratch) & 15u) != 0) DRF_FAIL(DRF_EINVAL, "scratch must be 16-byte aligned");
+    const size_t q_bytes = side_bytes(s.slots, s.q_heads, nq, s.head_dim), need = q_bytes + side_bytes(s.slots, s.kv_heads, nk, s.head_dim);
+    if (scratch_bytes < need) DRF_FAIL(DRF_EINVAL, "scratch of %zu bytes, %zu are needed", scratch_bytes, need);
+    hipStream_t st = (hipStream_t)hip_stream;
+
+    const int unit = s.dtype == DRF_BF16 ? 8 : 4;
+    bool vec = s.head_dim % unit == 0;
+    auto side = [&](const drf_heads* t, int tokens, int heads, int block, int n, const int32_t* lens, double* out) {
+        vec = vec && (reinterpret_cast<uintptr_t>(t->data) & 15u) == 0 && t->slot_stride % unit == 0 && t->token_stride % unit == 0 && t->head_stride % unit == 0;
+        return PoolSide{ t->data, t->slot_stride, t->token_stride, t->head_stride, tokens, heads, block, n, lens, out };
+    };
+    double* q_sums = (double*)scratch;
+    double* k_sums = (double*)((char*)scratch + q_bytes);
+    const PoolSide qs = side(q, s.q_tokens, s.q_heads, q_block, nq, s.q_lens, q_sums), ks = side(k, s.kv_tokens, s.kv_heads, kv_block, nk, s.kv_lens, k_sums);
+    int parts = 1;                                                          // workgroups over the heads of a block
+    while (parts * kWaves < s.q_heads && (long long)s.slots * (nq + nk) * parts < 2048) parts *= 2;
+    const long long q_groups = (long long)s.slots * nq * parts, groups = q_groups + (long long)s.slots * nk * parts;
+    const long long rows = (long long)s.slots * s.q_heads * ((nq + 15) / 16);
+    if (groups > 0x7fffffLL || rows > 0x7fffffLL) DRF_FAIL(DRF_ESHAPE, "too many blocks");
+    auto pool = [&](auto kern) { hipLaunchKernelGGL(kern, dim3((unsigned)groups), dim3(kThreads), 0, st, qs, ks, s.head_dim, (int)q_groups, parts); };
+    if (s.dtype == DRF_BF16) vec ? pool(pool_kernel<bf16_t, true>) : pool(pool_kernel<bf16_t, false>);
+    else vec ? pool(pool_kernel<float, true>) : pool(pool_kernel<float, false>);
+    DRF_HIP(hipGetLastError());
+
+    SelectArgs a{};
+    a.q = q_sums; a.k = k_sums; a.q_tokens = s.q_tokens; a.kv_tokens = s.kv_tokens; a.q_heads = s.q_heads; a.group = s.q_heads / s.kv_heads;
+    a.q_block = q_block; a.kv_block = kv_block; a.nq = nq; a.nk = nk; a.ksteps = (s.head_dim + 3) / 4; a.topk = topk;
+    a.words = (int)drf_block_words(s.kv_tokens, kv_block); a.q_lens = s.q_lens; a.kv_lens = s.kv_lens; a.blocks = blocks;
+    const size_t lds = (size_t)16 * ((nk + 15) / 16 * 16 + 2) * sizeof(double);
+    if (nk <= 64) return launch_select<1>(a, (unsigned)rows, lds, st);
+    if (nk <= 128) return launch_select<2>(a, (unsigned)rows, lds, st);
+    if (nk <= 256) return launch_select<4>(a, (unsigned)rows, lds, st);
+    if (nk <= 512) return launch_select<8>(a, (unsigned)rows, lds, st);
+    return launch_select<16>(a, (unsigned)rows, lds, st);
+}

@@ -19,12 +19,15 @@ COND_VECTOR, COND_CLASS, COND_TEXT = 0, 1, 2
 PLAN_ROW = 5
 PROF_GEMM, PROF_ATTN, PROF_ELEMWISE, PROF_UPDATE, PROF_PASS_FULL, PROF_PASS_OTHER = 0, 1, 2, 3, 4, 5
 DDIM, DDPM, EULER = 0, 1, 2
+ROPE_PAIRS, ROPE_HALVES = 0, 1
+QK_NONE, QK_RMS, QK_LAYER = 0, 1, 2
 
 # include/drf.h: the method's calls
 SYMBOLS = ["drf_denoiser_weight_count", "drf_denoiser_create", "drf_denoiser_destroy", "drf_denoiser_reserve", "drf_denoiser_use_graphs",
            "drf_eps_batched", "drf_eps_batched_static", "drf_skip_transition", "drf_refine_step", "drf_sample",
            "drf_skip_transition_noise", "drf_normal_fill", "drf_sample_noise", "drf_noise_count",
-           "drf_plan_build", "drf_last_error"]
+           "drf_plan_build", "drf_last_error",
+           "drf_rope", "drf_qk_norm_rope", "drf_block_words", "drf_block_select_scratch_bytes", "drf_block_select", "drf_block_attention"]
 # include/drf_measure.h: test and measurement hooks
 MEASURE_SYMBOLS = ["drf_eps_trace", "drf_profile_enable", "drf_profile_read", "drf_probe_gemm_bf16",
                    "drf_probe_attn_bf16", "drf_probe_cross_attn_bf16", "drf_probe_attn_route", "drf_probe_gemm_route", "drf_probe_block_route", "drf_probe_update_fused", "drf_graph_stats", "drf_calibrate_mfma_bf16", "drf_calibrate_copy"]
@@ -43,6 +46,24 @@ class SchedConfig(C.Structure):
 
 class Noise(C.Structure):
     _fields_ = [("z", C.c_void_p), ("seed", C.c_uint64), ("field0", C.c_uint32)]
+
+
+class Heads(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("slot_stride", C.c_int64), ("token_stride", C.c_int64), ("head_stride", C.c_int64)]
+
+
+class AttnShape(C.Structure):
+    _fields_ = [(k, C.c_int) for k in ("dtype", "slots", "q_tokens", "kv_tokens", "q_heads", "kv_heads", "head_dim")] + [
+        ("q_lens", C.c_void_p), ("kv_lens", C.c_void_p)]
+
+
+class RopeConfig(C.Structure):
+    _fields_ = [("n_axes", C.c_int), ("dim", C.c_int * 3), ("extent", C.c_int * 3), ("origin", C.c_double * 3), ("step", C.c_double * 3),
+                ("theta", C.c_double), ("layout", C.c_int)]
+
+
+class QkConfig(C.Structure):
+    _fields_ = [("norm", C.c_int), ("eps", C.c_double), ("q_scale", C.c_float)] + [(k, C.c_void_p) for k in ("q_gain", "q_bias", "k_gain", "k_bias")]
 
 
 class DrfError(RuntimeError):
@@ -101,6 +122,13 @@ def lib():
         L.drf_probe_block_route.argtypes = [C.c_int] * 5
         L.drf_probe_gemm_route.argtypes = [C.c_int] * 5 + [C.c_void_p]
         L.drf_last_error.restype = C.c_char_p
+        L.drf_rope.argtypes = [C.c_void_p] + [C.c_int] * 5 + [C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p, C.c_void_p, C.c_void_p]
+        L.drf_qk_norm_rope.argtypes = [C.c_void_p] * 4 + [C.c_size_t] + [C.c_void_p] * 5
+        L.drf_block_words.restype = L.drf_block_select_scratch_bytes.restype = C.c_size_t
+        L.drf_block_words.argtypes = [C.c_int, C.c_int]
+        L.drf_block_select_scratch_bytes.argtypes = [C.c_void_p, C.c_int, C.c_int]
+        L.drf_block_select.argtypes = [C.c_void_p] + [C.c_int] * 3 + [C.c_void_p] * 3 + [C.c_size_t, C.c_void_p, C.c_void_p]
+        L.drf_block_attention.argtypes = [C.c_void_p, C.c_int, C.c_int, C.c_float] + [C.c_void_p] * 6
         try:
             from . import _native               # built beside the library
             _native.bind(C.cast(L.drf_skip_transition_noise, C.c_void_p).value)
@@ -238,6 +266,140 @@ def refine_step(sched, x, eps, s_from, out=None):
         out = torch.empty_like(x)
     _check(lib().drf_refine_step(C.byref(sc), _dev(x, torch.float32), _dev(eps, torch.float32), s_from, batch,
                                  x.numel() // batch if batch else 0, _dev(out, torch.float32), _stream()))
+    return out
+
+
+def _dtype_of(t):
+    """drf_dtype of a tensor of heads."""
+    import torch
+    if t.dtype == torch.bfloat16:
+        return BF16
+    assert t.dtype == torch.float32, "expected bfloat16 or float32, got %s" % t.dtype
+    return F32
+
+
+def _heads(t, like=None):
+    """drf_heads of a device tensor [slots, tokens, heads, head_dim] whose head columns are contiguous."""
+    assert t.is_cuda and t.dim() == 4, "need a device tensor [slots, tokens, heads, head_dim]"
+    ss, ts, hs, cs = t.stride()
+    assert cs == 1 or t.shape[3] < 2, "a head's columns must be contiguous"
+    if like is not None:
+        assert t.dtype == like.dtype, "expected %s, got %s" % (like.dtype, t.dtype)
+        assert t.device == like.device, "tensors on %s and %s" % (like.device, t.device)
+    return Heads(t.data_ptr(), ss, ts, hs)
+
+
+def _current(t):
+    """The library launches on the current device: a tensor that is on another one is refused."""
+    import torch
+    assert t.is_cuda and t.device.index == torch.cuda.current_device(), "the tensor is on %s, which is not the current device" % t.device
+
+
+def _vector(t, n, dtype, what):
+    """Device pointer of a contiguous vector of n elements, or None."""
+    if t is not None:
+        assert t.shape == (n,), "%s must have shape (%d,)" % (what, n)
+    return _dev(t, dtype)
+
+
+def _positions(positions, rope, slots, tokens):
+    """(device pointer, stride between slots) of a table [tokens, axes] or [slots, tokens, axes]."""
+    import torch
+    if positions is None:
+        return None, 0
+    want = (tokens, rope.n_axes)
+    assert tuple(positions.shape) in (want, (slots,) + want), "positions must be [tokens, axes] or [slots, tokens, axes]"
+    return _dev(positions, torch.float32), tokens * rope.n_axes if positions.dim() == 3 else 0
+
+
+def rope_config(dims, extents, theta=10000.0, layout="pairs", origin=None, step=None):
+    """The rotation of rope() and qk_norm_rope(): columns, grid extent, origin and step of up to three axes (see include/drf.h)."""
+    n = len(dims)
+    if not 1 <= n <= 3 or len(extents) != n:
+        raise ValueError("one to three axes, with an extent for each")
+    rc = RopeConfig(n_axes=n, theta=float(theta), layout={"pairs": ROPE_PAIRS, "halves": ROPE_HALVES}[layout])
+    for a in range(n):
+        rc.dim[a], rc.extent[a] = int(dims[a]), int(extents[a])
+        rc.origin[a] = 0.0 if origin is None else float(origin[a])
+        rc.step[a] = 1.0 if step is None else float(step[a])
+    return rc
+
+
+def rope(x, config, positions=None, lens=None, out=None):
+    """x [slots, tokens, heads, head_dim] (any strides but the last) with its columns turned by their positions; out may be x."""
+    import torch
+    _current(x)
+    S, N, H, d = x.shape
+    if out is None:
+        out = torch.empty_like(x) if lens is None else x.clone()
+    assert out.shape == x.shape, "out must have the shape of x"
+    p, stride = _positions(positions, config, S, N)
+    _check(lib().drf_rope(C.byref(config), _dtype_of(x), S, N, H, d, _vector(lens, S, torch.int32, "lens"), p, stride, C.byref(_heads(x)),
+                          C.byref(_heads(out, x)), _stream()))
+    return out
+
+
+def qk_norm_rope(q, k, norm, config=None, q_gain=None, k_gain=None, q_bias=None, k_bias=None, eps=1e-6, q_scale=1.0, positions=None, lens=None,
+                 q_out=None, k_out=None):
+    """Norm ("none", "rms", "layer") of every head of q and k [slots, tokens, heads, head_dim], then the rotation; returns (q_out, k_out)."""
+    import torch
+    _current(q)
+    S, N, H, d = q.shape
+    assert k.shape[:2] == q.shape[:2] and k.shape[3] == d, "k must have the slots, tokens and head width of q"
+    if q_out is None:
+        q_out = torch.empty_like(q) if lens is None else q.clone()
+    if k_out is None:
+        k_out = torch.empty_like(k) if lens is None else k.clone()
+    assert q_out.shape == q.shape and k_out.shape == k.shape, "outputs must have the shapes of their inputs"
+    kind = {"none": QK_NONE, "rms": QK_RMS, "layer": QK_LAYER}[norm]
+    cfg = QkConfig(kind, float(eps), float(q_scale), *(_vector(t, d, torch.float32, what) for t, what in (
+        (q_gain, "q_gain"), (q_bias, "q_bias"), (k_gain, "k_gain"), (k_bias, "k_bias"))))
+    shape = AttnShape(_dtype_of(q), S, N, N, H, k.shape[2], d, _vector(lens, S, torch.int32, "lens"), None)
+    if positions is not None and config is None:
+        raise ValueError("positions without a rotation")
+    p, stride = _positions(positions, config, S, N)
+    _check(lib().drf_qk_norm_rope(C.byref(cfg), C.byref(config) if config is not None else None, C.byref(shape), p, stride, C.byref(_heads(q)),
+                                  C.byref(_heads(k, q)), C.byref(_heads(q_out, q)), C.byref(_heads(k_out, q)), _stream()))
+    return q_out, k_out
+
+
+def _shape(q, k, q_lens, kv_lens):
+    import torch
+    _current(q)
+    S, N, H, d = q.shape
+    assert k.shape[0] == S and k.shape[3] == d, "k must have the slots and head width of q"
+    return AttnShape(_dtype_of(q), S, N, k.shape[1], H, k.shape[2], d, _vector(q_lens, S, torch.int32, "q_lens"), _vector(kv_lens, S, torch.int32, "kv_lens"))
+
+
+def block_select(q, k, q_block, kv_block, topk, q_lens=None, kv_lens=None, out=None):
+    """Bit words [slots, heads, query blocks, words] (int32) of the topk key blocks whose mean lies nearest each query block's mean."""
+    import torch
+    shape = _shape(q, k, q_lens, kv_lens)
+    L = lib()
+    size = (shape.slots, shape.q_heads, -(-shape.q_tokens // q_block) if q_block > 0 else 0, L.drf_block_words(shape.kv_tokens, kv_block))
+    if out is None:
+        out = torch.empty(size, dtype=torch.int32, device=q.device)
+    assert tuple(out.shape) == size, "out must be %s" % (size,)
+    n = L.drf_block_select_scratch_bytes(C.byref(shape), q_block, kv_block)
+    scratch = torch.empty(n, dtype=torch.uint8, device=q.device)
+    _check(L.drf_block_select(C.byref(shape), q_block, kv_block, topk, C.byref(_heads(q)), C.byref(_heads(k, q)), scratch.data_ptr(), n,
+                              _dev(out, torch.int32), _stream()))
+    return out
+
+
+def block_attention(q, k, v, blocks, q_block, kv_block, scale=None, q_lens=None, kv_lens=None, out=None):
+    """softmax(scale q k^T) v over the key blocks that the words `blocks` (as block_select gives them) name for each query block; scale
+    1 / sqrt(head_dim) by default.  Rows behind a slot's q length are left as they were: zeros in an output made here."""
+    import torch
+    shape = _shape(q, k, q_lens, kv_lens)
+    assert v.shape == k.shape, "v must have the shape of k"
+    size = (shape.slots, shape.q_heads, -(-shape.q_tokens // q_block) if q_block > 0 else 0, lib().drf_block_words(shape.kv_tokens, kv_block))
+    assert tuple(blocks.shape) == size, "blocks must be %s" % (size,)
+    if out is None:
+        out = (torch.empty if q_lens is None else torch.zeros)(q.shape, dtype=q.dtype, device=q.device)
+    assert out.shape == q.shape, "out must have the shape of q"
+    _check(lib().drf_block_attention(C.byref(shape), q_block, kv_block, shape.head_dim ** -0.5 if scale is None else scale, _dev(blocks, torch.int32),
+                                     C.byref(_heads(q)), C.byref(_heads(k, q)), C.byref(_heads(v, q)), C.byref(_heads(out, q)), _stream()))
     return out
 
 
