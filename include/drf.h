@@ -407,6 +407,29 @@ drf_status drf_block_select(const drf_attn_shape* shape, int q_block, int kv_blo
 drf_status drf_block_attention(const drf_attn_shape* shape, int q_block, int kv_block, float scale, const uint32_t* blocks,
                                const drf_heads* q, const drf_heads* k, const drf_heads* v, const drf_heads* out, void* hip_stream);
 
+/*
+ * A denoiser whose self-attention has these operators in it.  Per block, in place of softmax(q k^T / sqrt(d)) v:
+ *   q, k = rotate(norm(q)), rotate(norm(k))      as drf_qk_norm_rope, token (row, column) of the patch grid at that position
+ *   out  = softmax(q k^T / sqrt(d)) v            over all keys (topk 0), or over the blocks that drf_block_select chooses
+ *                                                (drf_block_attention; token order is the patch grid's, row by row)
+ * Parameters: with DRF_QK_RMS q_gain [d], k_gain [d], with DRF_QK_LAYER q_gain, q_bias, k_gain, k_bias [d] each, in every block
+ * behind qkv_b.  additive_pos 0 leaves the sin-cos code of the tokens out.  DRF_BF16: q and k are rounded to bf16 before the norm
+ * and after the rotation.
+ * Every other call takes the handle as any other.  attn NULL, or one with nothing in it and additive_pos 1, is drf_denoiser_create.
+ */
+typedef struct {
+    drf_qk_norm qk_norm;
+    double norm_eps;
+    int rope_dim[2];                /* columns of a head that turn with the token's row, and with its column; 0, 0: none */
+    double rope_theta;              /* > 0 where anything turns */
+    drf_rope_layout rope_layout;
+    int additive_pos;
+    int q_block, kv_block, topk;    /* topk 0: every query attends to every key, and the block sizes are not looked at */
+} drf_attn_config;
+size_t drf_denoiser_weight_count_attn(const drf_dit_config* cfg, const drf_attn_config* attn);
+drf_status drf_denoiser_create_attn(const drf_dit_config* cfg, const drf_attn_config* attn, const float* host_weights, size_t count,
+                                    void* hip_stream, drf_denoiser** out);
+
 /* HOST, thread-local, valid until the next failing call on this thread. */
 const char* drf_last_error(void);
 

@@ -23,7 +23,10 @@ struct LinearW {
     int N = 0, K = 0;
 };
 
-struct BlockW { LinearW qkv, proj, xq, xkv, xo, fc1, fc2; };
+struct BlockW {
+    LinearW qkv, proj, xq, xkv, xo, fc1, fc2;
+    const float *q_gain = nullptr, *q_bias = nullptr, *k_gain = nullptr, *k_bias = nullptr;     // of the norms of q and k
+};
 
 // Device buffers of one batched pass beyond the caller's inputs and outputs: activations, the
 // conditioning front-end's rows and the modulation table, the K/V of a text context.  Either owned by
@@ -32,6 +35,7 @@ struct Workspace {
     float *resid = nullptr, *mod = nullptr, *cact32 = nullptr, *cscratch = nullptr;
     void *hbuf = nullptr, *qkv = nullptr, *mid = nullptr, *ybuf = nullptr, *ybuf2 = nullptr, *cact = nullptr;
     void *xkv = nullptr, *ctx_act = nullptr;    // cross-attention K/V cache [L][rows][ctx_len][2D] and its staging
+    void* sel = nullptr;                        // sums that the choice of key blocks compares, then the chosen blocks' words
     float* skpart = nullptr;                    // partial tiles of the split-K GEMM (bf16 path), or NULL: no split
 };
 
@@ -58,6 +62,8 @@ struct drf_denoiser {
     drf_dit_config cfg{};
     DitDims dm{};
     bool bf16 = false;
+    drf_attn_config attn{};         // operators in the self-attention; see drf_denoiser_create_attn
+    bool qk_pass = false;           // norms or rotation between the qkv Linear and the attention
     int n_mod = 0;                  // 6 L D + 2 D modulation columns per slot
     std::vector<void*> allocs;      // everything freed at destroy
     // parameters on the device
@@ -137,7 +143,53 @@ drf_status check_config(const drf_dit_config* c)
     return DRF_OK;
 }
 
-size_t weight_count(const drf_dit_config* c)
+// The rotation of the patch grid's rows and columns.
+drf_rope_config rope_of(const drf_dit_config* c, const drf_attn_config* a)
+{
+    drf_rope_config r{};
+    r.n_axes = 2;
+    for (int i = 0; i < 2; ++i) { r.dim[i] = a->rope_dim[i]; r.step[i] = 1.0; }
+    r.extent[0] = c->lat_h / c->patch; r.extent[1] = c->lat_w / c->patch;
+    r.theta = a->rope_theta; r.layout = a->rope_layout;
+    return r;
+}
+
+// Sizes of the self-attention over `slots` slots.
+drf_attn_shape shape_of(const drf_dit_config* c, int slots)
+{
+    drf_attn_shape s{};
+    s.dtype = c->dtype; s.slots = slots;
+    s.q_tokens = s.kv_tokens = (c->lat_h / c->patch) * (c->lat_w / c->patch);
+    s.q_heads = s.kv_heads = c->heads; s.head_dim = c->hidden / c->heads;
+    return s;
+}
+
+// (after check_config)  The operators check their own arguments before they look at buffers: calls of no slots do that.
+drf_status check_attn(const drf_dit_config* c, const drf_attn_config* a)
+{
+    if (!a) return DRF_OK;
+    const drf_attn_shape shape = shape_of(c, 0);
+    if (a->additive_pos != 0 && a->additive_pos != 1) DRF_FAIL(DRF_EINVAL, "additive_pos must be 0 or 1");
+    if (a->rope_dim[0] < 0 || a->rope_dim[1] < 0) DRF_FAIL(DRF_EINVAL, "rope_dim must be >= 0");
+    const bool turns = a->rope_dim[0] || a->rope_dim[1];
+    const drf_rope_config rope = rope_of(c, a);
+    drf_qk_config qk{};
+    qk.norm = a->qk_norm; qk.eps = a->qk_norm == DRF_QK_NONE ? 0.0 : a->norm_eps; qk.q_scale = 1.f;
+    drf_status rc = drf_qk_norm_rope(&qk, turns ? &rope : nullptr, &shape, nullptr, 0, nullptr, nullptr, nullptr, nullptr, nullptr);
+    if (rc != DRF_OK) return rc;
+    if (a->topk < 0) DRF_FAIL(DRF_EINVAL, "topk must be >= 0");
+    if (a->topk == 0) return DRF_OK;
+    return drf_block_select(&shape, a->q_block, a->kv_block, a->topk, nullptr, nullptr, nullptr, 0, nullptr, nullptr);
+}
+
+// Norm parameters of q and k together, per block.
+size_t norm_count(const drf_dit_config* c, const drf_attn_config* a)
+{
+    const size_t d = (size_t)(c->hidden / c->heads);
+    return !a || a->qk_norm == DRF_QK_NONE ? 0 : a->qk_norm == DRF_QK_RMS ? 2 * d : 4 * d;
+}
+
+size_t weight_count(const drf_dit_config* c, const drf_attn_config* a)
 {
     const size_t D = (size_t)c->hidden, P = (size_t)c->in_ch * c->patch * c->patch, R = (size_t)c->mlp_ratio;
     size_t n = D * P + D + D * kTFreq + D + D * D + D;
@@ -145,7 +197,7 @@ size_t weight_count(const drf_dit_config* c)
     else if (c->cond == DRF_COND_CLASS) n += ((size_t)c->cond_dim + 1) * D;
     size_t per = 6 * D * D + 6 * D + 3 * D * D + 3 * D + D * D + D + R * D * D + R * D + D * R * D + D;
     if (c->cond == DRF_COND_TEXT) per += D * D + D + 2 * D * (size_t)c->cond_dim + 2 * D + D * D + D;
-    n += per * (size_t)c->depth;
+    n += (per + norm_count(c, a)) * (size_t)c->depth;
     n += 2 * D * D + 2 * D + P * D + P;
     return n;
 }
@@ -184,7 +236,7 @@ struct ProfScope {
 
 // Sizes (bytes) of the Workspace members for a pass of `slots` slots, `cond_rows` conditioning rows and
 // `ctx_rows` distinct text contexts: one table both the owned and the static workspace are built from.
-struct WorkspaceBytes { size_t resid, hbuf, qkv, mid, ybuf, ybuf2, mod, cact32, cscratch, cact, xkv, ctx_act; };
+struct WorkspaceBytes { size_t resid, hbuf, qkv, mid, ybuf, ybuf2, mod, cact32, cscratch, cact, xkv, ctx_act, sel, sel_sums; };
 WorkspaceBytes workspace_bytes(const drf_denoiser* d, size_t slots, size_t cond_rows, size_t ctx_rows)
 {
     const size_t M = slots * d->dm.T, D = (size_t)d->dm.D, act = d->bf16 ? 2 : 4;
@@ -196,6 +248,11 @@ WorkspaceBytes workspace_bytes(const drf_denoiser* d, size_t slots, size_t cond_
     if (d->cfg.cond == DRF_COND_TEXT) {
         const size_t rl = ctx_rows * d->cfg.ctx_len;
         b.xkv = (size_t)d->dm.L * rl * 2 * D * act; b.ctx_act = rl * d->cfg.cond_dim * act;
+    }
+    if (d->attn.topk > 0 && slots > 0) {
+        const drf_attn_shape s = shape_of(&d->cfg, (int)slots);
+        b.sel_sums = drf_block_select_scratch_bytes(&s, d->attn.q_block, d->attn.kv_block);
+        b.sel = b.sel_sums + slots * d->dm.heads * ((d->dm.T + d->attn.q_block - 1) / d->attn.q_block) * drf_block_words(d->dm.T, d->attn.kv_block) * 4;
     }
     return b;
 }
@@ -209,7 +266,7 @@ drf_status ensure_workspace(drf_denoiser* d, int slots, hipStream_t st)
     Workspace& w = d->ws;
     d->cap_slots = 0;
     ++d->ws_gen;
-    dev_free(d, &w.resid); dev_free(d, &w.hbuf); dev_free(d, &w.qkv); dev_free(d, &w.mid); dev_free(d, &w.ybuf); dev_free(d, &w.ybuf2);
+    dev_free(d, &w.resid); dev_free(d, &w.hbuf); dev_free(d, &w.qkv); dev_free(d, &w.mid); dev_free(d, &w.ybuf); dev_free(d, &w.ybuf2); dev_free(d, &w.sel);
     const WorkspaceBytes b = workspace_bytes(d, (size_t)slots, 0, 0);
     drf_status rc;
     if (d->bf16 && !w.skpart && (rc = dev_alloc(d, (void**)&w.skpart, gemm_splitk_scratch_bytes())) != DRF_OK) return rc;
@@ -219,6 +276,7 @@ drf_status ensure_workspace(drf_denoiser* d, int slots, hipStream_t st)
     if ((rc = dev_alloc(d, &w.mid, b.mid)) != DRF_OK) return rc;
     if ((rc = dev_alloc(d, &w.ybuf, b.ybuf)) != DRF_OK) return rc;
     if ((rc = dev_alloc(d, &w.ybuf2, b.ybuf2)) != DRF_OK) return rc;
+    if (b.sel && (rc = dev_alloc(d, &w.sel, b.sel)) != DRF_OK) return rc;
     d->cap_slots = slots;
     return DRF_OK;
 }
@@ -274,13 +332,16 @@ Epilogue epi_store(void* out, int ldo, bool f32, bool gelu = false)
     return e;
 }
 
-Epilogue epi_heads(void* out, int slots, const DitDims& dm)
+// Factor that the attention wants its queries multiplied by before they are rounded.
+float wanted_q_scale(const DitDims& dm, int slots) { return attn_wants_scaled(dm.T, dm.heads, dm.d, slots) ? 1.4426950408889634f / sqrtf((float)dm.d) : 1.f; }
+
+Epilogue epi_heads(void* out, int slots, const DitDims& dm, float q_scale)
 {
     Epilogue e{};
     e.mode = EPI_STORE_HEADS; e.out = out; e.ldo = 3 * dm.D; e.out_f32 = 0;
     set_rows_per_slot(&e, dm.T);
     e.hid = dm.D; e.hd = dm.d; e.heads = dm.heads; e.plane = (size_t)slots * dm.T * dm.D;
-    e.q_scale = attn_wants_scaled(dm.T, dm.heads, dm.d, slots) ? 1.4426950408889634f / sqrtf((float)dm.d) : 1.f;
+    e.q_scale = q_scale;
     make_fast_div(dm.D, &e.hid_magic, &e.hid_shift);
     make_fast_div(dm.d, &e.hd_magic, &e.hd_shift);
     return e;
@@ -414,7 +475,39 @@ drf_status forward(drf_denoiser* d, const Workspace& ws, const float* x, const S
         const drf_status r = ln(shift, scale, mod_ld, store);
         return r != DRF_OK ? r : gemm(d, ws.hbuf, w, M, ep, st, ws.skpart);
     };
+    // q | k | v of the pass as tensors of heads, and the attention's output
+    const int64_t token = f32 ? 3 * D : dm.d, head = f32 ? dm.d : (int64_t)dm.T * dm.d, slot_rows = (int64_t)dm.T * (f32 ? 3 * D : D);
+    auto part_of_qkv = [&](int which) {
+        return drf_heads{ (char*)ws.qkv + (size_t)which * (f32 ? (size_t)D : (size_t)M * D) * act, slot_rows, token, head };
+    };
+    const drf_attn_shape shape = shape_of(&d->cfg, slots);
+    const bool sparse = d->attn.topk > 0;
+    const float q_scale = f32 || sparse ? 1.f : wanted_q_scale(dm, slots);
+    // norms and rotation of block l's q and k, in place
+    auto qk_pass = [&](const BlockW& b) -> drf_status {
+        if (!d->qk_pass) return DRF_OK;
+        drf_qk_config qc{};
+        qc.norm = d->attn.qk_norm; qc.eps = d->attn.qk_norm == DRF_QK_NONE ? 0.0 : d->attn.norm_eps; qc.q_scale = q_scale;
+        qc.q_gain = b.q_gain; qc.q_bias = b.q_bias; qc.k_gain = b.k_gain; qc.k_bias = b.k_bias;
+        const drf_rope_config rope = rope_of(&d->cfg, &d->attn);
+        const drf_heads q = part_of_qkv(0), k = part_of_qkv(1);
+        ProfScope ps(d, st, DRF_PROF_ELEMWISE, 4.0 * M * D * (double)act);
+        return drf_qk_norm_rope(&qc, rope.dim[0] || rope.dim[1] ? &rope : nullptr, &shape, nullptr, 0, &q, &k, &q, &k, st);
+    };
+    auto block_attention = [&]() -> drf_status {
+        const drf_heads q = part_of_qkv(0), k = part_of_qkv(1), v = part_of_qkv(2), out = { ws.hbuf, (int64_t)dm.T * D, D, dm.d };
+        const size_t sums = drf_block_select_scratch_bytes(&shape, d->attn.q_block, d->attn.kv_block);
+        uint32_t* words = (uint32_t*)((char*)ws.sel + sums);
+        {
+            ProfScope ps(d, st, DRF_PROF_ELEMWISE, 2.0 * M * D * (double)act);
+            const drf_status r = drf_block_select(&shape, d->attn.q_block, d->attn.kv_block, d->attn.topk, &q, &k, ws.sel, sums, words, st);
+            if (r != DRF_OK) return r;
+        }
+        ProfScope ps(d, st, DRF_PROF_ATTN, 4.0 * slots * dm.heads * (double)dm.T * std::min((double)d->attn.topk * d->attn.kv_block, (double)dm.T) * dm.d);
+        return drf_block_attention(&shape, d->attn.q_block, d->attn.kv_block, 1.f / sqrtf((float)dm.d), words, &q, &k, &v, &out, st);
+    };
     auto self_attention = [&]() -> drf_status {
+        if (sparse) return block_attention();
         AttnArgs aa{};
         aa.q = ws.qkv; aa.out = ws.hbuf; aa.ldo = D; aa.Nq = dm.T; aa.Nk = dm.T; aa.heads = dm.heads; aa.d = dm.d;
         aa.slots = slots; aa.kv_mod = 0;
@@ -426,7 +519,7 @@ drf_status forward(drf_denoiser* d, const Workspace& ws, const float* x, const S
             aa.k = (char*)ws.qkv + (size_t)M * D * act; aa.v = (char*)ws.qkv + (size_t)2 * M * D * act;
             aa.ldq = aa.ldk = dm.d;
             aa.q_slot_stride = aa.kv_batch_stride = (size_t)dm.T * D; aa.q_head_stride = aa.kv_head_stride = (size_t)dm.T * dm.d;
-            aa.q_scaled = attn_wants_scaled(dm.T, dm.heads, dm.d, slots);
+            aa.q_scaled = q_scale != 1.f;
         }
         ProfScope ps(d, st, DRF_PROF_ATTN, 4.0 * slots * dm.heads * (double)dm.T * dm.T * dm.d);
         return f32 ? launch_attn_f32(aa, st) : launch_attn_bf16(aa, st);
@@ -436,7 +529,7 @@ drf_status forward(drf_denoiser* d, const Workspace& ws, const float* x, const S
         // narrow models: everything of a block that works on its rows alone in one launch, and the self-attention before it too where that
         // pays; the keys and values that the launch writes for the next block are then others than those that it reads
         const size_t unit = (size_t)D * D, per_block = (4 + 2 * (size_t)dm.R) * unit;       // qkv | proj | (fc1, fc2) pieces
-        const Epilogue h = epi_heads(ws.qkv, slots, dm);
+        const Epilogue h = epi_heads(ws.qkv, slots, dm, q_scale);
         bf16_t* kv[2] = { (bf16_t*)ws.qkv, (bf16_t*)ws.mid };
         ChainArgs ca{};
         ca.resid = ws.resid; ca.mod_ld = nm; ca.tokens = dm.T; ca.slots = slots; ca.mlp_ratio = dm.R;
@@ -489,7 +582,8 @@ drf_status forward(drf_denoiser* d, const Workspace& ws, const float* x, const S
         const float* mrow = mod + (size_t)l * 6 * D;        // shift1 | scale1 | gate1 | shift2 | scale2 | gate2
         // bf16: q | k | v are stored head-major ([slot][head][token][d] planes) so that attention reads
         // whole contiguous tiles; fp32: packed rows
-        if ((rc = ln_linear(mrow, mrow + D, nm, true, b.qkv, f32 ? epi_store(ws.qkv, 3 * D, true) : with_warm(epi_heads(ws.qkv, slots, dm), &b.proj))) != DRF_OK) return rc;
+        if ((rc = ln_linear(mrow, mrow + D, nm, true, b.qkv, f32 ? epi_store(ws.qkv, 3 * D, true) : with_warm(epi_heads(ws.qkv, slots, dm, d->qk_pass ? 1.f : q_scale), &b.proj))) != DRF_OK) return rc;
+        if ((rc = qk_pass(b)) != DRF_OK) return rc;
         if ((rc = self_attention()) != DRF_OK) return rc;
         if (f32) {
             if ((rc = gemm(d, ws.hbuf, b.proj, M, epi_resid(ws.resid, D, mrow + 2 * D, nm, dm.T), st)) != DRF_OK) return rc;
@@ -535,11 +629,12 @@ drf_status forward(drf_denoiser* d, const Workspace& ws, const float* x, const S
 }
 
 // Algorithmic flops of one slot evaluation: 2 M N K of every Linear of the blocks and of the patch / final
-// projections, 4 T^2 D per self-attention (and 4 T ctx_len D per cross-attention), unpadded head width.
+// projections, 4 T^2 D per self-attention (of chosen blocks: 4 T keys D; and 4 T ctx_len D per cross-attention), unpadded head width.
 double slot_eval_flops(const drf_denoiser* d)
 {
     const double D = d->dm.D, T = d->dm.T, R = d->dm.R, P = d->dm.P;
-    double per = 2 * T * D * 3 * D + 2 * T * D * D + 2 * 2 * T * D * R * D + 4 * T * T * D;
+    const double keys = d->attn.topk > 0 ? std::min((double)d->attn.topk * d->attn.kv_block, T) : T;
+    double per = 2 * T * D * 3 * D + 2 * T * D * D + 2 * 2 * T * D * R * D + 4 * T * keys * D;
     if (d->cfg.cond == DRF_COND_TEXT) per += 2 * 2 * T * D * D + 4 * T * (double)d->cfg.ctx_len * D;
     return d->dm.L * per + 2 * 2 * T * D * P;
 }
@@ -595,6 +690,7 @@ drf_status carve_static(const drf_denoiser* d, int slots, Workspace* ws)
     ws->ybuf = take(b.ybuf); ws->ybuf2 = take(b.ybuf2);
     ws->mod = (float*)take(b.mod); ws->cact32 = (float*)take(b.cact32); ws->cscratch = (float*)take(b.cscratch); ws->cact = take(b.cact);
     ws->xkv = take(b.xkv); ws->ctx_act = take(b.ctx_act);
+    ws->sel = take(b.sel);
     if (off > (size_t)DRF_STATIC_SCRATCH_BYTES)
         DRF_FAIL(DRF_ESHAPE, "a pass of %d slots needs %zu bytes of scratch; the static array holds %zu", slots, off,
                  (size_t)DRF_STATIC_SCRATCH_BYTES);
@@ -752,18 +848,30 @@ drf_status eps_common(drf_denoiser* den, const float* x, const int32_t* t, const
 
 extern "C" size_t drf_denoiser_weight_count(const drf_dit_config* cfg)
 {
-    if (check_config(cfg) != DRF_OK) return 0;
-    return weight_count(cfg);
+    return drf_denoiser_weight_count_attn(cfg, nullptr);
+}
+
+extern "C" size_t drf_denoiser_weight_count_attn(const drf_dit_config* cfg, const drf_attn_config* attn)
+{
+    if (check_config(cfg) != DRF_OK || check_attn(cfg, attn) != DRF_OK) return 0;
+    return weight_count(cfg, attn);
 }
 
 extern "C" drf_status drf_denoiser_create(const drf_dit_config* cfg, const float* host_weights, size_t count,
                                           void* hip_stream, drf_denoiser** out)
 {
+    return drf_denoiser_create_attn(cfg, nullptr, host_weights, count, hip_stream, out);
+}
+
+extern "C" drf_status drf_denoiser_create_attn(const drf_dit_config* cfg, const drf_attn_config* attn, const float* host_weights, size_t count,
+                                               void* hip_stream, drf_denoiser** out)
+{
     drf_status rc = check_config(cfg);
     if (rc != DRF_OK) return rc;
+    if ((rc = check_attn(cfg, attn)) != DRF_OK) return rc;
     if (!host_weights || !out) DRF_FAIL(DRF_EINVAL, "NULL argument");
     *out = nullptr;
-    const size_t want = weight_count(cfg);
+    const size_t want = weight_count(cfg, attn);
     if (count != want) DRF_FAIL(DRF_EINVAL, "weight count %zu does not match configuration (%zu)", count, want);
     hipStream_t st = (hipStream_t)hip_stream;
     int ndev = 0;
@@ -772,6 +880,9 @@ extern "C" drf_status drf_denoiser_create(const drf_dit_config* cfg, const float
     drf_denoiser* d = new (std::nothrow) drf_denoiser();
     if (!d) DRF_FAIL(DRF_ENOMEM, "host allocation failed");
     d->cfg = *cfg;
+    d->attn.additive_pos = 1;
+    if (attn) d->attn = *attn;
+    d->qk_pass = d->attn.qk_norm != DRF_QK_NONE || d->attn.rope_dim[0] || d->attn.rope_dim[1];
     d->bf16 = cfg->dtype == DRF_BF16;
     DitDims& dm = d->dm;
     dm.D = cfg->hidden; dm.P = cfg->in_ch * cfg->patch * cfg->patch; dm.gh = cfg->lat_h / cfg->patch; dm.gw = cfg->lat_w / cfg->patch;
@@ -812,6 +923,12 @@ extern "C" drf_status drf_denoiser_create(const drf_dit_config* cfg, const float
         BlockW& b = d->blk[(size_t)l];
         ada_w_off[(size_t)l] = off; take(6 * D * D); ada_b_off[(size_t)l] = off; take(6 * D);
         take_linear(&b.qkv, 3 * D, D);
+        if (d->attn.qk_norm != DRF_QK_NONE) {
+            const size_t hd = (size_t)dm.d;
+            const bool biased = d->attn.qk_norm == DRF_QK_LAYER;
+            b.q_gain = take(hd); if (biased) b.q_bias = take(hd);
+            b.k_gain = take(hd); if (biased) b.k_bias = take(hd);
+        }
         take_linear(&b.proj, D, D);
         if (cfg->cond == DRF_COND_TEXT) {
             take_linear(&b.xq, D, D);
@@ -851,7 +968,8 @@ extern "C" drf_status drf_denoiser_create(const drf_dit_config* cfg, const float
         }
     }
 
-    if (d->bf16 && cfg->cond != DRF_COND_TEXT && chain_width(dm.D, dm.R)) {
+    // (that launch has the qkv Linear and, where it has it, the attention over all keys in one)
+    if (d->bf16 && cfg->cond != DRF_COND_TEXT && chain_width(dm.D, dm.R) && !d->qk_pass && d->attn.topk == 0) {
         const size_t unit = D * D;
         if ((rc = dev_alloc(d, (void**)&d->chain_w, (size_t)dm.L * (4 + 2 * R) * unit * 2)) != DRF_OK) return fail(rc);
         bf16_t* out = d->chain_w;
@@ -873,7 +991,7 @@ extern "C" drf_status drf_denoiser_create(const drf_dit_config* cfg, const float
     {
         std::vector<float> pos((size_t)dm.T * D);
         const size_t q4 = D / 4;
-        for (int py = 0; py < dm.gh; ++py)
+        for (int py = 0; py < (d->attn.additive_pos ? dm.gh : 0); ++py)
             for (int px = 0; px < dm.gw; ++px) {
                 float* row = pos.data() + ((size_t)py * dm.gw + px) * D;
                 for (size_t i = 0; i < q4; ++i) {

@@ -21,13 +21,16 @@ PROF_GEMM, PROF_ATTN, PROF_ELEMWISE, PROF_UPDATE, PROF_PASS_FULL, PROF_PASS_OTHE
 DDIM, DDPM, EULER = 0, 1, 2
 ROPE_PAIRS, ROPE_HALVES = 0, 1
 QK_NONE, QK_RMS, QK_LAYER = 0, 1, 2
+_QK = {"none": QK_NONE, "rms": QK_RMS, "layer": QK_LAYER}
+_LAYOUTS = {"pairs": ROPE_PAIRS, "halves": ROPE_HALVES}
 
 # include/drf.h: the method's calls
 SYMBOLS = ["drf_denoiser_weight_count", "drf_denoiser_create", "drf_denoiser_destroy", "drf_denoiser_reserve", "drf_denoiser_use_graphs",
            "drf_eps_batched", "drf_eps_batched_static", "drf_skip_transition", "drf_refine_step", "drf_sample",
            "drf_skip_transition_noise", "drf_normal_fill", "drf_sample_noise", "drf_noise_count",
            "drf_plan_build", "drf_last_error",
-           "drf_rope", "drf_qk_norm_rope", "drf_block_words", "drf_block_select_scratch_bytes", "drf_block_select", "drf_block_attention"]
+           "drf_rope", "drf_qk_norm_rope", "drf_block_words", "drf_block_select_scratch_bytes", "drf_block_select", "drf_block_attention",
+           "drf_denoiser_weight_count_attn", "drf_denoiser_create_attn"]
 # include/drf_measure.h: test and measurement hooks
 MEASURE_SYMBOLS = ["drf_eps_trace", "drf_profile_enable", "drf_profile_read", "drf_probe_gemm_bf16",
                    "drf_probe_attn_bf16", "drf_probe_cross_attn_bf16", "drf_probe_attn_route", "drf_probe_gemm_route", "drf_probe_block_route", "drf_probe_update_fused", "drf_graph_stats", "drf_calibrate_mfma_bf16", "drf_calibrate_copy"]
@@ -64,6 +67,11 @@ class RopeConfig(C.Structure):
 
 class QkConfig(C.Structure):
     _fields_ = [("norm", C.c_int), ("eps", C.c_double), ("q_scale", C.c_float)] + [(k, C.c_void_p) for k in ("q_gain", "q_bias", "k_gain", "k_bias")]
+
+
+class AttnConfig(C.Structure):
+    _fields_ = [("qk_norm", C.c_int), ("norm_eps", C.c_double), ("rope_dim", C.c_int * 2), ("rope_theta", C.c_double), ("rope_layout", C.c_int),
+                ("additive_pos", C.c_int), ("q_block", C.c_int), ("kv_block", C.c_int), ("topk", C.c_int)]
 
 
 class DrfError(RuntimeError):
@@ -122,6 +130,9 @@ def lib():
         L.drf_probe_block_route.argtypes = [C.c_int] * 5
         L.drf_probe_gemm_route.argtypes = [C.c_int] * 5 + [C.c_void_p]
         L.drf_last_error.restype = C.c_char_p
+        L.drf_denoiser_weight_count_attn.restype = C.c_size_t
+        L.drf_denoiser_weight_count_attn.argtypes = [C.c_void_p, C.c_void_p]
+        L.drf_denoiser_create_attn.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p, C.c_void_p]
         L.drf_rope.argtypes = [C.c_void_p] + [C.c_int] * 5 + [C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p, C.c_void_p, C.c_void_p]
         L.drf_qk_norm_rope.argtypes = [C.c_void_p] * 4 + [C.c_size_t] + [C.c_void_p] * 5
         L.drf_block_words.restype = L.drf_block_select_scratch_bytes.restype = C.c_size_t
@@ -147,6 +158,16 @@ def _check(status):
 def dit_config(d):
     return DitConfig(d["depth"], d["hidden"], d["heads"], d["mlp_ratio"], d["patch"], d["in_ch"], d["lat_h"],
                      d["lat_w"], d["dtype"], d["cond"], d["cond_dim"], d["ctx_len"])
+
+
+def attn_config(dit):
+    """drf_attn_config of a model whose dict has an "attn" entry (see I.param_shapes), else None."""
+    a = dit.get("attn")
+    if a is None:
+        return None
+    rope, blocks = a.get("rope_dim", (0, 0)), a.get("blocks", (0, 0, 0))
+    return AttnConfig(_QK[a.get("qk_norm", "none")], float(a.get("norm_eps", 1e-6)), (C.c_int * 2)(*rope), float(a.get("rope_theta", 10000.0)),
+                      _LAYOUTS[a.get("rope_layout", "pairs")], int(a.get("additive_pos", True)), *blocks)
 
 
 def sched_config(d):
@@ -181,8 +202,8 @@ def _dev(t, dtype=None):
 
 
 def denoiser_weight_count(dit):
-    cfg = dit_config(dit)
-    return int(lib().drf_denoiser_weight_count(C.byref(cfg)))
+    cfg, attn = dit_config(dit), attn_config(dit)
+    return int(lib().drf_denoiser_weight_count_attn(C.byref(cfg), None if attn is None else C.byref(attn)))
 
 
 def plan_build(sched, mode, n):
@@ -317,7 +338,7 @@ def rope_config(dims, extents, theta=10000.0, layout="pairs", origin=None, step=
     n = len(dims)
     if not 1 <= n <= 3 or len(extents) != n:
         raise ValueError("one to three axes, with an extent for each")
-    rc = RopeConfig(n_axes=n, theta=float(theta), layout={"pairs": ROPE_PAIRS, "halves": ROPE_HALVES}[layout])
+    rc = RopeConfig(n_axes=n, theta=float(theta), layout=_LAYOUTS[layout])
     for a in range(n):
         rc.dim[a], rc.extent[a] = int(dims[a]), int(extents[a])
         rc.origin[a] = 0.0 if origin is None else float(origin[a])
@@ -351,8 +372,7 @@ def qk_norm_rope(q, k, norm, config=None, q_gain=None, k_gain=None, q_bias=None,
     if k_out is None:
         k_out = torch.empty_like(k) if lens is None else k.clone()
     assert q_out.shape == q.shape and k_out.shape == k.shape, "outputs must have the shapes of their inputs"
-    kind = {"none": QK_NONE, "rms": QK_RMS, "layer": QK_LAYER}[norm]
-    cfg = QkConfig(kind, float(eps), float(q_scale), *(_vector(t, d, torch.float32, what) for t, what in (
+    cfg = QkConfig(_QK[norm], float(eps), float(q_scale), *(_vector(t, d, torch.float32, what) for t, what in (
         (q_gain, "q_gain"), (q_bias, "q_bias"), (k_gain, "k_gain"), (k_bias, "k_bias"))))
     shape = AttnShape(_dtype_of(q), S, N, N, H, k.shape[2], d, _vector(lens, S, torch.int32, "lens"), None)
     if positions is not None and config is None:
@@ -491,9 +511,9 @@ class Denoiser:
     def __init__(self, dit, host_weights):
         self.dit = dict(dit)
         w = np.ascontiguousarray(host_weights, np.float32)
-        cfg = dit_config(dit)
+        cfg, attn = dit_config(dit), attn_config(dit)
         h = C.c_void_p()
-        _check(lib().drf_denoiser_create(C.byref(cfg), w.ctypes.data_as(C.c_void_p), w.size, _stream(), C.byref(h)))
+        _check(lib().drf_denoiser_create_attn(C.byref(cfg), None if attn is None else C.byref(attn), w.ctypes.data_as(C.c_void_p), w.size, _stream(), C.byref(h)))
         self.h = h
 
     def close(self):

@@ -53,9 +53,13 @@ def config(idx, **dit_overrides):
 
 def param_shapes(dit):
     """(name, shape) of every parameter tensor in flat-array order; Linear weights
-    are [out, in]."""
+    are [out, in].  dit["attn"], if there: operators in the self-attention, a dict of qk_norm ("none", "rms", "layer"),
+    norm_eps, rope_dim (columns that turn with a token's row, with its column), rope_theta, rope_layout ("pairs",
+    "halves"), additive_pos and blocks (q_block, kv_block, topk)."""
     D, R = dit["hidden"], dit["mlp_ratio"]
     P = dit["in_ch"] * dit["patch"] ** 2
+    norm, hd = (dit.get("attn") or {}).get("qk_norm", "none"), D // dit["heads"]
+    norms = [n for n in ("q_gain", "q_bias", "k_gain", "k_bias") if norm == "layer" or norm == "rms" and n.endswith("gain")]
     out = [("patch_w", (D, P)), ("patch_b", (D,)),
            ("t_w1", (D, TFREQ)), ("t_b1", (D,)), ("t_w2", (D, D)), ("t_b2", (D,))]
     if dit["cond"] == COND_VECTOR:
@@ -65,8 +69,9 @@ def param_shapes(dit):
     for l in range(dit["depth"]):
         b = "blk%d." % l
         out += [(b + "ada_w", (6 * D, D)), (b + "ada_b", (6 * D,)),
-                (b + "qkv_w", (3 * D, D)), (b + "qkv_b", (3 * D,)),
-                (b + "proj_w", (D, D)), (b + "proj_b", (D,))]
+                (b + "qkv_w", (3 * D, D)), (b + "qkv_b", (3 * D,))]
+        out += [(b + n, (hd,)) for n in norms]
+        out += [(b + "proj_w", (D, D)), (b + "proj_b", (D,))]
         if dit["cond"] == COND_TEXT:
             out += [(b + "xq_w", (D, D)), (b + "xq_b", (D,)),
                     (b + "xkv_w", (2 * D, dit["cond_dim"])), (b + "xkv_b", (2 * D,)),
@@ -96,6 +101,13 @@ def _rng(stream, cfg_idx):
     return np.random.Generator(np.random.Philox(key=BASE_SEED + stream + cfg_idx))
 
 
+def _center_gains(dit, flat):
+    """Norm gains vary around one."""
+    for name, v in param_views(dit, flat).items() if dit.get("attn") else ():
+        if name.endswith("_gain"):
+            v += np.float32(1.0)
+
+
 def weights(dit, cfg_idx=0, init="paper"):
     """Flat fp32 parameter array.
     init="paper": every scalar ~ N(0, 0.02) (the workload definition).
@@ -106,6 +118,7 @@ def weights(dit, cfg_idx=0, init="paper"):
     flat = rng.standard_normal(n, dtype=np.float32)
     if init == "paper":
         flat *= np.float32(0.02)
+        _center_gains(dit, flat)
         return flat
     assert init == "loud"
     for name, v in param_views(dit, flat).items():
@@ -115,6 +128,7 @@ def weights(dit, cfg_idx=0, init="paper"):
             v *= np.float32(1.0 / np.sqrt(v.shape[1]))
         else:
             v *= np.float32(0.5)
+    _center_gains(dit, flat)
     return flat
 
 
