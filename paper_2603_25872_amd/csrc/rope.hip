@@ -3,9 +3,10 @@
 // One kernel for both: with n = (x - mean) / sqrt(var + eps) (or its simpler forms), p(c) the other column of c's pair and C, S its
 // cosine and signed sine,
 //   y_c = (n_c g_c + b_c) C_c + (n_p g_p + b_p) S_c = n_c A_c + n_p B_c + D_c,    A_c = g_c C_c, B_c = g_p S_c, D_c = b_c C_c + b_p S_c,
-// so gains, biases, the scale of the queries and the angles of a token come together in a table of two or three numbers a column, which a
-// workgroup forms once for its few tokens (angles in double precision: a position far from zero keeps its fraction of a turn) and uses for
-// every head of them.  What is left is a copy with a sum over d columns and two multiply-adds a column: bound by memory.
+// so gains, biases, the scale of the queries and the angles come together in two or three numbers a column, which a lane forms once for its
+// token and its columns and holds in registers over the token's heads.  The angles of a workgroup's tokens are formed once, by all its threads
+// (in double precision: a position far from zero keeps its fraction of a turn), while the first heads are on their way.  What is left is a copy
+// with a sum over a head's columns and two multiply-adds a column: bound by memory.
 #include <type_traits>
 
 #include "common.h"
@@ -19,12 +20,12 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 constexpr int kMaxD = 128, kMaxPairs = kMaxD / 2, kThreads = 256, kWaves = kThreads / 64;
 
 // The rotation as the kernels take it.
+struct Pair { double turns; int axis, first; };     // per unit of position, in whole turns; its axis and the lower of its columns
 struct Turns {
-    double turns[kMaxPairs];                // of pair i per unit of position, in whole turns
-    uint8_t axis[kMaxPairs], first[kMaxPairs], second[kMaxPairs];       // its axis and its two columns
-    uint8_t other[kMaxD];                   // the other column of a column's pair (itself where nothing turns)
+    Pair rec[kMaxPairs];
+    uint8_t pair[kMaxD], other[kMaxD];      // the pair of a column that turns, and the other column of it (itself where nothing turns)
     double origin[DRF_ROPE_AXES], step[DRF_ROPE_AXES];
-    int below[DRF_ROPE_AXES], extent[DRF_ROPE_AXES];    // tokens per unit of an axis, its extent
+    int below[DRF_ROPE_AXES];               // tokens per unit of an axis
     int pairs, columns, n_axes;             // columns: those that turn
     const float* positions;                 // or NULL: the grid
     size_t slot_stride;
@@ -43,9 +44,7 @@ struct HeadsArgs {
     int slots, tokens, d;
     const int32_t* lens;
     float eps;
-    int tile, tiles, parts, per_part;       // tokens a workgroup; heads in `parts` ranges of per_part
-    int heads_inner;                        // rows run over the heads of a token first
-    int granule;                            // columns that keep together in a pair's other half (DRF_ROPE_HALVES)
+    int tile, tiles, parts, head_waves;     // tokens a workgroup; its waves, head_waves of them over the heads, times `parts` workgroups
     Turns r;
 };
 
@@ -56,163 +55,195 @@ __device__ inline int slot_len(const int32_t* lens, int slot, int tokens)
     return n < 0 ? 0 : n < tokens ? n : tokens;
 }
 
-// cos and sin of pair i at token n of a slot
-__device__ inline void turn(const Turns& r, int slot, int n, int i, float* c, float* s)
+// position of token n of a slot on axis `axis`
+__device__ inline double position(const Turns& r, int slot, int n, int axis)
 {
-    const int a = r.axis[i];
-    double p;
-    if (r.positions) {
-        p = (double)r.positions[(size_t)slot * r.slot_stride + (size_t)n * r.n_axes + a];
-    } else {
-        int at = n / r.below[a];
-        if (a > 0) at %= r.extent[a];
-        p = fma(r.step[a], (double)at, r.origin[a]);
+    if (r.positions) return (double)r.positions[(size_t)slot * r.slot_stride + (size_t)n * r.n_axes + axis];
+    double p = 0.0;
+#pragma unroll
+    for (int a = 0; a < DRF_ROPE_AXES; ++a) {                       // (all axes, so that nothing waits for a table entry to know which)
+        if (a >= r.n_axes) break;
+        const int at = n / r.below[a];
+        n -= at * r.below[a];
+        const double x = fma(r.step[a], (double)at, r.origin[a]);
+        p = a == axis ? x : p;
     }
-    p *= r.turns[i];
+    return p;
+}
+
+// cos and sin of a turn of p units of position
+__device__ inline void turn(double p, double turns, float* c, float* s)
+{
+    p *= turns;
     sincospif(2.f * (float)(p - rint(p)), s, c);
 }
 
 template <typename T> __device__ inline float to_f32(T v) { return (float)v; }
 
-// Pieces of 16 bytes: a row (one head of one token) is P of them, one a lane, and a wave takes 64 / P rows at a time, so that all but the
-// last few lanes work at any head width.  NORM: a drf_qk_norm; ROPE: 0 none, 1 pairs, 2 halves.
+// Which columns a pair is of, and how the other ones of a lane's are read (a head's columns are read twice then, the second time from the near caches).
+enum { ROPE_NO = 0, ROPE_IN_LANE = 1, ROPE_PIECE = 2, ROPE_HALF_PIECE = 3, ROPE_ELEMENT = 4 };
+
+// A row (one head of one token) is P = d / E pieces of 16 bytes, one a lane, and a wave takes 64 / P tokens, so that all but the last few lanes
+// work at any head width, and U heads of them at a time.  NORM: a drf_qk_norm.
+constexpr int kHeads = 4;
 template <typename T, int NORM, int ROPE>
 __global__ void __launch_bounds__(kThreads) heads_kernel(const HeadsArgs a)
 {
-    constexpr int E = 16 / sizeof(T), U = 2;
+    constexpr int E = 16 / sizeof(T), U = kHeads;
     typedef T piece __attribute__((ext_vector_type(E)));
-    extern __shared__ __attribute__((aligned(16))) float tab[];     // [A, B, D][q, k][token][column]
-    const int d = a.d, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    typedef T half_piece __attribute__((ext_vector_type(E / 2)));
+    extern __shared__ __attribute__((aligned(16))) float tab[];     // [token][pair](cos, sin)
+    const int d = a.d, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    // consecutive tiles on one XCD (ids are dealt round-robin over the 8 of them, each with its own L2): they share the lines that a tile ends inside of
     int id = blockIdx.x;
+    {
+        const int q8 = gridDim.x >> 3, rem = gridDim.x & 7, xcd = id & 7;
+        id = xcd * q8 + (xcd < rem ? xcd : rem) + (id >> 3);
+    }
     const int part = id % a.parts;
     id /= a.parts;
-    const int slot = id / a.tiles, t0 = (id - slot * a.tiles) * a.tile;
-    const int left = slot_len(a.lens, slot, a.tokens) - t0;
+    const int slot = id / a.tiles, t0 = (id - slot * a.tiles) * a.tile, left = slot_len(a.lens, slot, a.tokens) - t0;
     if (left <= 0) return;
-    const int nt = left < a.tile ? left : a.tile;
-    const int all = a.q.heads + a.k.heads, h0 = part * a.per_part, h1 = h0 + a.per_part < all ? h0 + a.per_part : all, nh = h1 - h0;
-    const int plane = 2 * a.tile * d;
     const int P = d / E, rpw = 64 / P, lr = lane / P, lp = lane - lr * P;
+    const int tl = wave / a.head_waves * rpw + lr;                  // this lane's token of the tile
+    const bool live = lr < rpw && tl < left;
+    const int at = live ? tl : 0;                                   // (lanes without a row take part in the sums)
+    const int col = lr < rpw ? lp * E : 0;
+    // heads in chunks of U, the queries' and then the keys'; this wave's are c .. c1 - 1
+    const int q_chunks = (a.q.heads + U - 1) / U, chunks = q_chunks + (a.k.heads + U - 1) / U, waves = a.parts * a.head_waves;
+    const int w_id = part * a.head_waves + wave % a.head_waves, c1 = chunks * (w_id + 1) / waves;
+    int ch = chunks * w_id / waves;
 
-    // the table
-    if constexpr (ROPE != 0) {
-        for (int i = tid; i < nt * a.r.pairs; i += kThreads) {
-            const int n = i / a.r.pairs, p = i - n * a.r.pairs, c0 = a.r.first[p], c1 = a.r.second[p];
-            float c, s;
-            turn(a.r, slot, t0 + n, p, &c, &s);
+    // What the tables in the kernel's arguments and the norm's parameters give is asked for ahead of the heads: answers come in the order of the questions.
+    const int first_pair = ROPE != ROPE_NO ? threadIdx.x % a.r.pairs : 0;
+    Pair rec = a.r.rec[first_pair];
+    int oc[E], pc[E];                                               // of this lane's columns: the others of their pairs, their pairs
 #pragma unroll
-            for (int w = 0; w < 2; ++w) {
-                const Side& e = w ? a.k : a.q;
-                const float g0 = (e.gain ? e.gain[c0] : 1.f) * e.scale, g1 = (e.gain ? e.gain[c1] : 1.f) * e.scale;
-                float* t = tab + (w * a.tile + n) * d;
-                t[c0] = g0 * c; t[c1] = g1 * c;
-                t[plane + c0] = -g1 * s; t[plane + c1] = g0 * s;
-                if constexpr (NORM == DRF_QK_LAYER) {
-                    const float b0 = e.bias ? e.bias[c0] * e.scale : 0.f, b1 = e.bias ? e.bias[c1] * e.scale : 0.f;
-                    t[2 * plane + c0] = b0 * c - b1 * s; t[2 * plane + c1] = b0 * s + b1 * c;
-                }
-            }
-        }
+    for (int j = 0; j < E; ++j) {
+        oc[j] = ROPE == ROPE_IN_LANE ? col + (j ^ 1) : ROPE >= ROPE_PIECE ? a.r.other[col + j] : 0;
+        pc[j] = ROPE == ROPE_IN_LANE ? (col + j) / 2 : ROPE >= ROPE_PIECE ? a.r.pair[col + j] : 0;
     }
-    {
-        const int from = ROPE != 0 ? a.r.columns : 0, rest = d - from;
-        for (int i = tid; i < 2 * nt * rest; i += kThreads) {
-            const int row = i / rest, c = from + i - row * rest, w = row >= nt, n = row - w * nt;
-            const Side& e = w ? a.k : a.q;
-            float* t = tab + (w * a.tile + n) * d + c;
-            t[0] = (e.gain ? e.gain[c] : 1.f) * e.scale;
-            t[plane] = 0.f;
-            if constexpr (NORM == DRF_QK_LAYER) t[2 * plane] = e.bias ? e.bias[c] * e.scale : 0.f;
+    float g[E], go[E], b[E], bo[E];
+    auto parameters = [&](const Side& e) {
+#pragma unroll
+        for (int j = 0; j < E; ++j) { g[j] = go[j] = 1.f; b[j] = bo[j] = 0.f; }
+        if (NORM != DRF_QK_NONE && e.gain) {
+#pragma unroll
+            for (int j = 0; j < E; ++j) { g[j] = e.gain[col + j]; go[j] = e.gain[oc[j]]; }
         }
-    }
-    __syncthreads();
-
-    const int rows = nh * nt, inner = a.heads_inner ? nh : nt;
-    // sum over a row's lanes
-    auto row_sum = [&](float v) {
-        for (int o = 1; o < P; o <<= 1) {
-            const float u = __shfl_down(v, o, 64);
-            v += lp + o < P ? u : 0.f;
+        if (NORM == DRF_QK_LAYER && e.bias) {
+#pragma unroll
+            for (int j = 0; j < E; ++j) { b[j] = e.bias[col + j]; bo[j] = e.bias[oc[j]]; }
         }
-        return __shfl(v, lr * P, 64);
     };
-    for (int base = wave * rpw * U; base < rows; base += kWaves * rpw * U) {
-        piece x[U], xo[U];
-        T* y[U];
-        const float* t[U];
+    if (ch < c1) parameters(ch >= q_chunks ? a.k : a.q);
+    piece v[U], w[U];
+    auto load = [&](int chunk) {
+        const bool is_k = chunk >= q_chunks;
+        const Side& e = is_k ? a.k : a.q;
+        const int h0 = (is_k ? chunk - q_chunks : chunk) * U;
+        const T* x = (const T*)e.x + slot * e.xs + (int64_t)(t0 + at) * e.xt + h0 * e.xh;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int row = base + u * rpw + lr;
-            y[u] = nullptr;
-            if (lr < rpw && row < rows) {
-                const int o = row / inner, i = row - o * inner;
-                const int n = a.heads_inner ? o : i, hh = h0 + (a.heads_inner ? i : o), w = hh >= a.q.heads;
-                const Side& e = w ? a.k : a.q;
-                const int h = w ? hh - a.q.heads : hh;
-                const T* xr = (const T*)e.x + slot * e.xs + (int64_t)(t0 + n) * e.xt + h * e.xh;
-                x[u] = *reinterpret_cast<const piece*>(xr + lp * E);
-                if constexpr (ROPE == 2) {
-                    if (a.granule == E) {
-                        xo[u] = *reinterpret_cast<const piece*>(xr + a.r.other[lp * E]);
-                    } else if (E == 8 && a.granule == E / 2) {
-                        typedef T half_piece __attribute__((ext_vector_type(E / 2)));
-                        const half_piece lo = *reinterpret_cast<const half_piece*>(xr + a.r.other[lp * E]);
-                        const half_piece hi = *reinterpret_cast<const half_piece*>(xr + a.r.other[lp * E + E / 2]);
+            const T* xr = x + (h0 + u < e.heads ? u : 0) * e.xh;
+            v[u] = *reinterpret_cast<const piece*>(xr + col);
+            if constexpr (ROPE == ROPE_PIECE) {
+                w[u] = *reinterpret_cast<const piece*>(xr + oc[0]);
+            } else if constexpr (ROPE == ROPE_HALF_PIECE) {
+                const half_piece lo = *reinterpret_cast<const half_piece*>(xr + oc[0]), hi = *reinterpret_cast<const half_piece*>(xr + oc[E / 2]);
 #pragma unroll
-                        for (int j = 0; j < E / 2; ++j) { xo[u][j] = lo[j]; xo[u][j + E / 2] = hi[j]; }
-                    } else {
+                for (int j = 0; j < E / 2; ++j) { w[u][j] = lo[j]; w[u][j + E / 2] = hi[j]; }
+            } else if constexpr (ROPE == ROPE_ELEMENT) {
 #pragma unroll
-                        for (int j = 0; j < E; ++j) xo[u][j] = xr[a.r.other[lp * E + j]];
-                    }
-                }
-                y[u] = (T*)e.y + slot * e.ys + (int64_t)(t0 + n) * e.yt + h * e.yh + lp * E;
-                t[u] = tab + (w * a.tile + n) * d + lp * E;
-            } else {
-#pragma unroll
-                for (int j = 0; j < E; ++j) x[u][j] = (T)0.f;
-                if constexpr (ROPE == 2) xo[u] = x[u];
-                t[u] = tab;
+                for (int j = 0; j < E; ++j) w[u][j] = xr[oc[j]];
             }
         }
+    };
+    if (ch < c1) load(ch);
+    if constexpr (ROPE != ROPE_NO) {
+        const int nt = left < a.tile ? left : a.tile;
+        for (int i = threadIdx.x; i < nt * a.r.pairs; i += kThreads) {
+            const int n = i / a.r.pairs;
+            if (i >= kThreads) rec = a.r.rec[i - n * a.r.pairs];
+            turn(position(a.r, slot, t0 + n, rec.axis), rec.turns, &tab[2 * i], &tab[2 * i + 1]);
+        }
+        __syncthreads();
+    }
+    // sums over a row's lanes, of U rows at once
+    auto row_sums = [&](float (&t)[U]) {
+        for (int o = 1; o < P; o <<= 1) {
+            float r[U];
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            float v[E], o[E];
+            for (int u = 0; u < U; ++u) r[u] = __shfl_down(t[u], o, 64);
 #pragma unroll
-            for (int j = 0; j < E; ++j) v[j] = to_f32(x[u][j]);
-            float mean = 0.f, inv = 1.f;
-            if constexpr (NORM == DRF_QK_LAYER) {
-                float s = 0.f;
+            for (int u = 0; u < U; ++u) t[u] += lp + o < P ? r[u] : 0.f;
+        }
 #pragma unroll
-                for (int j = 0; j < E; ++j) s += v[j];
-                mean = row_sum(s) / (float)d;
+        for (int u = 0; u < U; ++u) t[u] = __shfl(t[u], lr * P, 64);
+    };
+    const float inv_d = 1.f / (float)d;
+    float ka[E], kb[E], kd[E];
+    int have = -1;                                                  // the side that they are for
+    for (; ch < c1; ++ch) {
+        const bool is_k = ch >= q_chunks;
+        const Side& e = is_k ? a.k : a.q;
+        if (have != (int)is_k) {
+            if (have >= 0) parameters(e);
+            have = is_k;
 #pragma unroll
-                for (int j = 0; j < E; ++j) v[j] -= mean;
+            for (int j = 0; j < E; ++j) {
+                float c = 1.f, s = 0.f;
+                if (ROPE != ROPE_NO && col + j < a.r.columns) {
+                    c = tab[2 * (at * a.r.pairs + pc[j])];
+                    s = tab[2 * (at * a.r.pairs + pc[j]) + 1];
+                    if (ROPE == ROPE_IN_LANE ? j % 2 == 0 : oc[j] > col + j) s = -s;    // (the first of a pair is the lower)
+                }
+                ka[j] = g[j] * e.scale * c; kb[j] = go[j] * e.scale * s;
+                if constexpr (NORM == DRF_QK_LAYER) kd[j] = (b[j] * c + bo[j] * s) * e.scale;
             }
-            if constexpr (NORM != DRF_QK_NONE) {
-                float s = 0.f;
+        }
+        const int h0 = (is_k ? ch - q_chunks : ch) * U;
+        T* y = (T*)e.y + slot * e.ys + (int64_t)(t0 + at) * e.yt + h0 * e.yh + col;
+        float mean[U], inv[U];
 #pragma unroll
-                for (int j = 0; j < E; ++j) s = fmaf(v[j], v[j], s);
-                inv = 1.f / sqrtf(row_sum(s) / (float)d + a.eps);
+        for (int u = 0; u < U; ++u) { mean[u] = 0.f; inv[u] = 1.f; }
+        if constexpr (NORM == DRF_QK_LAYER) {
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int j = 0; j < E; ++j) mean[u] += to_f32(v[u][j]);
+            row_sums(mean);
+#pragma unroll
+            for (int u = 0; u < U; ++u) mean[u] *= inv_d;
+        }
+        if constexpr (NORM != DRF_QK_NONE) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                float t = 0.f;
+#pragma unroll
+                for (int j = 0; j < E; ++j) t = fmaf(to_f32(v[u][j]) - mean[u], to_f32(v[u][j]) - mean[u], t);
+                inv[u] = t;
             }
-            if constexpr (ROPE == 1) {
+            row_sums(inv);
 #pragma unroll
-                for (int j = 0; j < E; ++j) o[j] = v[j ^ 1];
-            } else if constexpr (ROPE == 2) {
+            for (int u = 0; u < U; ++u) inv[u] = 1.f / sqrtf(inv[u] * inv_d + a.eps);
+        }
+        if (live) {
 #pragma unroll
-                for (int j = 0; j < E; ++j) o[j] = to_f32(xo[u][j]) - mean;
-            }
-            if (y[u]) {
+            for (int u = 0; u < U; ++u) {
                 piece out;
 #pragma unroll
                 for (int j = 0; j < E; ++j) {
-                    float r = v[j] * inv * t[u][j];
-                    if constexpr (ROPE != 0) r = fmaf(o[j] * inv, t[u][plane + j], r);
-                    if constexpr (NORM == DRF_QK_LAYER) r += t[u][2 * plane + j];
+                    float r = (to_f32(v[u][j]) - mean[u]) * ka[j];
+                    if constexpr (ROPE != ROPE_NO) r = fmaf(to_f32(ROPE == ROPE_IN_LANE ? v[u][j ^ 1] : w[u][j]) - mean[u], kb[j], r);
+                    if constexpr (NORM == DRF_QK_LAYER) r = fmaf(r, inv[u], kd[j]);
+                    else if constexpr (NORM == DRF_QK_RMS) r *= inv[u];
                     out[j] = (T)r;
                 }
-                *reinterpret_cast<piece*>(y[u]) = out;
+                if (h0 + u < e.heads) *reinterpret_cast<piece*>(y + u * e.yh) = out;
             }
         }
+        if (ch + 1 < c1) load(ch + 1);
     }
 }
 
@@ -264,12 +295,11 @@ __global__ void __launch_bounds__(kThreads) heads_any_kernel(const HeadsArgs a, 
         };
         float r = affine(v[j], c);
         if (c < a.r.columns) {
-            int i = 0;                          // the pair that column c belongs to
-            while (a.r.first[i] != c && a.r.second[i] != c) ++i;
+            const Pair& p = a.r.rec[a.r.pair[c]];
             float cs, sn_;
-            turn(a.r, slot, n, i, &cs, &sn_);
+            turn(position(a.r, slot, n, p.axis), p.turns, &cs, &sn_);
             const float z = affine(o[j], oc[j]);
-            r = a.r.first[i] == c ? fmaf(r, cs, -z * sn_) : fmaf(r, cs, z * sn_);
+            r = p.first == c ? fmaf(r, cs, -z * sn_) : fmaf(r, cs, z * sn_);
         }
         y[c] = (T)r;
     }
@@ -288,7 +318,7 @@ drf_status fill_turns(const drf_rope_config* rc, int head_dim, const float* posi
         if (rc->extent[a] < 1) DRF_FAIL(DRF_EINVAL, "axis %d: extent must be >= 1", a);
         if (!std::isfinite(rc->origin[a]) || !std::isfinite(rc->step[a])) DRF_FAIL(DRF_EINVAL, "axis %d: origin and step must be finite", a);
         if (below > 0x7fffffffLL) below = 0x7fffffffLL;         // no token index gets there
-        t->below[a] = (int)below; t->extent[a] = rc->extent[a];
+        t->below[a] = (int)below;
         t->origin[a] = rc->origin[a]; t->step[a] = rc->step[a];
         below *= rc->extent[a];
     }
@@ -299,11 +329,10 @@ drf_status fill_turns(const drf_rope_config* rc, int head_dim, const float* posi
         for (int i = 0; i < half; ++i) {
             const int p = t->pairs++;
             const bool pairs = rc->layout == DRF_ROPE_PAIRS;
-            t->axis[p] = (uint8_t)a;
-            t->first[p] = (uint8_t)(pairs ? column + 2 * i : column + i);
-            t->second[p] = (uint8_t)(pairs ? column + 2 * i + 1 : column + half + i);
-            t->other[t->first[p]] = t->second[p]; t->other[t->second[p]] = t->first[p];
-            t->turns[p] = std::pow(rc->theta, -2.0 * i / rc->dim[a]) / (2.0 * 3.14159265358979323846);
+            const int c0 = pairs ? column + 2 * i : column + i, c1 = pairs ? column + 2 * i + 1 : column + half + i;
+            t->rec[p] = { std::pow(rc->theta, -2.0 * i / rc->dim[a]) / (2.0 * 3.14159265358979323846), a, c0 };
+            t->other[c0] = (uint8_t)c1; t->other[c1] = (uint8_t)c0;
+            t->pair[c0] = t->pair[c1] = (uint8_t)p;
         }
         column += rc->dim[a];
     }
@@ -326,9 +355,16 @@ drf_status fill_side(const char* what, const drf_heads* x, const drf_heads* y, i
     return DRF_OK;
 }
 
-template <typename T, int NORM, int ROPE> void go(const HeadsArgs& a, unsigned grid, size_t lds, hipStream_t st)
+template <typename T, int NORM> void go(const HeadsArgs& a, int rope, unsigned grid, hipStream_t st)
 {
-    hipLaunchKernelGGL((heads_kernel<T, NORM, ROPE>), dim3(grid), dim3(kThreads), lds, st, a);
+    const size_t lds = rope == ROPE_NO ? 0 : (size_t)a.tile * a.r.pairs * 2 * sizeof(float);
+    switch (rope) {
+    case ROPE_NO: hipLaunchKernelGGL((heads_kernel<T, NORM, ROPE_NO>), dim3(grid), dim3(kThreads), lds, st, a); break;
+    case ROPE_IN_LANE: hipLaunchKernelGGL((heads_kernel<T, NORM, ROPE_IN_LANE>), dim3(grid), dim3(kThreads), lds, st, a); break;
+    case ROPE_PIECE: hipLaunchKernelGGL((heads_kernel<T, NORM, ROPE_PIECE>), dim3(grid), dim3(kThreads), lds, st, a); break;
+    case ROPE_HALF_PIECE: hipLaunchKernelGGL((heads_kernel<T, NORM, ROPE_HALF_PIECE>), dim3(grid), dim3(kThreads), lds, st, a); break;
+    default: hipLaunchKernelGGL((heads_kernel<T, NORM, ROPE_ELEMENT>), dim3(grid), dim3(kThreads), lds, st, a);
+    }
 }
 
 template <typename T> drf_status launch(HeadsArgs& a, int norm, int rope, bool vec, hipStream_t st)
@@ -343,24 +379,20 @@ template <typename T> drf_status launch(HeadsArgs& a, int norm, int rope, bool v
         DRF_HIP(hipGetLastError());
         return DRF_OK;
     }
-    a.tile = 8;
+    // A workgroup's waves share the tokens' angles: all four over the heads where there are that many chunks of them, the rest over more tokens.
+    const int chunks = (a.q.heads + kHeads - 1) / kHeads + (a.k.heads + kHeads - 1) / kHeads;
+    a.head_waves = chunks >= 4 ? 4 : chunks >= 2 ? 2 : 1;
+    a.tile = kWaves / a.head_waves * (64 / (a.d * (int)sizeof(T) / 16));
     a.tiles = (a.tokens + a.tile - 1) / a.tile;
     const long long groups = (long long)a.tiles * a.slots;
+    // and over several workgroups until there is one for every CU
     a.parts = 1;
-    while (a.parts < all && groups * a.parts < 1024) a.parts *= 2;
-    if (a.parts > all) a.parts = all;
-    a.per_part = (all + a.parts - 1) / a.parts;
-    a.parts = (all + a.per_part - 1) / a.per_part;
+    while (a.parts * 2 * a.head_waves <= chunks && groups * a.parts < 256) a.parts *= 2;
     if (groups * a.parts > 0x7fffffLL) DRF_FAIL(DRF_ESHAPE, "too many tokens");
-    // rows in the order that the memory of a token tile has
-    a.heads_inner = llabs(a.q.xh) < llabs(a.q.xt);
-    const size_t lds = (size_t)(norm == DRF_QK_LAYER ? 3 : 2) * 2 * a.tile * a.d * sizeof(float);
     const unsigned grid = (unsigned)(groups * a.parts);
-#define DRF_GO(N) (rope == 0 ? go<T, N, 0>(a, grid, lds, st) : rope == 1 ? go<T, N, 1>(a, grid, lds, st) : go<T, N, 2>(a, grid, lds, st))
-    if (norm == DRF_QK_NONE) DRF_GO(DRF_QK_NONE);
-    else if (norm == DRF_QK_RMS) DRF_GO(DRF_QK_RMS);
-    else DRF_GO(DRF_QK_LAYER);
-#undef DRF_GO
+    if (norm == DRF_QK_NONE) go<T, DRF_QK_NONE>(a, rope, grid, st);
+    else if (norm == DRF_QK_RMS) go<T, DRF_QK_RMS>(a, rope, grid, st);
+    else go<T, DRF_QK_LAYER>(a, rope, grid, st);
     DRF_HIP(hipGetLastError());
     return DRF_OK;
 }
@@ -369,11 +401,15 @@ drf_status run_heads(HeadsArgs& a, const drf_rope_config* rope, drf_dtype dtype,
 {
     const int unit = dtype == DRF_BF16 ? 8 : 4;
     vec = vec && a.d % unit == 0;
-    const int kind = !a.r.columns ? 0 : rope->layout == DRF_ROPE_PAIRS ? 1 : 2;
-    a.granule = unit;
-    if (kind == 2)
+    int kind = ROPE_NO;
+    if (a.r.columns && rope->layout == DRF_ROPE_PAIRS) {
+        kind = ROPE_IN_LANE;
+    } else if (a.r.columns) {
+        int granule = unit;                                         // columns that keep together in a pair's other half
         for (int i = 0; i < rope->n_axes; ++i)
-            while (rope->dim[i] / 2 % a.granule) a.granule /= 2;
+            while (rope->dim[i] / 2 % granule) granule /= 2;
+        kind = granule == unit ? ROPE_PIECE : dtype == DRF_BF16 && granule == unit / 2 ? ROPE_HALF_PIECE : ROPE_ELEMENT;
+    }
     return dtype == DRF_BF16 ? launch<bf16_t>(a, norm, kind, vec, st) : launch<float>(a, norm, kind, vec, st);
 }
 
