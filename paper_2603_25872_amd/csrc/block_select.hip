@@ -13,6 +13,7 @@ namespace drf {
 namespace {
 
 typedef double f64x4 __attribute__((ext_vector_type(4)));
+typedef double f64x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kMaxD = 128, kThreads = 256, kWaves = kThreads / 64;
 constexpr int kMaxBlocks = 1024;            // key blocks: 16 rows of scores fill 128 of a CU's 160 KB of LDS
@@ -22,7 +23,7 @@ struct PoolSide {
     int64_t xs, xt, xh;
     int tokens, heads, block, blocks;
     const int32_t* lens;
-    double* out;        // [slot][head][block / 16][k-step][64]: operand fragments of the 16 x 16 x 4 product, lane 16 (c % 4) + block % 16 of k-step c / 4
+    double* out;        // [slot][head][blocks up to a multiple of 16][columns up to a multiple of 8]
 };
 
 __device__ inline int slot_len(const int32_t* lens, int slot, int tokens)
@@ -30,11 +31,6 @@ __device__ inline int slot_len(const int32_t* lens, int slot, int tokens)
     if (!lens) return tokens;
     const int n = lens[slot];
     return n < 0 ? 0 : n < tokens ? n : tokens;
-}
-
-__device__ inline size_t fragment(int block, int c, int ksteps)
-{
-    return ((size_t)(block >> 4) * ksteps + (c >> 2)) * 64 + 16 * (c & 3) + (block & 15);
 }
 
 // A wave takes a head of a block: 64 / P rows at a time in pieces of 16 bytes (VEC), or a row at a time, a column or two a lane.
@@ -52,30 +48,36 @@ __global__ void __launch_bounds__(kThreads) pool_kernel(const PoolSide q, const 
     id /= parts;
     const int slot = id / s.blocks, block = id - slot * s.blocks, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int len = slot_len(s.lens, slot, s.tokens), n0 = block * s.block, end = n0 + s.block < len ? n0 + s.block : len;
-    const int ksteps = (d + 3) / 4, tiles = (s.blocks + 15) / 16;
+    const int width = (d + 7) / 8 * 8, padded = (s.blocks + 15) / 16 * 16;
     for (int h = part * kWaves + wave; h < s.heads; h += parts * kWaves) {
         const T* x = (const T*)s.x + slot * s.xs + h * s.xh;
-        double* out = s.out + ((size_t)slot * s.heads + h) * tiles * ksteps * 64;
+        double* out = s.out + (((size_t)slot * s.heads + h) * padded + block) * width;
         double sum[E];
 #pragma unroll
         for (int j = 0; j < E; ++j) sum[j] = 0.0;
         if constexpr (VEC) {
             const int P = d / E, rpw = 64 / P, lr = lane / P, lp = lane - lr * P;
-            if (lr < rpw)
-                for (int n = n0 + lr; n < end; n += rpw) {
-                    const piece v = *reinterpret_cast<const piece*>(x + (int64_t)n * s.xt + lp * E);
+            constexpr int U = 6;                                // rows in flight
+            for (int n = n0 + lr; n < end && lr < rpw; n += U * rpw) {
+                piece v[U];
 #pragma unroll
-                    for (int j = 0; j < E; ++j) sum[j] += (double)(float)v[j];
-                }
+                for (int u = 0; u < U; ++u) v[u] = *reinterpret_cast<const piece*>(x + (int64_t)(n + u * rpw < end ? n + u * rpw : n) * s.xt + lp * E);
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+                    if (n + u * rpw < end) {
+#pragma unroll
+                        for (int j = 0; j < E; ++j) sum[j] += (double)(float)v[u][j];
+                    }
+            }
             double* mine = part_sums[wave];                     // (a wave's LDS operations complete in order)
 #pragma unroll
             for (int j = 0; j < E; ++j) mine[lane * E + j] = sum[j];
             __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-            for (int c = lane; c < 4 * ksteps; c += 64) {
+            for (int c = lane; c < width; c += 64) {
                 double t = 0.0;
                 if (c < d)
                     for (int r = 0; r < rpw; ++r) t += mine[r * d + c];
-                out[fragment(block, c, ksteps)] = t;
+                out[c] = t;
             }
             __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
         } else {
@@ -85,7 +87,7 @@ __global__ void __launch_bounds__(kThreads) pool_kernel(const PoolSide q, const 
                     if (lane + 64 * j < d) sum[j] += (double)(float)x[(int64_t)n * s.xt + lane + 64 * j];
 #pragma unroll
             for (int j = 0; j < 2; ++j)
-                if (lane + 64 * j < 4 * ksteps) out[fragment(block, lane + 64 * j, ksteps)] = sum[j];
+                if (lane + 64 * j < width) out[lane + 64 * j] = sum[j];
         }
     }
 }
@@ -101,75 +103,120 @@ __device__ inline uint64_t key_of(double v)
 
 struct SelectArgs {
     const double *q, *k;
-    int q_tokens, kv_tokens, q_heads, group, q_block, kv_block, nq, nk, ksteps, topk, words;
+    int q_tokens, kv_tokens, q_heads, group, q_block, kv_block, nq, nk, pairs, topk, words;      // pairs: of k-steps, 8 columns each
     const int32_t *q_lens, *kv_lens;
     uint32_t* blocks;
 };
 
-// A workgroup takes 16 query blocks of a (slot, head): their scores against all key blocks on the 16 x 16 x 4 matrix instruction into LDS,
-// then a wave a row: the topk-th largest key by bisection over its bits (counting by ballots, until a bound splits off exactly topk), the
-// keys above it and of those equal to it the lowest blocks.  NK: keys a lane holds.
-template <int NK>
-__global__ void __launch_bounds__(kThreads) select_kernel(const SelectArgs a)
+// A workgroup takes 16 query blocks of a (slot, head): their scores against all key blocks on the 16 x 16 x 4 matrix instruction into LDS, then a
+// wave row after row.  Up to 64 blocks a row (NK = 1, a key a lane) every key's rank is counted against one key after another, four
+// instructions each; more of them have the topk-th largest key found by bisection over its bits, on scalars but for the comparisons (counting by
+// ballots, until a bound splits off exactly topk).  Latency bounds both, and with many rows of few blocks the instructions (64 slots x 16 heads x
+// 16 rows of 16 blocks).  NK: keys of a row that a lane holds; NW: waves.
+constexpr int kRows = 16;
+template <int NK, int NW>
+__global__ void __launch_bounds__(NW * 64) select_kernel(const SelectArgs a)
 {
+    constexpr int R = kRows / NW, kPairs = 6;                               // pairs of k-steps asked for at once
     extern __shared__ __attribute__((aligned(16))) double score[];          // [16][nk padded]
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int qtiles = (a.nq + 15) / 16, ktiles = (a.nk + 15) / 16, ld = ktiles * 16 + 2;
-    const int qt = blockIdx.x % qtiles, sh = blockIdx.x / qtiles, slot = sh / a.q_heads, h = sh - slot * a.q_heads;
+    // the rows of one head on one XCD (ids are dealt round-robin over the 8 of them, each with its own L2): they read the same sums of keys
+    int id = blockIdx.x;
+    {
+        const int q8 = gridDim.x >> 3, rem = gridDim.x & 7, xcd = id & 7;
+        id = xcd * q8 + (xcd < rem ? xcd : rem) + (id >> 3);
+    }
+    const int qt = id % qtiles, sh = id / qtiles, slot = sh / a.q_heads, h = sh - slot * a.q_heads;
     const int q_len = slot_len(a.q_lens, slot, a.q_tokens), kv_len = slot_len(a.kv_lens, slot, a.kv_tokens);
     const int n_valid = (kv_len + a.kv_block - 1) / a.kv_block;             // key blocks that hold a key
-    const double* q = a.q + ((size_t)sh * qtiles + qt) * a.ksteps * 64 + lane;
-    const double* k = a.k + ((size_t)slot * (a.q_heads / a.group) + h / a.group) * ktiles * a.ksteps * 64 + lane;
-    for (int t = wave; t < ktiles; t += kWaves) {
-        const double* kt = k + (size_t)t * a.ksteps * 64;
-        f64x4 acc = { 0.0, 0.0, 0.0, 0.0 };
-        for (int s = 0; s < a.ksteps; ++s) acc = __builtin_amdgcn_mfma_f64_16x16x4f64(q[s * 64], kt[s * 64], acc, 0, 0, 0);
+    // Operands of the product: row lane % 16 of a tile, and of every 8 columns 2 (lane / 16) in one k-step, the next in another (16 bytes a lane).
+    const int width = 8 * a.pairs;
+    const double* q = a.q + (((size_t)sh * qtiles + qt) * 16 + (lane & 15)) * width + 2 * (lane >> 4);
+    const double* k = a.k + (((size_t)slot * (a.q_heads / a.group) + h / a.group) * ktiles * 16 + (lane & 15)) * width + 2 * (lane >> 4);
+    for (int t = wave; t < ktiles; t += NW) {
+        const double* kt = k + (size_t)t * 16 * width;
+        f64x4 acc[2] = { { 0.0, 0.0, 0.0, 0.0 }, { 0.0, 0.0, 0.0, 0.0 } };
+        for (int s0 = 0; s0 < a.pairs; s0 += kPairs) {
+            f64x2 qv[kPairs], kv[kPairs];
+#pragma unroll
+            for (int j = 0; j < kPairs; ++j) {
+                const int s = s0 + j < a.pairs ? s0 + j : a.pairs - 1;
+                qv[j] = *reinterpret_cast<const f64x2*>(q + s * 8);
+                kv[j] = *reinterpret_cast<const f64x2*>(kt + s * 8);
+            }
+#pragma unroll
+            for (int j = 0; j < kPairs; ++j)
+                if (s0 + j < a.pairs) {
+                    acc[0] = __builtin_amdgcn_mfma_f64_16x16x4f64(qv[j][0], kv[j][0], acc[0], 0, 0, 0);
+                    acc[1] = __builtin_amdgcn_mfma_f64_16x16x4f64(qv[j][1], kv[j][1], acc[1], 0, 0, 0);
+                }
+        }
         // lane l holds column l % 16 of rows l / 16 + 4 r
         const int j = t * 16 + (lane & 15), left = kv_len - j * a.kv_block, count = left < a.kv_block ? left : a.kv_block;
 #pragma unroll
-        for (int r = 0; r < 4; ++r) score[((lane >> 4) + 4 * r) * ld + j] = count > 0 ? acc[r] / (double)count : 0.0;
+        for (int r = 0; r < 4; ++r) score[((lane >> 4) + 4 * r) * ld + j] = count > 0 ? (acc[0][r] + acc[1][r]) / (double)count : 0.0;
     }
     __syncthreads();
-    for (int r = wave; r < 16; r += kWaves) {
-        const int i = qt * 16 + r;
+    for (int r = 0; r < R; ++r) {
+        const int i = qt * kRows + wave * R + r;
         if (i >= a.nq) break;
         const int want = i * a.q_block >= q_len ? 0 : a.topk < n_valid ? a.topk : n_valid;
-        uint64_t key[NK];
+        uint64_t key[NK], chosen[NK];
 #pragma unroll
-        for (int c = 0; c < NK; ++c) key[c] = c * 64 + lane < n_valid ? key_of(score[r * ld + c * 64 + lane]) : 0;
-        uint64_t least = 0;
-        int above = n_valid;                                                // keys >= least
+        for (int c = 0; c < NK; ++c) key[c] = c * 64 + lane < n_valid ? key_of(score[(wave * R + r) * ld + c * 64 + lane]) : 0;
+        uint64_t least = 0;                                                 // the want-th largest key, or what splits as many off
+        int above = want > 0 ? n_valid : 0;                                 // keys >= least
         if (want > 0 && want < n_valid) {
-            for (int b = 63; b >= 0 && above != want; --b) {
-                const uint64_t bound = least | 1ull << b;
-                int n = 0;
+            if constexpr (NK == 1) {
+                int rank = 0;                                               // keys above this lane's
+                for (int j = 0; j < n_valid; ++j) {
+                    const uint64_t other = (uint64_t)__builtin_amdgcn_readlane((uint32_t)(key[0] >> 32), j) << 32 | (uint32_t)__builtin_amdgcn_readlane((uint32_t)key[0], j);
+                    rank += other > key[0];
+                }
+                // those with fewer than `want` above them: as many, or more if the least of them come several times
+                const uint64_t in = __ballot(key[0] != 0 && rank < want);
+                above = __popcll(in);
+                least = 1;
+                if (above == want) {
+                    key[0] = in >> lane & 1;                                // (1: chosen)
+                } else {
+                    int most = in >> lane & 1 ? rank : -1;
 #pragma unroll
-                for (int c = 0; c < NK; ++c) n += __popcll(__ballot(key[c] >= bound));
-                if (n >= want) { least = bound; above = n; }
+                    for (int o = 32; o; o >>= 1) { const int u = __shfl_xor(most, o, 64); most = u > most ? u : most; }
+                    const int at = __builtin_ctzll(__ballot((in >> lane & 1) && rank == most));
+                    least = (uint64_t)__builtin_amdgcn_readlane((uint32_t)(key[0] >> 32), at) << 32 | (uint32_t)__builtin_amdgcn_readlane((uint32_t)key[0], at);
+                }
+            } else {
+                for (int b = 63; b >= 0 && above != want; --b) {
+                    const uint64_t bound = least | 1ull << b;
+                    int n = 0;
+#pragma unroll
+                    for (int c = 0; c < NK; ++c) n += __popcll(__ballot(key[c] >= bound));
+                    if (n >= want) { least = bound; above = n; }
+                }
             }
         }
-        // keys > least are all chosen; of those equal to it the first that are still wanted
-        int equal = 0;
+#pragma unroll
+        for (int c = 0; c < NK; ++c) chosen[c] = above ? __ballot(key[c] != 0 && key[c] >= least) : 0;
         if (above != want) {
+            // of the keys equal to the least as many too many: the last of them go
             int more = 0;
 #pragma unroll
             for (int c = 0; c < NK; ++c) more += __popcll(__ballot(key[c] > least));
-            equal = want - more;
+            int equal = want - more;
+#pragma unroll
+            for (int c = 0; c < NK; ++c) {
+                const uint64_t same = __ballot(key[c] == least);
+                const int before = __popcll(same & ((1ull << lane) - 1)), here = __popcll(same);
+                chosen[c] = __ballot(key[c] > least || (key[c] == least && before < equal));
+                equal = equal > here ? equal - here : 0;
+            }
         }
         uint32_t* out = a.blocks + ((size_t)sh * a.nq + i) * a.words;
 #pragma unroll
-        for (int c = 0; c < NK; ++c) {
-            bool in = key[c] != 0 && key[c] >= least;
-            if (above != want) {
-                const uint64_t same = __ballot(key[c] == least && key[c] != 0);
-                const int before = __popcll(same & ((1ull << lane) - 1));
-                in = key[c] > least || (key[c] == least && key[c] != 0 && before < equal);
-                const int here = __popcll(same);
-                equal = equal > here ? equal - here : 0;
-            }
-            const uint64_t word = want > 0 ? __ballot(in) : 0;
-            if (lane < 2 && 2 * c + lane < a.words) out[2 * c + lane] = (uint32_t)(word >> (32 * lane));
-        }
+        for (int c = 0; c < NK; ++c)
+            if (lane < 2 && 2 * c + lane < a.words) out[2 * c + lane] = (uint32_t)(chosen[c] >> (32 * lane));
     }
 }
 
@@ -189,18 +236,18 @@ drf_status check_select(const drf_attn_shape* s, int q_block, int kv_block)
 
 size_t side_bytes(int slots, int heads, int blocks, int d)
 {
-    return (size_t)slots * heads * ((blocks + 15) / 16) * ((d + 3) / 4) * 64 * sizeof(double);
+    return (size_t)slots * heads * ((blocks + 15) / 16 * 16) * ((d + 7) / 8 * 8) * sizeof(double);
 }
 
-template <int NK> drf_status launch_select(const SelectArgs& a, unsigned grid, size_t lds, hipStream_t st)
+template <int NK, int NW> drf_status launch_select(const SelectArgs& a, unsigned grid, size_t lds, hipStream_t st)
 {
-    auto kern = select_kernel<NK>;
+    auto kern = select_kernel<NK, NW>;
     static bool attr_set = false;
     if (!attr_set) {
-        DRF_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, 16 * (64 * NK + 2) * (int)sizeof(double)));
+        DRF_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, kRows * (64 * NK + 2) * (int)sizeof(double)));
         attr_set = true;
     }
-    hipLaunchKernelGGL(kern, dim3(grid), dim3(kThreads), lds, st, a);
+    hipLaunchKernelGGL(kern, dim3(grid), dim3(NW * 64), lds, st, a);
     DRF_HIP(hipGetLastError());
     return DRF_OK;
 }
@@ -254,7 +301,7 @@ extern "C" drf_status drf_block_select(const drf_attn_shape* shape, int q_block,
     while (parts * kWaves < s.q_heads && (long long)s.slots * (nq + nk) * parts < 2048) parts *= 2;
     const long long q_groups = (long long)s.slots * nq * parts, groups = q_groups + (long long)s.slots * nk * parts;
     const long long rows = (long long)s.slots * s.q_heads * ((nq + 15) / 16);
-    if (groups > 0x7fffffLL || rows > 0x7fffffLL) DRF_FAIL(DRF_ESHAPE, "too many blocks");
+    if (groups > 0x7fffffLL || rows > 0x1fffffLL) DRF_FAIL(DRF_ESHAPE, "too many blocks");
     auto pool = [&](auto kern) { hipLaunchKernelGGL(kern, dim3((unsigned)groups), dim3(kThreads), 0, st, qs, ks, s.head_dim, (int)q_groups, parts); };
     if (s.dtype == DRF_BF16) vec ? pool(pool_kernel<bf16_t, true>) : pool(pool_kernel<bf16_t, false>);
     else vec ? pool(pool_kernel<float, true>) : pool(pool_kernel<float, false>);
@@ -262,12 +309,12 @@ extern "C" drf_status drf_block_select(const drf_attn_shape* shape, int q_block,
 
     SelectArgs a{};
     a.q = q_sums; a.k = k_sums; a.q_tokens = s.q_tokens; a.kv_tokens = s.kv_tokens; a.q_heads = s.q_heads; a.group = s.q_heads / s.kv_heads;
-    a.q_block = q_block; a.kv_block = kv_block; a.nq = nq; a.nk = nk; a.ksteps = (s.head_dim + 3) / 4; a.topk = topk;
+    a.q_block = q_block; a.kv_block = kv_block; a.nq = nq; a.nk = nk; a.pairs = (s.head_dim + 7) / 8; a.topk = topk;
     a.words = (int)drf_block_words(s.kv_tokens, kv_block); a.q_lens = s.q_lens; a.kv_lens = s.kv_lens; a.blocks = blocks;
-    const size_t lds = (size_t)16 * ((nk + 15) / 16 * 16 + 2) * sizeof(double);
-    if (nk <= 64) return launch_select<1>(a, (unsigned)rows, lds, st);
-    if (nk <= 128) return launch_select<2>(a, (unsigned)rows, lds, st);
-    if (nk <= 256) return launch_select<4>(a, (unsigned)rows, lds, st);
-    if (nk <= 512) return launch_select<8>(a, (unsigned)rows, lds, st);
-    return launch_select<16>(a, (unsigned)rows, lds, st);
+    const size_t lds = (size_t)kRows * ((nk + 15) / 16 * 16 + 2) * sizeof(double);
+    if (nk <= 64) return launch_select<1, 4>(a, (unsigned)rows, lds, st);
+    if (nk <= 128) return launch_select<2, 16>(a, (unsigned)rows, lds, st);
+    if (nk <= 256) return launch_select<4, 16>(a, (unsigned)rows, lds, st);
+    if (nk <= 512) return launch_select<8, 16>(a, (unsigned)rows, lds, st);
+    return launch_select<16, 16>(a, (unsigned)rows, lds, st);
 }

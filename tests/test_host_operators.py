@@ -86,7 +86,7 @@ def test_block_words_and_scratch():
     assert L.drf_block_words(-1, 64) == L.drf_block_words(64, 48) == 0
     need = lambda s, qb=64, kb=64: L.drf_block_select_scratch_bytes(C.byref(s), qb, kb)  # noqa: E731
     assert need(shape()) == 2 * (4 + 4) * 16 * 64 * 8                             # one tile of 16 blocks a head
-    assert need(shape(q_tokens=2000, head_dim=61)) == 2 * 4 * (32 + 16) * 64 * 8   # columns padded to four
+    assert need(shape(q_tokens=2000, head_dim=61)) == 2 * 4 * (32 + 16) * 64 * 8   # columns padded to eight
     assert need(shape(), 16) == need(shape(dtype=5)) == need(shape(head_dim=129)) == L.drf_block_select_scratch_bytes(None, 64, 64) == 0
 
 
