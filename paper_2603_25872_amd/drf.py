@@ -290,47 +290,121 @@ def refine_step(sched, x, eps, s_from, out=None):
     return out
 
 
-def _dtype_of(t):
-    """drf_dtype of a tensor of heads."""
+# ---- attention operators: what _native does, where that module is not there ----
+
+def _heads(t, like=None, same=False):
+    """(drf_heads, dtype, shape) of a device tensor [slots, tokens, heads, head_dim] whose head columns are contiguous."""
     import torch
-    if t.dtype == torch.bfloat16:
-        return BF16
-    assert t.dtype == torch.float32, "expected bfloat16 or float32, got %s" % t.dtype
-    return F32
-
-
-def _heads(t, like=None):
-    """drf_heads of a device tensor [slots, tokens, heads, head_dim] whose head columns are contiguous."""
     assert t.is_cuda and t.dim() == 4, "need a device tensor [slots, tokens, heads, head_dim]"
     ss, ts, hs, cs = t.stride()
     assert cs == 1 or t.shape[3] < 2, "a head's columns must be contiguous"
+    assert t.dtype in (torch.bfloat16, torch.float32), "expected bfloat16 or float32"
     if like is not None:
-        assert t.dtype == like.dtype, "expected %s, got %s" % (like.dtype, t.dtype)
-        assert t.device == like.device, "tensors on %s and %s" % (like.device, t.device)
+        assert t.dtype == like.dtype, "tensors of two types"
+        assert t.device == like.device, "tensors on two devices"
+        assert not same or t.shape == like.shape, "an output must have the shape of its input"
     return Heads(t.data_ptr(), ss, ts, hs)
 
 
-def _current(t):
-    """The library launches on the current device: a tensor that is on another one is refused."""
+def _vector(t, dtype, n, like, what):
+    """Device pointer of a contiguous tensor of n elements on the device of `like`, or None."""
+    if t is None:
+        return None
+    p = _dev(t, dtype)
+    assert t.device == like.device, "tensors on two devices"
+    assert t.numel() == n, "%s must have %d elements" % (what, n)
+    return p
+
+
+def _current(x):
+    """The current stream, if x is on the current device."""
     import torch
-    assert t.is_cuda and t.device.index == torch.cuda.current_device(), "the tensor is on %s, which is not the current device" % t.device
+    device = torch.cuda.current_device()
+    assert x.device.index == device, "the tensors are not on the current device"
+    return torch._C._cuda_getCurrentRawStream(device)
 
 
-def _vector(t, n, dtype, what):
-    """Device pointer of a contiguous vector of n elements, or None."""
-    if t is not None:
-        assert t.shape == (n,), "%s must have shape (%d,)" % (what, n)
-    return _dev(t, dtype)
+class _OperatorsCtypes:
+    """The operators' marshalling with ctypes."""
+
+    @staticmethod
+    def _positions(t, config, x):
+        import torch
+        if t is None:
+            return None, 0
+        if config is None:
+            raise ValueError("positions without a rotation")
+        axes = RopeConfig.from_address(config).n_axes
+        want = (x.shape[1], axes)
+        assert tuple(t.shape) in (want, (x.shape[0],) + want), "positions must be [tokens, axes] or [slots, tokens, axes]"
+        return _vector(t, torch.float32, t.numel(), x, "positions"), x.shape[1] * axes if t.dim() == 3 else 0
+
+    @staticmethod
+    def _shape(q, k, q_lens, kv_lens):
+        import torch
+        hq, hk = _heads(q), _heads(k, q)
+        assert q.shape[0] == k.shape[0] and q.shape[3] == k.shape[3], "k must have the slots and head width of q"
+        S = q.shape[0]
+        return hq, hk, AttnShape(BF16 if q.dtype == torch.bfloat16 else F32, S, q.shape[1], k.shape[1], q.shape[2], k.shape[2], q.shape[3],
+                                 _vector(q_lens, torch.int32, S, q, "q_lens"), _vector(kv_lens, torch.int32, S, q, "kv_lens"))
+
+    @staticmethod
+    def _words(shape, q_block, kv_block):
+        return (-(-shape.q_tokens // q_block) if q_block > 0 else 0) * shape.slots * shape.q_heads * _lib.drf_block_words(shape.kv_tokens, kv_block)
+
+    @classmethod
+    def rope(cls, x, out, config, positions, lens):
+        import torch
+        hx, ho = _heads(x), _heads(out, x, True)
+        p, stride = cls._positions(positions, config, x)
+        ln = _vector(lens, torch.int32, x.shape[0], x, "lens")
+        return _lib.drf_rope(config, BF16 if x.dtype == torch.bfloat16 else F32, *x.shape, ln, p, stride, C.byref(hx), C.byref(ho), _current(x))
+
+    @classmethod
+    def qk_norm_rope(cls, q, k, q_out, k_out, norm, eps, q_scale, q_gain, q_bias, k_gain, k_bias, config, positions, lens):
+        import torch
+        hq, hk, hqo, hko = _heads(q), _heads(k, q), _heads(q_out, q, True), _heads(k_out, k, True)
+        assert q.shape[:2] == k.shape[:2] and q.shape[3] == k.shape[3], "k must have the slots, tokens and head width of q"
+        cfg = QkConfig(norm, eps, q_scale, *(_vector(t, torch.float32, q.shape[3], q, "a norm's parameters") for t in (q_gain, q_bias, k_gain, k_bias)))
+        p, stride = cls._positions(positions, config, q)
+        S, N, H, d = q.shape
+        shape = AttnShape(BF16 if q.dtype == torch.bfloat16 else F32, S, N, N, H, k.shape[2], d, _vector(lens, torch.int32, S, q, "lens"), None)
+        return _lib.drf_qk_norm_rope(C.byref(cfg), config, C.byref(shape), p, stride, C.byref(hq), C.byref(hk), C.byref(hqo), C.byref(hko), _current(q))
+
+    @classmethod
+    def block_select(cls, q, k, out, q_block, kv_block, topk, q_lens, kv_lens, scratch):
+        import torch
+        hq, hk, shape = cls._shape(q, k, q_lens, kv_lens)
+        n = _lib.drf_block_select_scratch_bytes(C.byref(shape), q_block, kv_block)
+        o = _vector(out, torch.int32, cls._words(shape, q_block, kv_block), q, "the blocks' words")
+        sc = _vector(scratch, torch.float32, n // 4, q, "scratch")
+        return _lib.drf_block_select(C.byref(shape), q_block, kv_block, topk, C.byref(hq), C.byref(hk), sc, n, o, _current(q))
+
+    @classmethod
+    def block_attention(cls, q, k, v, blocks, out, q_block, kv_block, scale, q_lens, kv_lens):
+        import torch
+        hq, hk, shape = cls._shape(q, k, q_lens, kv_lens)
+        hv, ho = _heads(v, k, True), _heads(out, q, True)
+        w = _vector(blocks, torch.int32, cls._words(shape, q_block, kv_block), q, "the blocks' words")
+        return _lib.drf_block_attention(C.byref(shape), q_block, kv_block, scale, w, C.byref(hq), C.byref(hk), C.byref(hv), C.byref(ho), _current(q))
 
 
-def _positions(positions, rope, slots, tokens):
-    """(device pointer, stride between slots) of a table [tokens, axes] or [slots, tokens, axes]."""
+_ops = None             # _native or _OperatorsCtypes, at the first operator
+
+
+def _operators():
+    global _ops
     import torch
-    if positions is None:
-        return None, 0
-    want = (tokens, rope.n_axes)
-    assert tuple(positions.shape) in (want, (slots,) + want), "positions must be [tokens, axes] or [slots, tokens, axes]"
-    return _dev(positions, torch.float32), tokens * rope.n_axes if positions.dim() == 3 else 0
+    L = lib()
+    try:
+        from . import _native
+        _native.bind_operators(tuple(C.cast(f, C.c_void_p).value for f in (L.drf_rope, L.drf_qk_norm_rope, L.drf_block_words, L.drf_block_select_scratch_bytes,
+                                                                           L.drf_block_select, L.drf_block_attention)),
+                               torch.float32, torch.bfloat16, torch.int32, torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream)
+        _ops = _native
+    except ImportError:
+        _ops = _OperatorsCtypes
+    return _ops
 
 
 def rope_config(dims, extents, theta=10000.0, layout="pairs", origin=None, step=None):
@@ -347,63 +421,39 @@ def rope_config(dims, extents, theta=10000.0, layout="pairs", origin=None, step=
 
 
 def rope(x, config, positions=None, lens=None, out=None):
-    """x [slots, tokens, heads, head_dim] (any strides but the last) with its columns turned by their positions; out may be x."""
+    """x [slots, tokens, heads, head_dim] (any strides but the last) with its columns turned by their positions; out may be x.  Rows behind a
+    slot's length are left as they were: those of x in an output made here."""
     import torch
-    _current(x)
-    S, N, H, d = x.shape
     if out is None:
         out = torch.empty_like(x) if lens is None else x.clone()
-    assert out.shape == x.shape, "out must have the shape of x"
-    p, stride = _positions(positions, config, S, N)
-    _check(lib().drf_rope(C.byref(config), _dtype_of(x), S, N, H, d, _vector(lens, S, torch.int32, "lens"), p, stride, C.byref(_heads(x)),
-                          C.byref(_heads(out, x)), _stream()))
+    _check((_ops or _operators()).rope(x, out, C.addressof(config), positions, lens))
     return out
 
 
 def qk_norm_rope(q, k, norm, config=None, q_gain=None, k_gain=None, q_bias=None, k_bias=None, eps=1e-6, q_scale=1.0, positions=None, lens=None,
                  q_out=None, k_out=None):
-    """Norm ("none", "rms", "layer") of every head of q and k [slots, tokens, heads, head_dim], then the rotation; returns (q_out, k_out)."""
+    """Norm ("none", "rms", "layer") of every head of q and k [slots, tokens, heads, head_dim], then the rotation; returns (q_out, k_out).  Outputs may
+    be their inputs; rows behind a slot's length as in rope()."""
     import torch
-    _current(q)
-    S, N, H, d = q.shape
-    assert k.shape[:2] == q.shape[:2] and k.shape[3] == d, "k must have the slots, tokens and head width of q"
     if q_out is None:
         q_out = torch.empty_like(q) if lens is None else q.clone()
     if k_out is None:
         k_out = torch.empty_like(k) if lens is None else k.clone()
-    assert q_out.shape == q.shape and k_out.shape == k.shape, "outputs must have the shapes of their inputs"
-    cfg = QkConfig(_QK[norm], float(eps), float(q_scale), *(_vector(t, d, torch.float32, what) for t, what in (
-        (q_gain, "q_gain"), (q_bias, "q_bias"), (k_gain, "k_gain"), (k_bias, "k_bias"))))
-    shape = AttnShape(_dtype_of(q), S, N, N, H, k.shape[2], d, _vector(lens, S, torch.int32, "lens"), None)
-    if positions is not None and config is None:
-        raise ValueError("positions without a rotation")
-    p, stride = _positions(positions, config, S, N)
-    _check(lib().drf_qk_norm_rope(C.byref(cfg), C.byref(config) if config is not None else None, C.byref(shape), p, stride, C.byref(_heads(q)),
-                                  C.byref(_heads(k, q)), C.byref(_heads(q_out, q)), C.byref(_heads(k_out, q)), _stream()))
+    _check((_ops or _operators()).qk_norm_rope(q, k, q_out, k_out, _QK[norm], float(eps), float(q_scale), q_gain, q_bias, k_gain, k_bias,
+                                               None if config is None else C.addressof(config), positions, lens))
     return q_out, k_out
-
-
-def _shape(q, k, q_lens, kv_lens):
-    import torch
-    _current(q)
-    S, N, H, d = q.shape
-    assert k.shape[0] == S and k.shape[3] == d, "k must have the slots and head width of q"
-    return AttnShape(_dtype_of(q), S, N, k.shape[1], H, k.shape[2], d, _vector(q_lens, S, torch.int32, "q_lens"), _vector(kv_lens, S, torch.int32, "kv_lens"))
 
 
 def block_select(q, k, q_block, kv_block, topk, q_lens=None, kv_lens=None, out=None):
     """Bit words [slots, heads, query blocks, words] (int32) of the topk key blocks whose mean lies nearest each query block's mean."""
     import torch
-    shape = _shape(q, k, q_lens, kv_lens)
-    L = lib()
-    size = (shape.slots, shape.q_heads, -(-shape.q_tokens // q_block) if q_block > 0 else 0, L.drf_block_words(shape.kv_tokens, kv_block))
+    ops = _ops or _operators()
+    S, N, H, d = q.shape
     if out is None:
-        out = torch.empty(size, dtype=torch.int32, device=q.device)
-    assert tuple(out.shape) == size, "out must be %s" % (size,)
-    n = L.drf_block_select_scratch_bytes(C.byref(shape), q_block, kv_block)
-    scratch = torch.empty(n, dtype=torch.uint8, device=q.device)
-    _check(L.drf_block_select(C.byref(shape), q_block, kv_block, topk, C.byref(_heads(q)), C.byref(_heads(k, q)), scratch.data_ptr(), n,
-                              _dev(out, torch.int32), _stream()))
+        out = torch.empty((S, H, -(-N // q_block) if q_block > 0 else 0, _lib.drf_block_words(k.shape[1], kv_block)), dtype=torch.int32, device=q.device)
+    shape = AttnShape(F32, S, N, k.shape[1], H, k.shape[2], d, None, None)
+    scratch = torch.empty(_lib.drf_block_select_scratch_bytes(C.byref(shape), q_block, kv_block) // 4, dtype=torch.float32, device=q.device)
+    _check(ops.block_select(q, k, out, q_block, kv_block, topk, q_lens, kv_lens, scratch))
     return out
 
 
@@ -411,15 +461,9 @@ def block_attention(q, k, v, blocks, q_block, kv_block, scale=None, q_lens=None,
     """softmax(scale q k^T) v over the key blocks that the words `blocks` (as block_select gives them) name for each query block; scale
     1 / sqrt(head_dim) by default.  Rows behind a slot's q length are left as they were: zeros in an output made here."""
     import torch
-    shape = _shape(q, k, q_lens, kv_lens)
-    assert v.shape == k.shape, "v must have the shape of k"
-    size = (shape.slots, shape.q_heads, -(-shape.q_tokens // q_block) if q_block > 0 else 0, lib().drf_block_words(shape.kv_tokens, kv_block))
-    assert tuple(blocks.shape) == size, "blocks must be %s" % (size,)
     if out is None:
         out = (torch.empty if q_lens is None else torch.zeros)(q.shape, dtype=q.dtype, device=q.device)
-    assert out.shape == q.shape, "out must have the shape of q"
-    _check(lib().drf_block_attention(C.byref(shape), q_block, kv_block, shape.head_dim ** -0.5 if scale is None else scale, _dev(blocks, torch.int32),
-                                     C.byref(_heads(q)), C.byref(_heads(k, q)), C.byref(_heads(v, q)), C.byref(_heads(out, q)), _stream()))
+    _check((_ops or _operators()).block_attention(q, k, v, blocks, out, q_block, kv_block, q.shape[3] ** -0.5 if scale is None else scale, q_lens, kv_lens))
     return out
 
 

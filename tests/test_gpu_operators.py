@@ -520,3 +520,38 @@ def test_two_streams_at_once(torch, drf):
     torch.cuda.synchronize()
     for n, g in enumerate(got):
         assert all(torch.equal(a, b) for a, b in zip(g, want[n % 2])), n
+
+
+# ---- the binding -------------------------------------------------------------------------------------------
+
+
+def test_both_marshallings_give_the_same(torch, drf, monkeypatch):
+    """The calls through the CPython module and through ctypes: results bit for bit, and the same tensors refused before anything is launched."""
+    torch.manual_seed(2)
+    x = torch.randn(2, 70, 3, 4, 64, device="cuda").bfloat16()
+    cfg, gains, lens = drf.rope_config((32, 32), (1, 9)), torch.rand(64, device="cuda"), torch.tensor([70, 31], dtype=torch.int32, device="cuda")
+    table = torch.rand(2, 70, 2, device="cuda")
+    q, k, v = x.unbind(2)
+    f = q.float()
+    words = drf.block_select(q, k, 32, 32, 2)
+    forms = (drf._operators(), drf._OperatorsCtypes)
+    assert forms[0] is not forms[1]                                             # built beside the library here
+    got = []
+    for form in forms:
+        monkeypatch.setattr(drf, "_ops", form)
+        out = [drf.rope(q, cfg), drf.rope(f, cfg, positions=table, lens=lens), *chain(drf, x.clone(), cfg, gains, 32, 64, 1, lens),
+               *drf.qk_norm_rope(q, k[:, :, :2], "layer", None, gains, gains, gains, gains, q_scale=2.0), drf.block_attention(q, k, v, words, 32, 32, scale=0.5)]
+        bad = []
+        for call in (lambda: drf.rope(q, cfg, out=f), lambda: drf.rope(q, cfg, out=k[:, :69]), lambda: drf.rope(q[0], cfg), lambda: drf.rope(q.half(), cfg),
+                     lambda: drf.rope(q.transpose(2, 3), cfg), lambda: drf.rope(q.cpu(), cfg), lambda: drf.rope(q, cfg, lens=lens.long()), lambda: drf.rope(q, cfg, lens=lens[:1]),
+                     lambda: drf.rope(q, cfg, lens=lens.cpu()), lambda: drf.rope(q, cfg, positions=table[:, :, :1]), lambda: drf.rope(q, cfg, positions=table[0, 0]),
+                     lambda: drf.qk_norm_rope(q, k, "rms", None, positions=table), lambda: drf.qk_norm_rope(q, k[:, 1:], "rms"), lambda: drf.qk_norm_rope(q, k, "rms", q_gain=gains[1:]),
+                     lambda: drf.qk_norm_rope(q, k, "none", q_gain=gains), lambda: drf.qk_norm_rope(q, k, "rms", q_bias=gains), lambda: drf.block_select(q, k[:1], 32, 32, 1),
+                     lambda: drf.block_select(q, k, 48, 32, 1), lambda: drf.block_select(q, k, 32, 32, 0), lambda: drf.block_select(q, k[:, :, :3], 32, 32, 1),
+                     lambda: drf.block_attention(q, k, v, words[..., :0], 32, 32), lambda: drf.block_attention(q, k, v, words, 64, 32), lambda: drf.block_attention(q, k, f, words, 32, 32),
+                     lambda: drf.block_attention(q, k, v, words, 32, 32, scale=-1.0), lambda: drf.block_attention(q, k, v.contiguous()[:, 1:], words, 32, 32)):
+            with pytest.raises((AssertionError, ValueError, drf.DrfError)) as e:
+                call()
+            bad.append((type(e.value), e.value.status if isinstance(e.value, drf.DrfError) else None))
+        got.append((out, bad))
+    assert all(torch.equal(a, b) for a, b in zip(got[0][0], got[1][0])) and got[0][1] == got[1][1]
