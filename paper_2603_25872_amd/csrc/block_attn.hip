@@ -387,12 +387,12 @@ __global__ void __launch_bounds__(64 * W, P8 > 11 && QB == 2 ? 1 : 2) block_attn
             }
             // Matrix instruction m of the NM beside which this buffer is refilled, a copy or two behind each: all of them at once would keep the
             // wave from issuing anything else until the CU's one path to memory had taken them.
-            constexpr int NM = (QB == 2 ? KS : 0) + 2 * DT;
+            constexpr int NM = (QB == 2 ? KS : 0) + 2 * DT, PER = NM > 0 ? NM : 1;
             auto refill = [&](int m) {
                 if constexpr (ISSUE) {
                     if (m == 0) asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");        // the values' fragments are out
 #pragma unroll
-                    for (int j = m * COPIES / NM; j < (m + 1) * COPIES / NM; ++j) copy(n2, buf, j);
+                    for (int j = m * COPIES / PER; j < (m + 1) * COPIES / PER; ++j) copy(n2, buf, j);
                     __builtin_amdgcn_sched_barrier(0x406);      // vector and scalar arithmetic may cross
                 }
             };
@@ -445,11 +445,12 @@ __global__ void __launch_bounds__(64 * W, P8 > 11 && QB == 2 ? 1 : 2) block_attn
         run(std::true_type{}, n0, n1);
     } else {
         run(std::false_type{}, n0, n1);
-        // Scores so far above the first step's that a sum overflows (or anything that is not a number, which stays what it is): once more
-        // with a reference that follows them.
+        // Scores so far above the first step's that a sum overflows (or anything that is not a number, which stays what it is), or a first step
+        // that was all of -infinity and so no reference, below which all others may vanish: once more with a reference that follows them.
         float top = 0.f;
 #pragma unroll
         for (int b = 0; b < QB; ++b) {
+            if (m_run[b] == kNone) top = INFINITY;
             if (!C::ONES) top = __builtin_elementwise_maximum(top, l_run[b]);
 #pragma unroll
             for (int t = 0; t < DT; ++t)

@@ -252,56 +252,56 @@ template <typename T, int NORM>
 __global__ void __launch_bounds__(kThreads) heads_any_kernel(const HeadsArgs a, long long rows)
 {
     const int lane = threadIdx.x & 63, d = a.d, all = a.q.heads + a.k.heads;
-    const long long row = (long long)blockIdx.x * kWaves + (threadIdx.x >> 6);
-    if (row >= rows) return;
-    const int hh = (int)(row % all);
-    const long long sn = row / all;
-    const int slot = (int)(sn / a.tokens), n = (int)(sn % a.tokens), w = hh >= a.q.heads, h = w ? hh - a.q.heads : hh;
-    if (n >= slot_len(a.lens, slot, a.tokens)) return;
-    const Side& e = w ? a.k : a.q;
-    const T* x = (const T*)e.x + slot * e.xs + (int64_t)n * e.xt + h * e.xh;
-    T* y = (T*)e.y + slot * e.ys + (int64_t)n * e.yt + h * e.yh;
-    auto wave_sum = [](float v) {
+    for (long long row = (long long)blockIdx.x * kWaves + (threadIdx.x >> 6); row < rows; row += (long long)gridDim.x * kWaves) {
+        const int hh = (int)(row % all);
+        const long long sn = row / all;
+        const int slot = (int)(sn / a.tokens), n = (int)(sn % a.tokens), w = hh >= a.q.heads, h = w ? hh - a.q.heads : hh;
+        if (n >= slot_len(a.lens, slot, a.tokens)) continue;
+        const Side& e = w ? a.k : a.q;
+        const T* x = (const T*)e.x + slot * e.xs + (int64_t)n * e.xt + h * e.xh;
+        T* y = (T*)e.y + slot * e.ys + (int64_t)n * e.yt + h * e.yh;
+        auto wave_sum = [](float v) {
 #pragma unroll
-        for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o, 64);
-        return v;
-    };
-    float v[2], o[2];
-    int oc[2];
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-        const int c = lane + 64 * j;
-        oc[j] = c < d ? (c < a.r.columns ? a.r.other[c] : c) : 0;
-        v[j] = c < d ? to_f32(x[c]) : 0.f;
-        o[j] = c < d ? to_f32(x[oc[j]]) : 0.f;
-    }
-    float mean = 0.f, inv = 1.f;
-    if constexpr (NORM == DRF_QK_LAYER) mean = wave_sum(v[0] + v[1]) / (float)d;
-    if constexpr (NORM != DRF_QK_NONE) {
-        float s = 0.f;
-#pragma unroll
-        for (int j = 0; j < 2; ++j) s += lane + 64 * j < d ? (v[j] - mean) * (v[j] - mean) : 0.f;
-        inv = 1.f / sqrtf(wave_sum(s) / (float)d + a.eps);
-    }
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-        const int c = lane + 64 * j;
-        if (c >= d) continue;
-        auto affine = [&](float z, int col) {
-            z = (z - mean) * inv;
-            if (e.gain) z *= e.gain[col];
-            if (e.bias) z += e.bias[col];
-            return z * e.scale;
+            for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o, 64);
+            return v;
         };
-        float r = affine(v[j], c);
-        if (c < a.r.columns) {
-            const Pair& p = a.r.rec[a.r.pair[c]];
-            float cs, sn_;
-            turn(position(a.r, slot, n, p.axis), p.turns, &cs, &sn_);
-            const float z = affine(o[j], oc[j]);
-            r = p.first == c ? fmaf(r, cs, -z * sn_) : fmaf(r, cs, z * sn_);
+        float v[2], o[2];
+        int oc[2];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const int c = lane + 64 * j;
+            oc[j] = c < d ? (c < a.r.columns ? a.r.other[c] : c) : 0;
+            v[j] = c < d ? to_f32(x[c]) : 0.f;
+            o[j] = c < d ? to_f32(x[oc[j]]) : 0.f;
         }
-        y[c] = (T)r;
+        float mean = 0.f, inv = 1.f;
+        if constexpr (NORM == DRF_QK_LAYER) mean = wave_sum(v[0] + v[1]) / (float)d;
+        if constexpr (NORM != DRF_QK_NONE) {
+            float s = 0.f;
+#pragma unroll
+            for (int j = 0; j < 2; ++j) s += lane + 64 * j < d ? (v[j] - mean) * (v[j] - mean) : 0.f;
+            inv = 1.f / sqrtf(wave_sum(s) / (float)d + a.eps);
+        }
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const int c = lane + 64 * j;
+            if (c >= d) continue;
+            auto affine = [&](float z, int col) {
+                z = (z - mean) * inv;
+                if (e.gain) z *= e.gain[col];
+                if (e.bias) z += e.bias[col];
+                return z * e.scale;
+            };
+            float r = affine(v[j], c);
+            if (c < a.r.columns) {
+                const Pair& p = a.r.rec[a.r.pair[c]];
+                float cs, sn_;
+                turn(position(a.r, slot, n, p.axis), p.turns, &cs, &sn_);
+                const float z = affine(o[j], oc[j]);
+                r = p.first == c ? fmaf(r, cs, -z * sn_) : fmaf(r, cs, z * sn_);
+            }
+            y[c] = (T)r;
+        }
     }
 }
 
@@ -371,8 +371,7 @@ template <typename T> drf_status launch(HeadsArgs& a, int norm, int rope, bool v
 {
     const int all = a.q.heads + a.k.heads;
     if (!vec) {
-        const long long rows = (long long)a.slots * a.tokens * all, grid = (rows + kWaves - 1) / kWaves;
-        if (grid > 0x7fffffLL) DRF_FAIL(DRF_ESHAPE, "too many unaligned rows");
+        const long long rows = (long long)a.slots * a.tokens * all, most = (rows + kWaves - 1) / kWaves, grid = most < 1 << 20 ? most : 1 << 20;
         if (norm == DRF_QK_NONE) hipLaunchKernelGGL((heads_any_kernel<T, DRF_QK_NONE>), dim3((unsigned)grid), dim3(kThreads), 0, st, a, rows);
         else if (norm == DRF_QK_RMS) hipLaunchKernelGGL((heads_any_kernel<T, DRF_QK_RMS>), dim3((unsigned)grid), dim3(kThreads), 0, st, a, rows);
         else hipLaunchKernelGGL((heads_any_kernel<T, DRF_QK_LAYER>), dim3((unsigned)grid), dim3(kThreads), 0, st, a, rows);

@@ -421,6 +421,95 @@ def test_block_attention_scores_of_minus_infinity(torch, drf, dtype):
         check(drf.block_attention(q, k, v, pack(torch, mask), 32, 32), want, dtype, slack_of(dtype, d, mag, size))
 
 
+def many(torch, drf, q, k, v, mask, qv, kv, vv, q_block, kv_block, tiles, q_lens=None, kv_lens=None, out=None, scale=None):
+    """Attention on as many copies of the slots as give `tiles` 32-query tiles (how many there are chooses how waves share them): every copy's
+    result is the first one's, which has the float64 result."""
+    S, N, H, d = q.shape
+    c = -(-tiles // (-(-N // 32) * H * S))
+    more = lambda t: None if t is None else t.repeat((c,) + (1,) * (t.dim() - 1))  # noqa: E731
+    dev = lambda a: None if a is None else more(torch.from_numpy(a).cuda())  # noqa: E731
+    got = drf.block_attention(more(q), more(k), more(v), more(pack(torch, mask)), q_block, kv_block, scale, dev(q_lens), dev(kv_lens), out=more(out))
+    want, mag, size = attended(qv, kv, vv, mask, q_block, kv_block, d ** -0.5 if scale is None else scale, q_lens, kv_lens)
+    if out is not None:
+        inside = np.broadcast_to((np.arange(N)[None] < (np.full(S, N) if q_lens is None else q_lens)[:, None])[:, :, None, None], want.shape)
+        want = np.where(inside, want, out.double().cpu().numpy())
+    check(got[:S], want, "bf16", slack_of("bf16", d, mag, size))
+    got = got.view(torch.int16).view(c, S, N, H, d)
+    assert torch.equal(got, got[:1].expand_as(got))
+
+
+# Tiles where a wave takes 32 queries of its own, and 64.
+TILES = [600, 1100]
+
+
+@pytest.mark.parametrize("tiles", TILES)
+@pytest.mark.parametrize("d", range(8, 129, 8))
+@pytest.mark.parametrize("N,M,q_block,kv_block", [(1, 33, 32, 32), (97, 257, 128, 64), (200, 390, 64, 32), (65, 64, 64, 64), (130, 700, 128, 128)])
+def test_block_attention_of_many_tiles(torch, drf, tiles, d, N, M, q_block, kv_block):
+    rng = np.random.default_rng(d + N)
+    (q, qv), (k, kv), (v, vv) = (tensor(torch, rng, (2, n, h, d), "bf16", "rows") for n, h in ((N, 4), (M, 2), (M, 2)))
+    many(torch, drf, q, k, v, random_mask(rng, 2, 4, N, M, q_block, kv_block, 0.5), qv, kv, vv, q_block, kv_block, tiles)
+
+
+@pytest.mark.parametrize("tiles", TILES)
+@pytest.mark.parametrize("d", [24, 64, 72, 128])
+@pytest.mark.parametrize("steepest", [1.0, 4.0, 16.0])
+def test_block_attention_of_many_tiles_scores_that_grow(torch, drf, tiles, d, steepest):
+    """The first step's scores are small, later ones larger: by what sums in fp32 hold beside them, and by far more."""
+    rng = np.random.default_rng(d)
+    N, M = 96, 640
+    (q, _), (k, _), (v, vv) = (tensor(torch, rng, (1, n, 2, d), "bf16", "plain") for n in (N, M, M))
+    q, k = (q * 2).to(q.dtype), (k * torch.linspace(0.2, steepest, M, device="cuda").view(1, M, 1, 1)).to(k.dtype)
+    for turn in (k, k.flip(1)):
+        many(torch, drf, q, turn, v, random_mask(rng, 1, 2, N, M, 64, 32, 0.7), q.double().cpu().numpy(), turn.double().cpu().numpy(), vv, 64, 32, tiles)
+
+
+@pytest.mark.parametrize("tiles", [1] + TILES)
+@pytest.mark.parametrize("d", [40, 64, 72])
+def test_block_attention_of_many_tiles_lengths_and_masked_places(torch, drf, tiles, d):
+    rng = np.random.default_rng(d)
+    S, N, H, qb, kb = 6, 170, 2, 64, 32
+    q_lens, kv_lens = np.array([0, 1, 65, 170, 500, 128], np.int32), np.array([170, 33, 0, 169, 1, -7], np.int32)
+    mask = random_mask(rng, S, H, N, N, qb, kb, 0.5)
+    mask[:, 1] = mask[:, 0]
+    (q, qv), (k, kv), (v, vv) = (tensor(torch, rng, (S, N, H, d), "bf16", "rows") for _ in range(3))
+    used = np.repeat(mask.any((1, 2)), kb, axis=1)[:, :N] & (np.arange(N)[None] < kv_lens[:, None])
+    for t in (k, v):
+        t[torch.from_numpy(~used).cuda()] = float("nan")
+    q[torch.from_numpy(np.arange(N)[None] >= q_lens[:, None]).cuda()] = float("inf")
+    out = torch.full((S, N, H, d), 7.0, dtype=q.dtype, device="cuda")
+    kv, vv = (np.where(used[:, :, None, None], x, 0) for x in (kv, vv))
+    many(torch, drf, q, k, v, mask, qv, kv, vv, qb, kb, tiles, q_lens, kv_lens, out)
+
+
+@pytest.mark.parametrize("tiles", [1] + TILES)
+@pytest.mark.parametrize("d", [64, 72])
+def test_block_attention_behind_a_step_of_no_weight(torch, drf, tiles, d):
+    """A list's first keys score -infinity, the others so low that their exponentials alone would vanish."""
+    rng = np.random.default_rng(d)
+    N, M = 96, 160
+    (q, qv), (k, kv), (v, vv) = (tensor(torch, rng, (1, n, 2, d), "bf16", "plain") for n in (N, M, M))
+    q[..., 0] = 1.0
+    qv[..., 0] = 1.0
+    q[..., 1:], qv[..., 1:] = q[..., 1:] / 4, qv[..., 1:] / 4                  # (exact)
+    kv[:, :64, :, 0], kv[:, 64:, :, 0] = -np.inf, -8192.0
+    k.copy_(torch.from_numpy(kv))
+    mask = np.ones((1, 2, 2, 5), bool)
+    mask[0, 1, 1] = [1, 0, 0, 0, 1]
+    many(torch, drf, q, k, v, mask, qv, kv, vv, 64, 32, tiles)
+
+
+@pytest.mark.parametrize("S,N,M", [(0, 5, 5), (2, 0, 40), (2, 40, 0)])
+def test_operators_of_nothing(torch, drf, S, N, M):
+    q, k = (torch.randn(S, n, 2, 64, device="cuda").bfloat16() for n in (N, M))
+    cfg = drf.rope_config((64,), (1,))
+    assert drf.rope(q, cfg).shape == q.shape
+    assert drf.qk_norm_rope(q, q, "rms", cfg)[0].shape == q.shape
+    words = drf.block_select(q, k, 32, 32, 2)
+    assert words.shape == (S, 2, -(-N // 32), -(-M // 32 // 32))
+    assert not drf.block_attention(q, k, k, words, 32, 32).any()
+
+
 def test_block_attention_ignores_bits_behind_the_last_block(torch, drf):
     rng = np.random.default_rng(8)
     (q, _), (k, _), (v, _) = (tensor(torch, rng, (1, 70, 2, 64), "bf16", "plain") for _ in range(3))
