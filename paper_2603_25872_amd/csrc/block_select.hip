@@ -33,7 +33,9 @@ __device__ inline int slot_len(const int32_t* lens, int slot, int tokens)
     return n < 0 ? 0 : n < tokens ? n : tokens;
 }
 
-// A wave takes a head of a block: 64 / P rows at a time in pieces of 16 bytes (VEC), or a row at a time, a column or two a lane.
+// A wave takes a head of a block: 64 / P rows at a time in pieces of 16 bytes (VEC), or a row at a time, a column or two a lane.  Bound by the read
+// of q and k: 64 slots x 1024 tokens x 32 heads of 72 in bf16, 302 MB, 63 us (4.8 TB/s); 2 x 19344 x 16 heads of 64 in fp32, 158 MB, 39 us
+// (4.0) from memory and 16 out of the Infinity Cache.  Six rows in flight a lane, and a block's sums stored as one row: by columns, where 8 bytes of a line leave at a time, the first took 87 us.
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(kThreads) pool_kernel(const PoolSide q, const PoolSide k, int d, int q_groups, int parts)
 {
@@ -110,14 +112,16 @@ struct SelectArgs {
 
 // A workgroup takes 16 query blocks of a (slot, head): their scores against all key blocks on the 16 x 16 x 4 matrix instruction into LDS, then a
 // wave row after row.  Up to 64 blocks a row (NK = 1, a key a lane) every key's rank is counted against one key after another, four
-// instructions each; more of them have the topk-th largest key found by bisection over its bits, on scalars but for the comparisons (counting by
-// ballots, until a bound splits off exactly topk).  Latency bounds both, and with many rows of few blocks the instructions (64 slots x 16 heads x
-// 16 rows of 16 blocks).  NK: keys of a row that a lane holds; NW: waves.
+// instructions each; more of them have the topk-th largest key found by bisection over its bits, the upper 32 first, on scalars but for the
+// comparisons (counting by ballots, until a bound splits off exactly topk).  Latency bounds both, and with many rows of few blocks the instructions:
+// 2 slots x 8 heads x 152 rows of 303 blocks 16 us on 160 workgroups (21.9 with two batches of sums a tile and 64-bit comparisons throughout; 4 of
+// it are the bisection), 64 x 16 x 16 rows of 16 blocks 11.  Nine pairs at once are slower where eight do (17.0).  NK: keys of a row that a lane
+// holds; NW: waves.
 constexpr int kRows = 16;
 template <int NK, int NW>
 __global__ void __launch_bounds__(NW * 64) select_kernel(const SelectArgs a)
 {
-    constexpr int R = kRows / NW, kPairs = 6;                               // pairs of k-steps asked for at once
+    constexpr int R = kRows / NW, kPairs = NW == 16 ? 8 : 6;                // pairs of k-steps asked for at once
     extern __shared__ __attribute__((aligned(16))) double score[];          // [16][nk padded]
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int qtiles = (a.nq + 15) / 16, ktiles = (a.nk + 15) / 16, ld = ktiles * 16 + 2;
@@ -134,15 +138,16 @@ __global__ void __launch_bounds__(NW * 64) select_kernel(const SelectArgs a)
     const int width = 8 * a.pairs;
     const double* q = a.q + (((size_t)sh * qtiles + qt) * 16 + (lane & 15)) * width + 2 * (lane >> 4);
     const double* k = a.k + (((size_t)slot * (a.q_heads / a.group) + h / a.group) * ktiles * 16 + (lane & 15)) * width + 2 * (lane >> 4);
+    f64x2 qv[kPairs];                                                       // stay where they are all of a row's
     for (int t = wave; t < ktiles; t += NW) {
         const double* kt = k + (size_t)t * 16 * width;
         f64x4 acc[2] = { { 0.0, 0.0, 0.0, 0.0 }, { 0.0, 0.0, 0.0, 0.0 } };
         for (int s0 = 0; s0 < a.pairs; s0 += kPairs) {
-            f64x2 qv[kPairs], kv[kPairs];
+            f64x2 kv[kPairs];
 #pragma unroll
             for (int j = 0; j < kPairs; ++j) {
                 const int s = s0 + j < a.pairs ? s0 + j : a.pairs - 1;
-                qv[j] = *reinterpret_cast<const f64x2*>(q + s * 8);
+                if (t == wave || a.pairs > kPairs) qv[j] = *reinterpret_cast<const f64x2*>(q + s * 8);
                 kv[j] = *reinterpret_cast<const f64x2*>(kt + s * 8);
             }
 #pragma unroll
@@ -188,7 +193,18 @@ __global__ void __launch_bounds__(NW * 64) select_kernel(const SelectArgs a)
                     least = (uint64_t)__builtin_amdgcn_readlane((uint32_t)(key[0] >> 32), at) << 32 | (uint32_t)__builtin_amdgcn_readlane((uint32_t)key[0], at);
                 }
             } else {
-                for (int b = 63; b >= 0 && above != want; --b) {
+                uint32_t high[NK], low = 0;
+#pragma unroll
+                for (int c = 0; c < NK; ++c) high[c] = (uint32_t)(key[c] >> 32);
+                for (int b = 31; b >= 0 && above != want; --b) {
+                    const uint32_t bound = low | 1u << b;
+                    int n = 0;
+#pragma unroll
+                    for (int c = 0; c < NK; ++c) n += __popcll(__ballot(high[c] >= bound));
+                    if (n >= want) { low = bound; above = n; }
+                }
+                least = (uint64_t)low << 32;
+                for (int b = 31; b >= 0 && above != want; --b) {
                     const uint64_t bound = least | 1ull << b;
                     int n = 0;
 #pragma unroll
