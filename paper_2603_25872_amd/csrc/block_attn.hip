@@ -111,7 +111,10 @@ __device__ inline float max3(float a, float b, float c) { return __builtin_eleme
 // the only waits are for the copies of a step that were asked for a whole step before.  Two buffers of 32 keys: while a step is computed the
 // fragments of the next are read out of one and the step after it lands in the other.  With QB = 2 every fragment is used twice and one
 // block's scores are formed beside the other's exponentials.  W waves share a tile of queries where there are few (each takes every W-th
-// step; joined through LDS).
+// step; joined through LDS).  Bound by the matrix instructions and, beside them, the exponentials and the way of K and V into LDS: 4 slots x 16384
+// queries x 12 heads of 128 over 16 of 128 blocks of 128, 825 GFLOP, 0.90 - 0.94 ms, 0.9 PFLOP/s (a large library product reaches 1.23 here, the
+// instruction by itself 1.94; without the copies it would be 0.73, without their waits the same).  6 x 4096 x 16 of 72 over 8 of 64 blocks of 64,
+// 58 GFLOP over 226 MB of q, k, v and result, 82 us, 97 with nothing of them in the caches: half of it is that read.
 template <int P8, int QB, int W>
 __global__ void __launch_bounds__(64 * W, P8 > 11 && QB == 2 ? 1 : 2) block_attn_kernel(const BlockArgs a, int q_tiles, int n_items)
 {
@@ -575,13 +578,20 @@ __global__ void __launch_bounds__(64 * W, P8 > 11 && QB == 2 ? 1 : 2) block_attn
     }
 }
 
-// fp32 on the fp32 matrix instruction (16 x 16 x 4), operands straight from memory, a step's all asked for at once; DQ = ceil(d / 16).
-// VEC: width, strides and addresses allow 16-byte loads of Q and K.
+// fp32 on the fp32 matrix instruction (16 x 16 x 4), operands straight from memory, a step's all asked for at once; DQ >= ceil(d / 16) tiles of
+// columns.  Few steps: bound by the chain of a mask word, a step's rows, its products and exponentials and the join; many: by the loads' way through
+// the CU's one path and the products in turn.  A lane's column of V is one of each of up to four tiles, so that they come in one load: 7 slots x
+// 1000 queries x 4 heads of 32 over 5 of 32 blocks of 32 take 14.8 us (15.7 with a tile's columns side by side, 4 bytes a load), 4 x 1024 x 8 of 64
+// over 4 of 16 blocks of 64 43 (50), 12 x 256 x 16 of 72 over 2 of 4 51 (64, of which 5 are columns behind the width), 2 x 4096 x 8 of 128 over 8 of
+// 64 280 (312; 17.2 GFLOP).
+// VEC: width, strides and addresses allow accesses of 16 bytes.
 constexpr int kF32Waves = 4;
 template <int DQ, bool VEC>
 __global__ void __launch_bounds__(kF32Waves * 64) block_attn_f32_kernel(const BlockArgs a, int q_tiles)
 {
-    __shared__ f32x4 po[kF32Waves][DQ][64];
+    constexpr int E = !VEC ? 1 : DQ % 4 == 0 ? 4 : DQ % 2 == 0 ? 2 : 1;     // columns of V that a lane loads at once: one of each of E tiles
+    typedef float vec __attribute__((ext_vector_type(E)));
+    __shared__ float po[kF32Waves][4][DQ][64];
     __shared__ float pm[kF32Waves][16], pl[kF32Waves][16];
     const int lane = threadIdx.x & 63, l16 = lane & 15, quarter = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -620,14 +630,20 @@ __global__ void __launch_bounds__(kF32Waves * 64) block_attn_f32_kernel(const Bl
 #pragma unroll
             for (int c = 0; c < DQ; ++c) kf[t][c] = load4(K + (int64_t)rc * a.k.token, c * 16 + 4 * quarter);
         }
-        // V^T operand of k-slice (t, r): key 16 t + 4 quarter + r, column 16 c + l16
+        // V^T operand of k-slice (t, r): key 16 t + 4 quarter + r, row l16 of tile c is column E l16 + c % E of those from 16 (c - c % E) on
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 const int row = kv0 + 16 * t + 4 * quarter + r;
 #pragma unroll
-                for (int c = 0; c < DQ; ++c) vf[t][r][c] = row < kv_len && c * 16 + l16 < d ? V[(int64_t)row * a.v.token + c * 16 + l16] : 0.f;
+                for (int c = 0; c < DQ; c += E) {
+                    const int col = 16 * c + E * l16;
+                    vec v = {};
+                    if (row < kv_len && col < d) v = *reinterpret_cast<const vec*>(V + (int64_t)row * a.v.token + col);
+#pragma unroll
+                    for (int j = 0; j < E; ++j) vf[t][r][c + j] = v[j];
+                }
             }
         float mx = -INFINITY;
 #pragma unroll
@@ -664,7 +680,9 @@ __global__ void __launch_bounds__(kF32Waves * 64) block_attn_f32_kernel(const Bl
     l_run += __shfl_xor(l_run, 32, 64);
     if (quarter == 0) { pm[wave][l16] = m_run; pl[wave][l16] = l_run; }
 #pragma unroll
-    for (int c = 0; c < DQ; ++c) po[wave][c][lane] = o[c];
+    for (int c = 0; c < DQ; ++c)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) po[wave][r][c][lane] = o[c][r];
     __syncthreads();
     float m_all = pm[0][l16], l_all = 0.f, f[kF32Waves];
 #pragma unroll
@@ -677,14 +695,18 @@ __global__ void __launch_bounds__(kF32Waves * 64) block_attn_f32_kernel(const Bl
     if (q >= q_len) return;
     const float inv = l_all > 0.f ? 1.f / l_all : l_all != l_all ? l_all : 0.f;
     float* op = (float*)a.out + slot * a.out_slot + (int64_t)q * a.out_token + h * a.out_head;
-    for (int c = wave; c < DQ; c += kF32Waves) {
-        f32x4 v = po[0][c][lane] * f[0];
 #pragma unroll
-        for (int w = 1; w < kF32Waves; ++w) v += po[w][c][lane] * f[w];
-        v *= inv;
+    for (int c = 0; c < DQ; c += E) {                           // wave w joins row 4 quarter + w of every tile
+        const int col = 16 * c + E * (4 * quarter + wave);
+        vec v;
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
-            if (c * 16 + 4 * quarter + r < d) op[c * 16 + 4 * quarter + r] = v[r];
+        for (int j = 0; j < E; ++j) {
+            float x = po[0][wave][c + j][lane] * f[0];
+#pragma unroll
+            for (int w = 1; w < kF32Waves; ++w) x = fmaf(po[w][wave][c + j][lane], f[w], x);
+            v[j] = x * inv;
+        }
+        if (col < d) *reinterpret_cast<vec*>(op + col) = v;
     }
 }
 
@@ -731,7 +753,8 @@ template <int DQ> drf_status launch_f32(const BlockArgs& a, hipStream_t st)
     const long long items = (long long)q_tiles * a.q_heads * a.slots;
     if (items > 0x7fffffLL) DRF_FAIL(DRF_ESHAPE, "too many queries");
     auto aligned = [](const Rows& r) { return (reinterpret_cast<uintptr_t>(r.p) & 15u) == 0 && r.slot % 4 == 0 && r.token % 4 == 0 && r.head % 4 == 0; };
-    if (a.d % 4 == 0 && aligned(a.q) && aligned(a.k)) hipLaunchKernelGGL((block_attn_f32_kernel<DQ, true>), dim3((unsigned)items), dim3(kF32Waves * 64), 0, st, a, q_tiles);
+    const Rows out = { a.out, a.out_slot, a.out_token, a.out_head };
+    if (a.d % 4 == 0 && aligned(a.q) && aligned(a.k) && aligned(a.v) && aligned(out)) hipLaunchKernelGGL((block_attn_f32_kernel<DQ, true>), dim3((unsigned)items), dim3(kF32Waves * 64), 0, st, a, q_tiles);
     else hipLaunchKernelGGL((block_attn_f32_kernel<DQ, false>), dim3((unsigned)items), dim3(kF32Waves * 64), 0, st, a, q_tiles);
     DRF_HIP(hipGetLastError());
     return DRF_OK;
@@ -744,6 +767,7 @@ drf_status launch_block_attn(const BlockArgs& a, drf_dtype dtype, hipStream_t st
         case 1: return launch_f32<1>(a, st);
         case 2: return launch_f32<2>(a, st);
         case 3: case 4: return launch_f32<4>(a, st);
+        case 5: case 6: return launch_f32<6>(a, st);
         default: return launch_f32<8>(a, st);
         }
     }

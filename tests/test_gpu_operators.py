@@ -510,6 +510,13 @@ def test_operators_of_nothing(torch, drf, S, N, M):
     assert not drf.block_attention(q, k, k, words, 32, 32).any()
 
 
+@pytest.mark.parametrize("d", [32, 48, 64, 72, 96, 128])
+@pytest.mark.parametrize("layout", ["odd", "heads"])
+def test_block_attention_fp32_layouts(torch, drf, d, layout):
+    """Rows and heads that are not aligned to 16 bytes, and heads that lie outside of the tokens."""
+    attend(torch, drf, "f32", 2, 70, 200, 4, 2, d, 32, 32, random_mask(np.random.default_rng(d), 2, 4, 70, 200, 32, 32, 0.5), layout=layout)
+
+
 def test_block_attention_ignores_bits_behind_the_last_block(torch, drf):
     rng = np.random.default_rng(8)
     (q, _), (k, _), (v, _) = (tensor(torch, rng, (1, 70, 2, 64), "bf16", "plain") for _ in range(3))
