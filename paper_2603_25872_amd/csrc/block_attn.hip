@@ -101,6 +101,13 @@ template <bool LOW> __device__ inline void copy_pieces(uint32_t dst, uint32_t of
     else asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" :: "s"(dst), "v"(off), "s"(src) : "memory");
 }
 
+// The same for the lanes of two scalar masks.
+__device__ inline void copy_pieces_of(uint32_t low, uint32_t high, uint32_t dst, uint32_t off, const bf16_t* src)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_mov_b32 exec_lo, %3\n\ts_mov_b32 exec_hi, %4\n\tglobal_load_lds_dwordx4 %1, %2\n\ts_mov_b64 exec, -1"
+                 :: "s"(dst), "v"(off), "s"(src), "s"(low), "s"(high) : "memory");
+}
+
 constexpr float kTau = 8.f;                                     // lazy-rescale headroom of the online softmax, in log2 units
 constexpr float kNone = -3.4028235e38f;                         // no reference score yet
 constexpr float kFar = 1.8446744e19f;                           // 2^64: sums up to here (of a reference of weight 1) have lost nothing
@@ -111,19 +118,22 @@ __device__ inline float max3(float a, float b, float c) { return __builtin_eleme
 // the only waits are for the copies of a step that were asked for a whole step before.  Two buffers of 32 keys: while a step is computed the
 // fragments of the next are read out of one and the step after it lands in the other.  With QB = 2 every fragment is used twice and one
 // block's scores are formed beside the other's exponentials.  W waves share a tile of queries where there are few (each takes every W-th
-// step; joined through LDS).  Bound by the matrix instructions and, beside them, the exponentials and the way of K and V into LDS: 4 slots x 16384
-// queries x 12 heads of 128 over 16 of 128 blocks of 128, 825 GFLOP, 0.90 - 0.94 ms, 0.9 PFLOP/s (a large library product reaches 1.23 here, the
-// instruction by itself 1.94; without the copies it would be 0.73, without their waits the same).  6 x 4096 x 16 of 72 over 8 of 64 blocks of 64,
-// 58 GFLOP over 226 MB of q, k, v and result, 82 us, 97 with nothing of them in the caches: half of it is that read.
-template <int P8, int QB, int W>
-__global__ void __launch_bounds__(64 * W, P8 > 11 && QB == 2 ? 1 : 2) block_attn_kernel(const BlockArgs a, int q_tiles, int n_items)
+// step; joined through LDS).  SH = 2 waves, of 64 queries of one block each, share its list and the buffers (one copies K, the other V), with a
+// barrier where a buffer has landed and one where it is free.
+// Bound by the matrix instructions and, beside them, the exponentials and the way of K and V into LDS: 4 slots x 16384 queries x 12 heads of 128
+// over 16 of 128 blocks of 128, 825 GFLOP, 0.89 ms, 0.93 PFLOP/s (a large library product reaches 1.23 here, the instruction by itself 1.94; by
+// waves of their own 0.94 ms, of which the copies were 0.2 and their waits nothing).  6 x 4096 x 16 of 72 over 8 of 64 blocks of 64, 58 GFLOP over
+// 226 MB of q, k, v and result, 82 us, 97 with nothing of them in the caches: half of it is that read.
+template <int P8, int QB, int W, int SH>
+__global__ void __launch_bounds__(64 * W * SH, P8 > 11 && QB == 2 ? 1 : 2) block_attn_kernel(const BlockArgs a, int q_tiles, int n_items)
 {
     using C = Cfg<P8>;
     constexpr int d = C::d, KS = C::KS, DT = C::DT, DT1 = C::DT1, KP = C::KP, VP = C::VP, LDO = C::LDO;
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
     const int lane = threadIdx.x & 63, l32 = lane & 31, half = lane >> 5;
-    const int wave = W > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0;
-    unsigned char* mem = smem + wave * C::WAVE;
+    static_assert(SH == 1 || (W == 1 && QB == 2), "two waves of 64 queries share their keys");
+    const int wave = W * SH > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0;
+    unsigned char* mem = smem + (SH > 1 ? 0 : wave * C::WAVE);
     // consecutive items (query tiles of one head) on one XCD: ids are dealt round-robin over the 8 of them, each with its own L2
     int item = blockIdx.x;
     {
@@ -131,22 +141,42 @@ __global__ void __launch_bounds__(64 * W, P8 > 11 && QB == 2 ? 1 : 2) block_attn
         item = xcd * q8 + (xcd < rem ? xcd : rem) + (item >> 3);
     }
     const int tile = item % q_tiles, sh = item / q_tiles, slot = sh / a.q_heads, h = sh - slot * a.q_heads;
-    const int q0 = tile * 32 * QB, q_len = slot_len(a.q_lens, slot, a.nq), kv_len = slot_len(a.kv_lens, slot, a.nk);
-    if (q0 >= q_len) return;
+    const int tile_q0 = tile * 32 * QB * SH, q_len = slot_len(a.q_lens, slot, a.nq), kv_len = slot_len(a.kv_lens, slot, a.nk);
+    if (tile_q0 >= q_len) return;
+    const int q0 = tile_q0 + (SH > 1 ? wave * 32 * QB : 0);     // (of two waves the second's queries may all lie behind the last: it works for the first)
     const bf16x8 zero8 = { 0, 0, 0, 0, 0, 0, 0, 0 };
     const bf16_t* Q = (const bf16_t*)a.q.p + slot * a.q.slot + h * a.q.head;
     const bf16_t* K = (const bf16_t*)a.k.p + slot * a.k.slot + h / a.group * a.k.head;
     const bf16_t* V = (const bf16_t*)a.v.p + slot * a.v.slot + h / a.group * a.v.head;
     const int ldk = (int)a.k.token, ldv = (int)a.v.token;
 
-    Walk<W> walk(a, slot, h, q0, kv_len, wave);
+    Walk<W> walk(a, slot, h, tile_q0, kv_len, W > 1 ? wave : 0);
     const uint32_t lds = (uint32_t)(uintptr_t)(DRF_LDS_PTR unsigned char*)mem;
-    uint32_t ko[C::KI], vo[C::VI];                              // of a lane's pieces from the step's first row (pieces of row padding take any)
+    // of a lane's pieces from the step's first row (pieces of row padding take any); of two waves the first copies K, the second V
+    constexpr int MOST = C::KI > C::VI ? C::KI : C::VI, COPIES = SH > 1 ? MOST : C::KI + C::VI;
+    uint32_t ko[SH > 1 ? 1 : C::KI], vo[SH > 1 ? MOST : C::VI];
+    const bool copies_k = SH > 1 && wave == 0;
     auto offsets = [&](int left) {
         int l = lane;
         asm volatile("" : "+v"(l));                             // formed anew each time: the lane's parts of it need no registers in between
+        if constexpr (SH > 1) {
+            if (copies_k) {
 #pragma unroll
-        for (int i = 0; i < C::KI; ++i) {
+                for (int i = 0; i < MOST; ++i) {
+                    const int id = i * 64 + l, r = id / KP, c = id % KP;
+                    vo[i] = (uint32_t)((r < left ? r : left - 1) * ldk + (c < P8 ? c : 0) * 8) * 2u;
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < MOST; ++i) {
+                    const int id = i * 64 + l, r = id / VP, c = id % VP;
+                    vo[i] = (uint32_t)((r < left ? r : left - 1) * ldv + (c < P8 ? c : 0) * 8) * 2u;
+                }
+            }
+            return;
+        }
+#pragma unroll
+        for (int i = 0; i < (SH > 1 ? 0 : C::KI); ++i) {
             const int id = i * 64 + l, r = id / KP, c = id % KP;
             ko[i] = (uint32_t)((r < left ? r : left - 1) * ldk + (c < P8 ? c : 0) * 8) * 2u;
         }
@@ -164,10 +194,22 @@ __global__ void __launch_bounds__(64 * W, P8 > 11 && QB == 2 ? 1 : 2) block_attn
         return kv0;
     };
     // copy j of the step at kv0
-    constexpr int COPIES = C::KI + C::VI;
+    const int ldc = copies_k ? ldk : ldv;
+    const bf16_t* const from = copies_k ? K : V;
     auto copy = [&](int kv0, int buf, int j) {
         const uint32_t b = lds + (uint32_t)buf * C::BUF;
-        if (j < C::KI) {
+        if constexpr (SH > 1) {
+            const bf16_t* src = from + (int64_t)kv0 * ldc;
+            const uint32_t dst = b + (copies_k ? 0u : (uint32_t)C::KBYTES) + j * 1024u;
+            // (rows come in 32s: a last copy is of half a wave or a whole one)
+            const int left_k = kStep * KP - 64 * j, left_v = kStep * VP - 64 * j;
+            if (left_k >= 64 && left_v >= 64) {
+                copy_pieces<false>(dst, vo[j], src);
+            } else {
+                const int left = copies_k ? left_k : left_v;
+                copy_pieces_of(__builtin_amdgcn_readfirstlane(left > 0 ? -1 : 0), __builtin_amdgcn_readfirstlane(left >= 64 ? -1 : 0), dst, vo[j], src);
+            }
+        } else if (j < C::KI) {
             const bf16_t* src = K + (int64_t)kv0 * ldk;
             if (j == C::KI - 1 && kStep * KP % 64) copy_pieces<true>(b + j * 1024u, ko[j], src);
             else copy_pieces<false>(b + j * 1024u, ko[j], src);
@@ -183,7 +225,10 @@ __global__ void __launch_bounds__(64 * W, P8 > 11 && QB == 2 ? 1 : 2) block_attn
         for (int j = 0; j < COPIES; ++j) copy(kv0, buf, j);
     };
     // every copy has landed, every LDS read is done
-    auto settle_memory = [&]() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory"); };
+    auto settle_memory = [&]() {
+        if constexpr (SH > 1) asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    };
     // values behind the last key of a landed step that the keys end inside of are zero, not repeated (a weight of zero takes no NaN with it)
     auto tail = [&](int kv0, int buf) {
         const int left = kv_len - kv0;
@@ -385,7 +430,8 @@ __global__ void __launch_bounds__(64 * W, P8 > 11 && QB == 2 ? 1 : 2) block_attn
         auto step = [&](auto issue_c, auto more_c) {
             constexpr bool ISSUE = decltype(issue_c)::value, MORE = decltype(more_c)::value;
             if constexpr (MORE) {
-                asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+                if constexpr (SH > 1) asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
+                else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
                 if (!ISSUE) tail(n1, buf ^ 1);
             }
             // Matrix instruction m of the NM beside which this buffer is refilled, a copy or two behind each: all of them at once would keep the
@@ -393,7 +439,10 @@ __global__ void __launch_bounds__(64 * W, P8 > 11 && QB == 2 ? 1 : 2) block_attn
             constexpr int NM = (QB == 2 ? KS : 0) + 2 * DT, PER = NM > 0 ? NM : 1;
             auto refill = [&](int m) {
                 if constexpr (ISSUE) {
-                    if (m == 0) asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");        // the values' fragments are out
+                    if (m == 0) {                               // the values' fragments are out
+                        if constexpr (SH > 1) asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+                        else asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                    }
 #pragma unroll
                     for (int j = m * COPIES / PER; j < (m + 1) * COPIES / PER; ++j) copy(n2, buf, j);
                     __builtin_amdgcn_sched_barrier(0x406);      // vector and scalar arithmetic may cross
@@ -466,8 +515,15 @@ __global__ void __launch_bounds__(64 * W, P8 > 11 && QB == 2 ? 1 : 2) block_attn
                     for (int r = 0; r < 4; r += 2) top = max3(top, fabsf(ot[b][i][r]), fabsf(ot[b][i][r + 1]));
             }
         }
-        if (__any(!(top < kFar))) {
-            walk = Walk<W>(a, slot, h, q0, kv_len, wave);
+        bool again = __any(!(top < kFar));
+        if constexpr (SH > 1) {                                 // for both if for one
+            uint32_t* flag = reinterpret_cast<uint32_t*>(mem + C::WAVE);
+            if (lane == 0) flag[wave] = again;
+            settle_memory();
+            again = __builtin_amdgcn_readfirstlane(flag[0] | flag[1]) != 0;
+        }
+        if (again) {
+            walk = Walk<W>(a, slot, h, tile_q0, kv_len, 0);
             offsets(kStep);
             settle_memory();
             n0 = next_step();
@@ -499,7 +555,8 @@ __global__ void __launch_bounds__(64 * W, P8 > 11 && QB == 2 ? 1 : 2) block_attn
     if constexpr (W == 1) {
         // a block's 32 x d tile is transposed through LDS, so that rows leave in 16-byte pieces (a wave's LDS operations complete in order)
         settle_memory();
-        bf16_t* so = reinterpret_cast<bf16_t*>(mem);
+        static_assert(SH * 32 * LDO * 2 <= C::WAVE, "LDS layout");
+        bf16_t* so = reinterpret_cast<bf16_t*>(mem) + (SH > 1 ? wave * 32 * LDO : 0);
 #pragma unroll
         for (int b = 0; b < QB; ++b) {
             if (q0 + b * 32 >= q_len) break;
@@ -712,21 +769,21 @@ __global__ void __launch_bounds__(kF32Waves * 64) block_attn_f32_kernel(const Bl
 
 int log2_of(int b) { return b == 32 ? 5 : b == 64 ? 6 : b == 128 ? 7 : 0; }
 
-template <int P8, int QB, int W> drf_status launch_bf16_as(const BlockArgs& a, hipStream_t st)
+template <int P8, int QB, int W, int SH> drf_status launch_bf16_as(const BlockArgs& a, hipStream_t st)
 {
     using C = Cfg<P8>;
-    constexpr int smem = W * (W > 1 && C::JOIN > C::WAVE ? C::JOIN : C::WAVE);
+    constexpr int smem = W * (W > 1 && C::JOIN > C::WAVE ? C::JOIN : C::WAVE) + (SH > 1 ? 16 : 0);
     static_assert(smem <= 160 * 1024, "LDS of a CU");
-    auto kern = block_attn_kernel<P8, QB, W>;
+    auto kern = block_attn_kernel<P8, QB, W, SH>;
     static bool attr_set = false;
     if (!attr_set) {
         DRF_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, smem));
         attr_set = true;
     }
-    const int q_tiles = (a.nq + 32 * QB - 1) / (32 * QB);
+    const int q_tiles = (a.nq + 32 * QB * SH - 1) / (32 * QB * SH);
     const long long items = (long long)q_tiles * a.q_heads * a.slots;
-    if (items > 0x1ffffffLL / W) DRF_FAIL(DRF_ESHAPE, "too many queries");
-    hipLaunchKernelGGL(kern, dim3((unsigned)items), dim3(64 * W), smem, st, a, q_tiles, (int)items);
+    if (items > 0x1ffffffLL / (W * SH)) DRF_FAIL(DRF_ESHAPE, "too many queries");
+    hipLaunchKernelGGL(kern, dim3((unsigned)items), dim3(64 * W * SH), smem, st, a, q_tiles, (int)items);
     DRF_HIP(hipGetLastError());
     return DRF_OK;
 }
@@ -737,14 +794,19 @@ template <int P8, int QB, int W> drf_status launch_bf16_as(const BlockArgs& a, h
 //    waves fill a CU: 512 9.6 : 13.7 : 20.8; 1024 18.4 : 15.4 : 21.6).  Two waves are between, eight lose from 512 tiles on and gain up to 8 % before;
 //  - a wave to 32 queries while that leaves no SIMD with two (2048 queries 13.0 : 17.5; of 128 18.4 : 23.9), and for query blocks of 32;
 //  - a wave to 64 queries otherwise, which reads every fragment of K and V once for two blocks of queries (4096 queries 18.8 : 19.2; of 128 36.1 : 28.2;
-//    6 slots x 4096 107.8 : 84.2).
+//    6 slots x 4096 107.8 : 84.2);
+//  - two such waves on one copy of the keys for query blocks of 128 and widths from 96 on, where a SIMD's registers hold one wave in any case: 4 x 16384
+//    x 12 heads of 128 890 : 941, 1 x 4096 x 16 27.9 : 28.8, 2 x 8192 x 16 of 96 132 : 140.  Narrower heads have several waves to a SIMD that do better
+//    without each other's waits (4 x 2048 x 8 of 64 22.9 : 18.9, of 32 39.3 : 36.6; 6 x 4096 x 16 of 72 95.7 : 99.2 the other way).
 template <int P8> drf_status launch_bf16(const BlockArgs& a, hipStream_t st)
 {
     constexpr int per_cu = 160 * 1024 / Cfg<P8>::WAVE < 8 ? 160 * 1024 / Cfg<P8>::WAVE : 8;
     const long long tiles = (long long)((a.nq + 31) / 32) * a.q_heads * a.slots;
-    if (tiles * 4 <= 256 * per_cu) return launch_bf16_as<P8, 1, 4>(a, st);
-    if (tiles <= 1024 || a.q_shift == 5) return launch_bf16_as<P8, 1, 1>(a, st);
-    return launch_bf16_as<P8, 2, 1>(a, st);
+    if (tiles * 4 <= 256 * per_cu) return launch_bf16_as<P8, 1, 4, 1>(a, st);
+    if (tiles <= 1024 || a.q_shift == 5) return launch_bf16_as<P8, 1, 1, 1>(a, st);
+    if constexpr (P8 > 11)
+        if (a.q_shift == 7) return launch_bf16_as<P8, 2, 1, 2>(a, st);
+    return launch_bf16_as<P8, 2, 1, 1>(a, st);
 }
 
 template <int DQ> drf_status launch_f32(const BlockArgs& a, hipStream_t st)

@@ -454,21 +454,23 @@ def test_block_attention_of_many_tiles(torch, drf, tiles, d, N, M, q_block, kv_b
 @pytest.mark.parametrize("tiles", TILES)
 @pytest.mark.parametrize("d", [24, 64, 72, 128])
 @pytest.mark.parametrize("steepest", [1.0, 4.0, 16.0])
-def test_block_attention_of_many_tiles_scores_that_grow(torch, drf, tiles, d, steepest):
+@pytest.mark.parametrize("qb", [64, 128])
+def test_block_attention_of_many_tiles_scores_that_grow(torch, drf, tiles, d, steepest, qb):
     """The first step's scores are small, later ones larger: by what sums in fp32 hold beside them, and by far more."""
     rng = np.random.default_rng(d)
     N, M = 96, 640
     (q, _), (k, _), (v, vv) = (tensor(torch, rng, (1, n, 2, d), "bf16", "plain") for n in (N, M, M))
     q, k = (q * 2).to(q.dtype), (k * torch.linspace(0.2, steepest, M, device="cuda").view(1, M, 1, 1)).to(k.dtype)
     for turn in (k, k.flip(1)):
-        many(torch, drf, q, turn, v, random_mask(rng, 1, 2, N, M, 64, 32, 0.7), q.double().cpu().numpy(), turn.double().cpu().numpy(), vv, 64, 32, tiles)
+        many(torch, drf, q, turn, v, random_mask(rng, 1, 2, N, M, qb, 32, 0.7), q.double().cpu().numpy(), turn.double().cpu().numpy(), vv, qb, 32, tiles)
 
 
 @pytest.mark.parametrize("tiles", [1] + TILES)
-@pytest.mark.parametrize("d", [40, 64, 72])
-def test_block_attention_of_many_tiles_lengths_and_masked_places(torch, drf, tiles, d):
+@pytest.mark.parametrize("d", [40, 64, 72, 104])
+@pytest.mark.parametrize("qb", [64, 128])
+def test_block_attention_of_many_tiles_lengths_and_masked_places(torch, drf, tiles, d, qb):
     rng = np.random.default_rng(d)
-    S, N, H, qb, kb = 6, 170, 2, 64, 32
+    S, N, H, kb = 6, 170, 2, 32
     q_lens, kv_lens = np.array([0, 1, 65, 170, 500, 128], np.int32), np.array([170, 33, 0, 169, 1, -7], np.int32)
     mask = random_mask(rng, S, H, N, N, qb, kb, 0.5)
     mask[:, 1] = mask[:, 0]
@@ -483,8 +485,9 @@ def test_block_attention_of_many_tiles_lengths_and_masked_places(torch, drf, til
 
 
 @pytest.mark.parametrize("tiles", [1] + TILES)
-@pytest.mark.parametrize("d", [64, 72])
-def test_block_attention_behind_a_step_of_no_weight(torch, drf, tiles, d):
+@pytest.mark.parametrize("d", [64, 72, 128])
+@pytest.mark.parametrize("qb", [64, 128])
+def test_block_attention_behind_a_step_of_no_weight(torch, drf, tiles, d, qb):
     """A list's first keys score -infinity, the others so low that their exponentials alone would vanish."""
     rng = np.random.default_rng(d)
     N, M = 96, 160
@@ -494,9 +497,9 @@ def test_block_attention_behind_a_step_of_no_weight(torch, drf, tiles, d):
     q[..., 1:], qv[..., 1:] = q[..., 1:] / 4, qv[..., 1:] / 4                  # (exact)
     kv[:, :64, :, 0], kv[:, 64:, :, 0] = -np.inf, -8192.0
     k.copy_(torch.from_numpy(kv))
-    mask = np.ones((1, 2, 2, 5), bool)
-    mask[0, 1, 1] = [1, 0, 0, 0, 1]
-    many(torch, drf, q, k, v, mask, qv, kv, vv, 64, 32, tiles)
+    mask = np.ones((1, 2, -(-N // qb), 5), bool)
+    mask[0, 1, -1] = [1, 0, 0, 0, 1]
+    many(torch, drf, q, k, v, mask, qv, kv, vv, qb, 32, tiles)
 
 
 @pytest.mark.parametrize("S,N,M", [(0, 5, 5), (2, 0, 40), (2, 40, 0)])
