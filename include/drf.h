@@ -353,7 +353,7 @@ typedef struct {
  *   positions   DEVICE fp32 or NULL: element (slot s, token n, axis a) at positions[s * positions_slot_stride +
  *               n * n_axes + a] (stride 0: one table for all slots); replaces the grid, origin and step
  *   out         may be x itself (the same address and strides); otherwise the two do not overlap
- * head_dim <= 128.  16-byte aligned tensors whose strides and head_dim are multiples of 16 bytes take 16-byte
+ * head_dim <= 128, tokens <= 2^30.  16-byte aligned tensors whose strides and head_dim are multiples of 16 bytes take 16-byte
  * accesses; all others one element at a time.
  */
 drf_status drf_rope(const drf_rope_config* rope, drf_dtype dtype, int slots, int tokens, int heads, int head_dim,
@@ -402,7 +402,7 @@ drf_status drf_block_select(const drf_attn_shape* shape, int q_block, int kv_blo
  * caller's own choice as well as drf_block_select's; bits of blocks beyond the keys do not count).  A query with no key gives
  * zeros.  Rows of out behind a slot's q length are left as they were; keys and values behind its kv length, and of blocks
  * not chosen, are not looked at.  out overlaps no input.
- * head_dim <= 128; DRF_BF16: head_dim % 8 == 0, 16-byte aligned tensors, strides % 8 == 0.  token strides below 2^24.
+ * head_dim <= 128, tokens <= 2^30; DRF_BF16: head_dim % 8 == 0, 16-byte aligned tensors, strides % 8 == 0.  token strides below 2^24.
  */
 drf_status drf_block_attention(const drf_attn_shape* shape, int q_block, int kv_block, float scale, const uint32_t* blocks,
                                const drf_heads* q, const drf_heads* k, const drf_heads* v, const drf_heads* out, void* hip_stream);

@@ -871,6 +871,7 @@ extern "C" drf_status drf_block_attention(const drf_attn_shape* shape, int q_blo
     if (s.head_dim > kMaxD) DRF_FAIL(DRF_ESHAPE, "head_dim must be <= %d (got %d)", kMaxD, s.head_dim);
     if (!log2_of(q_block) || !log2_of(kv_block)) DRF_FAIL(DRF_EINVAL, "blocks of %d queries and %d keys: each must be 32, 64 or 128", q_block, kv_block);
     if (!(scale > 0.f) || !std::isfinite(scale)) DRF_FAIL(DRF_EINVAL, "scale must be a positive number");
+    if (s.q_tokens > 1 << 30 || s.kv_tokens > 1 << 30) DRF_FAIL(DRF_ESHAPE, "more than 2^30 tokens");
     if (s.slots == 0 || s.q_tokens == 0) return DRF_OK;
     if (!q || !k || !v || !out || !q->data || !out->data || (s.kv_tokens > 0 && (!k->data || !v->data || !blocks))) DRF_FAIL(DRF_EINVAL, "NULL buffer");
     for (const drf_heads* t : { q, k, v, out }) {

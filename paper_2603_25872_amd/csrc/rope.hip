@@ -420,6 +420,7 @@ drf_status check_sizes(drf_dtype dtype, int slots, int tokens, int heads, int he
     if (slots < 0 || tokens < 0 || heads < 1 || head_dim < 1) DRF_FAIL(DRF_EINVAL, "slots and tokens must be >= 0, heads and head_dim >= 1");
     if (head_dim > kMaxD) DRF_FAIL(DRF_ESHAPE, "head_dim must be <= %d (got %d)", kMaxD, head_dim);
     if (heads > 65535) DRF_FAIL(DRF_ESHAPE, "more than 65535 heads");
+    if (tokens > 1 << 30) DRF_FAIL(DRF_ESHAPE, "more than 2^30 tokens");
     return DRF_OK;
 }
 

@@ -122,6 +122,19 @@ def test_bad_attentions_are_refused():
     assert call(shape(slots=0), q=None, k=None, v=None, out=None, blocks=None) == call(shape(q_tokens=0), q=None, out=None) == 0
 
 
+@pytest.mark.parametrize("tokens", [2 ** 30 + 1, 2 ** 31 - 1])
+def test_more_tokens_than_are_counted_are_refused(tokens):
+    """Sizes whose tiles, rounded up, would not fit 32 bits."""
+    L, t = drf.lib(), heads()
+    rc, cfg = drf.rope_config((64,), (1,)), drf.QkConfig(norm=0, q_scale=1.0)
+    assert L.drf_rope(C.byref(rc), 1, 1, tokens, 4, 64, None, None, 0, C.byref(t), C.byref(t), None) == ESHAPE
+    s = shape(q_tokens=tokens, kv_tokens=tokens)
+    assert L.drf_qk_norm_rope(C.byref(cfg), C.byref(rc), C.byref(s), None, 0, *[C.byref(t)] * 4, None) == ESHAPE
+    for over in (dict(q_tokens=tokens), dict(kv_tokens=tokens)):
+        assert L.drf_block_attention(C.byref(shape(**over)), 64, 64, C.c_float(1.0), FAKE, *[C.byref(t)] * 4, None) == ESHAPE
+    assert L.drf_block_select(C.byref(shape(q_tokens=tokens)), 32, 64, 4, C.byref(t), C.byref(t), FAKE, 1 << 62, FAKE, None) == ESHAPE
+
+
 def test_binding_refuses_what_it_cannot_describe():
     import torch
     x = torch.zeros(1, 4, 2, 8)
