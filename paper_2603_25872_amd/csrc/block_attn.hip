@@ -1,8 +1,9 @@
 // Attention over the key blocks that a bit mask gives each block of queries.
 //
-// bf16: flash-style, a wave takes 64 (or 32) queries of one query block and walks its list of key blocks in steps of 32 keys.  Scores are computed
-// transposed (S^T = K Q^T), so that a lane owns one query column: the online softmax needs one exchange between the halves of a wave, and the
-// probabilities are where the second product (O^T = V^T P^T) wants them.  A block that is not chosen is never read.
+// bf16: one pass over the keys, exponentials against a reference score.  A wave takes 64 (or 32) queries of one query block and walks its list of
+// key blocks in steps of 32 keys.  Scores are computed transposed (S^T = K Q^T), so that a lane owns one query column: a reference needs one
+// exchange between the halves of a wave, and the probabilities are where the second product (O^T = V^T P^T) wants them.  A block that is not
+// chosen is never read.
 // fp32: a workgroup takes 16 queries, its four waves the steps in turn, each with a softmax of its own; joined through LDS.
 #include <type_traits>
 #include <utility>
