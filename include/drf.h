@@ -408,6 +408,16 @@ drf_status drf_block_attention(const drf_attn_shape* shape, int q_block, int kv_
                                const drf_heads* q, const drf_heads* k, const drf_heads* v, const drf_heads* out, void* hip_stream);
 
 /*
+ * The same where few queries attend to many keys (one token to a long context): several workgroups share a head's queries, leave their
+ * parts in `scratch` and a second launch joins them.  scratch: DEVICE, 16-byte aligned, drf_block_attention_scratch_bytes() bytes of any
+ * content, for one call at a time; NULL, or 0 of those bytes: exactly drf_block_attention.  Sums are formed in another order then.
+ */
+size_t drf_block_attention_scratch_bytes(const drf_attn_shape* shape);
+drf_status drf_block_attention_split(const drf_attn_shape* shape, int q_block, int kv_block, float scale, const uint32_t* blocks,
+                                     const drf_heads* q, const drf_heads* k, const drf_heads* v, const drf_heads* out, void* scratch,
+                                     size_t scratch_bytes, void* hip_stream);
+
+/*
  * A denoiser whose self-attention has these operators in it.  Per block, in place of softmax(q k^T / sqrt(d)) v:
  *   q, k = rotate(norm(q)), rotate(norm(k))      as drf_qk_norm_rope, token (row, column) of the patch grid at that position
  *   out  = softmax(q k^T / sqrt(d)) v            over all keys (topk 0), or over the blocks that drf_block_select chooses

@@ -175,7 +175,7 @@ PyObject* bind(PyObject*, PyObject* address)
 
 struct Operators {
     decltype(&drf_rope) rope; decltype(&drf_qk_norm_rope) qk; decltype(&drf_block_words) words; decltype(&drf_block_select_scratch_bytes) scratch;
-    decltype(&drf_block_select) select; decltype(&drf_block_attention) attend;
+    decltype(&drf_block_select) select; decltype(&drf_block_attention_scratch_bytes) parts; decltype(&drf_block_attention_split) attend;
 } g_ops = {};
 PyObject *g_f32, *g_bf16, *g_i32, *g_device, *g_stream;     // dtypes; what gives the current device, and the current stream of a device
 
@@ -385,27 +385,29 @@ PyObject* block_select(PyObject*, PyObject* const* a, Py_ssize_t n)
     DRF_RUN(g_ops.select(&s, qb, kb, topk, &q.h, &k.h, scratch, bytes, (uint32_t*)out, stream));
 }
 
-// block_attention(q, k, v, blocks, out, q_block, kv_block, scale, q_lens, kv_lens) -> status
+// block_attention(q, k, v, blocks, out, q_block, kv_block, scale, q_lens, kv_lens, scratch) -> status
 PyObject* block_attention(PyObject*, PyObject* const* a, Py_ssize_t n)
 {
     Tensor q, k, v, out;
     drf_attn_shape s;
     int qb = 0, kb = 0;
-    void *blocks = nullptr, *stream = nullptr;
-    if (!ready(n, 10) || !attn_shape(a[0], a[1], a[8], a[9], &q, &k, &s) || !heads(a[2], &k, true, &v) || !heads(a[4], &q, true, &out)) return nullptr;
+    void *blocks = nullptr, *scratch = nullptr, *stream = nullptr;
+    if (!ready(n, 11) || !attn_shape(a[0], a[1], a[8], a[9], &q, &k, &s) || !heads(a[2], &k, true, &v) || !heads(a[4], &q, true, &out)) return nullptr;
     if (!to_int(a[5], &qb) || !to_int(a[6], &kb)) return nullptr;
     const double scale = PyFloat_AsDouble(a[7]);
     if (scale == -1.0 && PyErr_Occurred()) return nullptr;
-    if (!vector(a[3], g_i32, mask_words(s, qb, kb), q.device, "the blocks' words", &blocks) || !current(q, &stream)) return nullptr;
-    DRF_RUN(g_ops.attend(&s, qb, kb, (float)scale, (const uint32_t*)blocks, &q.h, &k.h, &v.h, &out.h, stream));
+    const size_t bytes = a[10] == Py_None ? 0 : g_ops.parts(&s);
+    if (!vector(a[3], g_i32, mask_words(s, qb, kb), q.device, "the blocks' words", &blocks) || !vector(a[10], g_f32, (long long)(bytes / 4), q.device, "scratch", &scratch) ||
+        !current(q, &stream)) return nullptr;
+    DRF_RUN(g_ops.attend(&s, qb, kb, (float)scale, (const uint32_t*)blocks, &q.h, &k.h, &v.h, &out.h, scratch, bytes, stream));
 }
 
 // bind_operators((addresses), float32, bfloat16, int32, current device, current stream of a device)
 PyObject* bind_operators(PyObject*, PyObject* const* a, Py_ssize_t n)
 {
-    if (n != 6 || !PyTuple_Check(a[0]) || PyTuple_GET_SIZE(a[0]) != 6) { PyErr_SetString(PyExc_TypeError, "bind_operators() takes six addresses and five objects"); return nullptr; }
-    void* p[6];
-    for (int i = 0; i < 6; ++i)
+    if (n != 6 || !PyTuple_Check(a[0]) || PyTuple_GET_SIZE(a[0]) != 7) { PyErr_SetString(PyExc_TypeError, "bind_operators() takes seven addresses and five objects"); return nullptr; }
+    void* p[7];
+    for (int i = 0; i < 7; ++i)
         if (!(p[i] = PyLong_AsVoidPtr(PyTuple_GET_ITEM(a[0], i)))) {
             if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "NULL address");
             return nullptr;
@@ -413,7 +415,7 @@ PyObject* bind_operators(PyObject*, PyObject* const* a, Py_ssize_t n)
     PyObject** keep[5] = { &g_f32, &g_bf16, &g_i32, &g_device, &g_stream };
     for (int i = 0; i < 5; ++i) { Py_INCREF(a[1 + i]); Py_XSETREF(*keep[i], a[1 + i]); }
     g_ops = { (decltype(g_ops.rope))p[0], (decltype(g_ops.qk))p[1], (decltype(g_ops.words))p[2], (decltype(g_ops.scratch))p[3], (decltype(g_ops.select))p[4],
-              (decltype(g_ops.attend))p[5] };
+              (decltype(g_ops.parts))p[5], (decltype(g_ops.attend))p[6] };
     Py_RETURN_NONE;
 }
 

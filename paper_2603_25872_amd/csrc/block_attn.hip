@@ -34,6 +34,8 @@ struct BlockArgs {
     int slots, nq, nk, q_heads, group, d;       // group: query heads a kv head
     int q_shift, kv_shift, q_blocks, words;     // log2 of the block sizes
     float scale_log2;                           // log2(e) * scale
+    int split;                                  // workgroups to a tile, where four waves share it; more than one: they leave their part in `parts`
+    float* parts;                               // [tile][split][32][d + 4]: O, and m and l behind it
 };
 
 __device__ inline int slot_len(const int32_t* lens, int slot, int tokens)
@@ -73,6 +75,39 @@ template <int W> struct Walk {
             if (kv0 >= len) { sub = 1 << (shift - 5); continue; }           // the last block ends before its last step
             ++sub;
             if (W == 1 || skip-- == 0) { skip = W - 1; return kv0; }
+        }
+    }
+};
+
+// The same of one in `every`, past whole words and blocks of them at once.  (Apart, since its few instructions more cost the other 5 to 10 %.)
+struct WalkOfParts {
+    Walk<1>::scalar_ptr row; uint32_t last_mask; int words, len, shift, w = -1, base = 0, sub, skip, every; uint32_t bits = 0;
+    __device__ WalkOfParts(const BlockArgs& a, int slot, int h, int q0, int len_, int first, int every_) : skip(first), every(every_)
+    {
+        const Walk<1> all(a, slot, h, q0, len_, 0);
+        row = all.row; last_mask = all.last_mask; words = all.words; len = all.len; shift = all.shift; sub = all.sub;
+    }
+    __device__ int next()
+    {
+        const int n = 1 << (shift - 5);                         // steps of a block; those that the last block has not count too (none follows)
+        for (;;) {
+            if (sub == n) {
+                while (bits == 0) {
+                    if (w + 1 >= words) return -1;
+                    ++w;
+                    bits = row[w] & (w + 1 == words ? last_mask : ~0u);
+                }
+                const int all = __builtin_popcount(bits) * n;
+                if (skip >= all) { skip -= all; bits = 0; continue; }
+                for (; skip >= n; skip -= n) bits &= bits - 1;
+                base = (32 * w + __builtin_ctz(bits)) << shift;
+                bits &= bits - 1;
+                sub = 0;
+            }
+            const int kv0 = base + kStep * sub;
+            if (kv0 >= len) { sub = n; continue; }
+            ++sub;
+            if (skip-- == 0) { skip = every - 1; return kv0; }
         }
     }
 };
@@ -125,7 +160,7 @@ __device__ inline float max3(float a, float b, float c) { return __builtin_eleme
 // over 16 of 128 blocks of 128, 825 GFLOP, 0.89 ms, 0.93 PFLOP/s (a large library product reaches 1.23 here, the instruction by itself 1.94; by
 // waves of their own 0.94 ms, of which the copies were 0.2 and their waits nothing).  6 x 4096 x 16 of 72 over 8 of 64 blocks of 64, 58 GFLOP over
 // 226 MB of q, k, v and result, 82 us, 97 with nothing of them in the caches: half of it is that read.
-template <int P8, int QB, int W, int SH>
+template <int P8, int QB, int W, int SH, bool SPLIT>
 __global__ void __launch_bounds__(64 * W * SH, P8 > 11 && QB == 2 ? 1 : 2) block_attn_kernel(const BlockArgs a, int q_tiles, int n_items)
 {
     using C = Cfg<P8>;
@@ -141,6 +176,8 @@ __global__ void __launch_bounds__(64 * W * SH, P8 > 11 && QB == 2 ? 1 : 2) block
         const int q8 = n_items >> 3, rem = n_items & 7, xcd = item & 7;
         item = xcd * q8 + (xcd < rem ? xcd : rem) + (item >> 3);
     }
+    const int part = SPLIT ? item % a.split : 0;
+    if (SPLIT) item /= a.split;
     const int tile = item % q_tiles, sh = item / q_tiles, slot = sh / a.q_heads, h = sh - slot * a.q_heads;
     const int tile_q0 = tile * 32 * QB * SH, q_len = slot_len(a.q_lens, slot, a.nq), kv_len = slot_len(a.kv_lens, slot, a.nk);
     if (tile_q0 >= q_len) return;
@@ -151,7 +188,10 @@ __global__ void __launch_bounds__(64 * W * SH, P8 > 11 && QB == 2 ? 1 : 2) block
     const bf16_t* V = (const bf16_t*)a.v.p + slot * a.v.slot + h / a.group * a.v.head;
     const int ldk = (int)a.k.token, ldv = (int)a.v.token;
 
-    Walk<W> walk(a, slot, h, tile_q0, kv_len, W > 1 ? wave : 0);
+    auto walk = [&] {
+        if constexpr (SPLIT) return WalkOfParts(a, slot, h, tile_q0, kv_len, part * W + wave, a.split * W);
+        else return Walk<W>(a, slot, h, tile_q0, kv_len, W > 1 ? wave : 0);
+    }();
     const uint32_t lds = (uint32_t)(uintptr_t)(DRF_LDS_PTR unsigned char*)mem;
     // of a lane's pieces from the step's first row (pieces of row padding take any); of two waves the first copies K, the second V
     constexpr int MOST = C::KI > C::VI ? C::KI : C::VI, COPIES = SH > 1 ? MOST : C::KI + C::VI;
@@ -620,7 +660,6 @@ __global__ void __launch_bounds__(64 * W * SH, P8 > 11 && QB == 2 ? 1 : 2) block
                 f[w] = mw == kNone ? 0.f : __builtin_amdgcn_exp2f((mw - m) * sl2);
                 lt = fmaf(all[w * (C::JOIN / 4) + r * LDJ + d + 1], f[w], lt);
             }
-            const float inv = inverse(lt);
             float v[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[e] = 0.f;
@@ -628,11 +667,47 @@ __global__ void __launch_bounds__(64 * W * SH, P8 > 11 && QB == 2 ? 1 : 2) block
             for (int w = 0; w < W; ++w)
 #pragma unroll
                 for (int e = 0; e < 8; ++e) v[e] = fmaf(all[w * (C::JOIN / 4) + r * LDJ + c * 8 + e], f[w], v[e]);
-            bf16x8 y;
+            if constexpr (SPLIT) {
+                float* mine = a.parts + (((size_t)item * a.split + part) * 32 + r) * LDJ;
+                *reinterpret_cast<f32x4*>(mine + c * 8) = (f32x4){ v[0], v[1], v[2], v[3] };
+                *reinterpret_cast<f32x4*>(mine + c * 8 + 4) = (f32x4){ v[4], v[5], v[6], v[7] };
+                if (c == 0) { mine[d] = m; mine[d + 1] = lt; }
+            } else {
+                const float inv = inverse(lt);
+                bf16x8 y;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) y[e] = (bf16_t)(v[e] * inv);
-            *reinterpret_cast<bf16x8*>(out + (int64_t)(q0 + r) * a.out_token + c * 8) = y;
+                for (int e = 0; e < 8; ++e) y[e] = (bf16_t)(v[e] * inv);
+                *reinterpret_cast<bf16x8*>(out + (int64_t)(q0 + r) * a.out_token + c * 8) = y;
+            }
         }
+    }
+}
+
+// The parts of a tile's workgroups to its result: a thread 8 columns of a row.
+__global__ void __launch_bounds__(256) join_parts_kernel(const BlockArgs a, int q_tiles)
+{
+    const int tile = blockIdx.x % q_tiles, sh = blockIdx.x / q_tiles, slot = sh / a.q_heads, h = sh - slot * a.q_heads;
+    const int d = a.d, ld = d + 4, pieces = d / 8, q0 = tile * 32, q_len = slot_len(a.q_lens, slot, a.nq);
+    const float* parts = a.parts + (size_t)blockIdx.x * a.split * 32 * ld;
+    bf16_t* out = (bf16_t*)a.out + slot * a.out_slot + h * a.out_head;
+    for (int id = threadIdx.x; id < 32 * pieces; id += 256) {
+        const int r = id / pieces, c = id % pieces;
+        if (q0 + r >= q_len) break;
+        float m = kNone, l = 0.f, v[8] = {};
+        for (int p = 0; p < a.split; ++p) m = __builtin_elementwise_maximum(m, parts[(p * 32 + r) * ld + d]);
+        for (int p = 0; p < a.split; ++p) {
+            const float* from = parts + (p * 32 + r) * ld;
+            const float f = from[d] == kNone ? 0.f : __builtin_amdgcn_exp2f((from[d] - m) * a.scale_log2);
+            const f32x4 lo = *reinterpret_cast<const f32x4*>(from + c * 8), hi = *reinterpret_cast<const f32x4*>(from + c * 8 + 4);
+            l = fmaf(from[d + 1], f, l);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) { v[e] = fmaf(lo[e], f, v[e]); v[4 + e] = fmaf(hi[e], f, v[4 + e]); }
+        }
+        const float inv = l > 0.f ? 1.f / l : l != l ? l : 0.f;
+        bf16x8 y;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) y[e] = (bf16_t)(v[e] * inv);
+        *reinterpret_cast<bf16x8*>(out + (int64_t)(q0 + r) * a.out_token + c * 8) = y;
     }
 }
 
@@ -770,23 +845,45 @@ __global__ void __launch_bounds__(kF32Waves * 64) block_attn_f32_kernel(const Bl
 
 int log2_of(int b) { return b == 32 ? 5 : b == 64 ? 6 : b == 128 ? 7 : 0; }
 
-template <int P8, int QB, int W, int SH> drf_status launch_bf16_as(const BlockArgs& a, hipStream_t st)
+template <int P8, int QB, int W, int SH, bool SPLIT = false> drf_status launch_bf16_as(const BlockArgs& a, hipStream_t st)
 {
     using C = Cfg<P8>;
     constexpr int smem = W * (W > 1 && C::JOIN > C::WAVE ? C::JOIN : C::WAVE) + (SH > 1 ? 16 : 0);
     static_assert(smem <= 160 * 1024, "LDS of a CU");
-    auto kern = block_attn_kernel<P8, QB, W, SH>;
+    auto kern = block_attn_kernel<P8, QB, W, SH, SPLIT>;
     static bool attr_set = false;
     if (!attr_set) {
         DRF_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, smem));
         attr_set = true;
     }
     const int q_tiles = (a.nq + 32 * QB * SH - 1) / (32 * QB * SH);
-    const long long items = (long long)q_tiles * a.q_heads * a.slots;
+    const long long items = (long long)q_tiles * a.q_heads * a.slots * (SPLIT ? a.split : 1);
     if (items > 0x1ffffffLL / (W * SH)) DRF_FAIL(DRF_ESHAPE, "too many queries");
     hipLaunchKernelGGL(kern, dim3((unsigned)items), dim3(64 * W * SH), smem, st, a, q_tiles, (int)items);
+    if constexpr (SPLIT) {
+        DRF_HIP(hipGetLastError());
+        hipLaunchKernelGGL(join_parts_kernel, dim3((unsigned)(items / a.split)), dim3(256), 0, st, a, q_tiles);
+    }
     DRF_HIP(hipGetLastError());
     return DRF_OK;
+}
+
+// Workgroups to a tile of 32 queries: where the tiles leave most CUs idle and the keys are many, since one CU's way to memory (some 43 bytes a ns) then
+// bounds the call.  1 query x 16 heads of 72 over 128 blocks of 64 of 16384 keys 22 us, 55 with a workgroup to a head.  The second launch and
+// the parts cost what they save from 2048 chosen keys a head down, so shorter contexts are left whole.
+int split_of(const drf_attn_shape& s)
+{
+    if (s.dtype != DRF_BF16) return 1;
+    const long long tiles = (long long)((s.q_tokens + 31LL) / 32) * s.q_heads * s.slots;
+    if (tiles == 0 || tiles > 64 || s.kv_tokens < 8192) return 1;
+    const long long idle = 256 / tiles, keys = s.kv_tokens / 1024;
+    return (int)(idle < keys ? idle : keys);
+}
+
+size_t parts_bytes(const drf_attn_shape& s, int split)
+{
+    if (split < 2) return 0;
+    return (size_t)((s.q_tokens + 31LL) / 32) * s.q_heads * s.slots * split * 32 * (s.head_dim + 4) * sizeof(float);
 }
 
 // How many queries a wave takes, and whether four waves share them, by what the chip then holds at once (1024 SIMDs, 256 CUs):
@@ -803,6 +900,7 @@ template <int P8> drf_status launch_bf16(const BlockArgs& a, hipStream_t st)
 {
     constexpr int per_cu = 160 * 1024 / Cfg<P8>::WAVE < 8 ? 160 * 1024 / Cfg<P8>::WAVE : 8;
     const long long tiles = (long long)((a.nq + 31) / 32) * a.q_heads * a.slots;
+    if (a.split > 1) return launch_bf16_as<P8, 1, 4, 1, true>(a, st);
     if (tiles * 4 <= 256 * per_cu) return launch_bf16_as<P8, 1, 4, 1>(a, st);
     if (tiles <= 1024 || a.q_shift == 5) return launch_bf16_as<P8, 1, 1, 1>(a, st);
     if constexpr (P8 > 11)
@@ -860,8 +958,21 @@ drf_status launch_block_attn(const BlockArgs& a, drf_dtype dtype, hipStream_t st
 
 using namespace drf;
 
+extern "C" size_t drf_block_attention_scratch_bytes(const drf_attn_shape* shape)
+{
+    if (!shape || shape->slots < 0 || shape->q_tokens < 0 || shape->kv_tokens < 0 || shape->q_heads < 1 || shape->head_dim < 1 || shape->head_dim > kMaxD) return 0;
+    return parts_bytes(*shape, split_of(*shape));
+}
+
 extern "C" drf_status drf_block_attention(const drf_attn_shape* shape, int q_block, int kv_block, float scale, const uint32_t* blocks,
                                           const drf_heads* q, const drf_heads* k, const drf_heads* v, const drf_heads* out, void* hip_stream)
+{
+    return drf_block_attention_split(shape, q_block, kv_block, scale, blocks, q, k, v, out, nullptr, 0, hip_stream);
+}
+
+extern "C" drf_status drf_block_attention_split(const drf_attn_shape* shape, int q_block, int kv_block, float scale, const uint32_t* blocks,
+                                                const drf_heads* q, const drf_heads* k, const drf_heads* v, const drf_heads* out, void* scratch,
+                                                size_t scratch_bytes, void* hip_stream)
 {
     if (!shape) DRF_FAIL(DRF_EINVAL, "shape is NULL");
     const drf_attn_shape& s = *shape;
@@ -892,5 +1003,13 @@ extern "C" drf_status drf_block_attention(const drf_attn_shape* shape, int q_blo
     a.q_blocks = (int)(((long long)s.q_tokens + q_block - 1) / q_block);
     a.words = (int)drf_block_words(s.kv_tokens, kv_block);
     a.scale_log2 = 1.4426950408889634f * scale;
+    a.split = 1;
+    if (scratch) {
+        const int split = split_of(s);
+        if (reinterpret_cast<uintptr_t>(scratch) & 15u) DRF_FAIL(DRF_EINVAL, "scratch must be 16-byte aligned");
+        if (scratch_bytes < parts_bytes(s, split)) DRF_FAIL(DRF_EINVAL, "scratch of %zu bytes, %zu are needed", scratch_bytes, parts_bytes(s, split));
+        a.split = split;
+        a.parts = (float*)scratch;
+    }
     return launch_block_attn(a, s.dtype, (hipStream_t)hip_stream);
 }

@@ -29,7 +29,7 @@ SYMBOLS = ["drf_denoiser_weight_count", "drf_denoiser_create", "drf_denoiser_des
            "drf_eps_batched", "drf_eps_batched_static", "drf_skip_transition", "drf_refine_step", "drf_sample",
            "drf_skip_transition_noise", "drf_normal_fill", "drf_sample_noise", "drf_noise_count",
            "drf_plan_build", "drf_last_error",
-           "drf_rope", "drf_qk_norm_rope", "drf_block_words", "drf_block_select_scratch_bytes", "drf_block_select", "drf_block_attention",
+           "drf_rope", "drf_qk_norm_rope", "drf_block_words", "drf_block_select_scratch_bytes", "drf_block_select", "drf_block_attention", "drf_block_attention_scratch_bytes", "drf_block_attention_split",
            "drf_denoiser_weight_count_attn", "drf_denoiser_create_attn"]
 # include/drf_measure.h: test and measurement hooks
 MEASURE_SYMBOLS = ["drf_eps_trace", "drf_profile_enable", "drf_profile_read", "drf_probe_gemm_bf16",
@@ -140,6 +140,9 @@ def lib():
         L.drf_block_select_scratch_bytes.argtypes = [C.c_void_p, C.c_int, C.c_int]
         L.drf_block_select.argtypes = [C.c_void_p] + [C.c_int] * 3 + [C.c_void_p] * 3 + [C.c_size_t, C.c_void_p, C.c_void_p]
         L.drf_block_attention.argtypes = [C.c_void_p, C.c_int, C.c_int, C.c_float] + [C.c_void_p] * 6
+        L.drf_block_attention_scratch_bytes.argtypes = [C.c_void_p]
+        L.drf_block_attention_scratch_bytes.restype = C.c_size_t
+        L.drf_block_attention_split.argtypes = [C.c_void_p, C.c_int, C.c_int, C.c_float] + [C.c_void_p] * 6 + [C.c_size_t, C.c_void_p]
         try:
             from . import _native               # built beside the library
             _native.bind(C.cast(L.drf_skip_transition_noise, C.c_void_p).value)
@@ -381,12 +384,14 @@ class _OperatorsCtypes:
         return _lib.drf_block_select(C.byref(shape), q_block, kv_block, topk, C.byref(hq), C.byref(hk), sc, n, o, _current(q))
 
     @classmethod
-    def block_attention(cls, q, k, v, blocks, out, q_block, kv_block, scale, q_lens, kv_lens):
+    def block_attention(cls, q, k, v, blocks, out, q_block, kv_block, scale, q_lens, kv_lens, scratch):
         import torch
         hq, hk, shape = cls._shape(q, k, q_lens, kv_lens)
         hv, ho = _heads(v, k, True), _heads(out, q, True)
         w = _vector(blocks, torch.int32, cls._words(shape, q_block, kv_block), q, "the blocks' words")
-        return _lib.drf_block_attention(C.byref(shape), q_block, kv_block, scale, w, C.byref(hq), C.byref(hk), C.byref(hv), C.byref(ho), _current(q))
+        n = 0 if scratch is None else _lib.drf_block_attention_scratch_bytes(C.byref(shape))
+        return _lib.drf_block_attention_split(C.byref(shape), q_block, kv_block, scale, w, C.byref(hq), C.byref(hk), C.byref(hv), C.byref(ho),
+                                              _vector(scratch, torch.float32, n // 4, q, "scratch"), n, _current(q))
 
 
 _ops = None             # _native or _OperatorsCtypes, at the first operator
@@ -399,7 +404,7 @@ def _operators():
     try:
         from . import _native
         _native.bind_operators(tuple(C.cast(f, C.c_void_p).value for f in (L.drf_rope, L.drf_qk_norm_rope, L.drf_block_words, L.drf_block_select_scratch_bytes,
-                                                                           L.drf_block_select, L.drf_block_attention)),
+                                                                           L.drf_block_select, L.drf_block_attention_scratch_bytes, L.drf_block_attention_split)),
                                torch.float32, torch.bfloat16, torch.int32, torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream)
         _ops = _native
     except ImportError:
@@ -463,7 +468,12 @@ def block_attention(q, k, v, blocks, q_block, kv_block, scale=None, q_lens=None,
     import torch
     if out is None:
         out = (torch.empty if q_lens is None else torch.zeros)(q.shape, dtype=q.dtype, device=q.device)
-    _check((_ops or _operators()).block_attention(q, k, v, blocks, out, q_block, kv_block, q.shape[3] ** -0.5 if scale is None else scale, q_lens, kv_lens))
+    ops, scratch = _ops or _operators(), None
+    if k.shape[1] >= 8192:                                                      # (shorter contexts are never split)
+        shape = AttnShape(BF16 if q.dtype == torch.bfloat16 else F32, q.shape[0], q.shape[1], k.shape[1], q.shape[2], k.shape[2], q.shape[3], None, None)
+        n = _lib.drf_block_attention_scratch_bytes(C.byref(shape))
+        scratch = torch.empty(n // 4, dtype=torch.float32, device=q.device) if n else None
+    _check(ops.block_attention(q, k, v, blocks, out, q_block, kv_block, q.shape[3] ** -0.5 if scale is None else scale, q_lens, kv_lens, scratch))
     return out
 
 

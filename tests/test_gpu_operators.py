@@ -520,6 +520,50 @@ def test_block_attention_fp32_layouts(torch, drf, d, layout):
     attend(torch, drf, "f32", 2, 70, 200, 4, 2, d, 32, 32, random_mask(np.random.default_rng(d), 2, 4, 70, 200, 32, 32, 0.5), layout=layout)
 
 
+@pytest.mark.parametrize("d", [8, 40, 64, 72, 96, 128])
+@pytest.mark.parametrize("N,M,H,kv_block,share", [(1, 8192, 2, 64, 0.5), (33, 8200, 3, 32, 0.02), (1, 9000, 16, 128, 1.0), (5, 20000, 1, 32, 0.7), (64, 8255, 2, 128, 0.3), (1, 8192, 64, 64, 0.1)])
+def test_block_attention_of_few_queries_over_many_keys(torch, drf, d, N, M, H, kv_block, share):
+    """Several workgroups to a head: lists of every length, parts with no step, lengths that leave most of the keys or all of them out."""
+    rng = np.random.default_rng(N + d)
+    kv_heads = 1 if H % 2 else H // 2
+    mask = random_mask(rng, 1, H, N, M, 32, kv_block, share)
+    mask[:, 0, 0] = 0
+    attend(torch, drf, "bf16", 1, N, M, H, kv_heads, d, 32, kv_block, mask, layout="rows")
+    mask[:, 0, 0, -1] = 1                                                       # one block, which the keys end inside of
+    for length in (M - 1, 700, 1, 0):
+        attend(torch, drf, "bf16", 1, N, M, H, kv_heads, d, 32, kv_block, mask, layout="heads", kv_lens=np.array([length], np.int32))
+
+
+def test_block_attention_parts_in_a_replayed_graph_and_beside_the_unsplit_call(torch, drf):
+    rng = np.random.default_rng(4)
+    (q, qv), (k, kv), (v, vv) = (tensor(torch, rng, (2, n, 2, 64), "bf16", "plain") for n in (3, 8192, 8192))
+    mask = random_mask(rng, 2, 2, 3, 8192, 32, 64, 0.4)
+    words, lens, out = pack(torch, mask), torch.tensor([2, 3], dtype=torch.int32, device="cuda"), torch.full((2, 3, 2, 64), 7.0, dtype=q.dtype, device="cuda")
+    run = lambda: drf.block_attention(q, k, v, words, 32, 64, None, lens, out=out)  # noqa: E731
+    want, mag, size = attended(qv, kv, vv, mask, 32, 64, 0.125, np.array([2, 3]))
+    want[0, 2] = 7.0
+    for t in (torch.cuda.current_stream(), torch.cuda.Stream()):
+        t.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(t):
+            run()
+        torch.cuda.current_stream().wait_stream(t)
+        check(out, want, "bf16", slack_of("bf16", 64, mag, size))
+    eager, g = out.clone(), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        run()
+    for _ in range(3):
+        out[0, :2] = out[1] = 0.0
+        g.replay()
+        assert torch.equal(out, eager)
+        run()
+        assert torch.equal(out, eager)
+    whole = torch.full_like(out, 7.0)
+    hs = [drf._heads(t) for t in (q, k, v, whole)]
+    shape = drf.AttnShape(drf.BF16, 2, 3, 8192, 2, 2, 64, lens.data_ptr(), None)
+    assert drf.lib().drf_block_attention(drf.C.byref(shape), 32, 64, 0.125, words.data_ptr(), *[drf.C.byref(h) for h in hs], drf._current(q)) == 0
+    check(whole, want, "bf16", slack_of("bf16", 64, mag, size))
+
+
 def test_block_attention_ignores_bits_behind_the_last_block(torch, drf):
     rng = np.random.default_rng(8)
     (q, _), (k, _), (v, _) = (tensor(torch, rng, (1, 70, 2, 64), "bf16", "plain") for _ in range(3))
@@ -633,13 +677,15 @@ def test_both_marshallings_give_the_same(torch, drf, monkeypatch):
     q, k, v = x.unbind(2)
     f = q.float()
     words = drf.block_select(q, k, 32, 32, 2)
+    far, some = torch.randn(2, 8192, 4, 64, device="cuda").bfloat16(), torch.full((2, 4, 1, 8), 0x1234567, dtype=torch.int32, device="cuda")
     forms = (drf._operators(), drf._OperatorsCtypes)
     assert forms[0] is not forms[1]                                             # built beside the library here
     got = []
     for form in forms:
         monkeypatch.setattr(drf, "_ops", form)
         out = [drf.rope(q, cfg), drf.rope(f, cfg, positions=table, lens=lens), *chain(drf, x.clone(), cfg, gains, 32, 64, 1, lens),
-               *drf.qk_norm_rope(q, k[:, :, :2], "layer", None, gains, gains, gains, gains, q_scale=2.0), drf.block_attention(q, k, v, words, 32, 32, scale=0.5)]
+               *drf.qk_norm_rope(q, k[:, :, :2], "layer", None, gains, gains, gains, gains, q_scale=2.0), drf.block_attention(q, k, v, words, 32, 32, scale=0.5),
+               drf.block_attention(q[:, :2], far, far, some, 32, 32)]
         bad = []
         for call in (lambda: drf.rope(q, cfg, out=f), lambda: drf.rope(q, cfg, out=k[:, :69]), lambda: drf.rope(q[0], cfg), lambda: drf.rope(q.half(), cfg),
                      lambda: drf.rope(q.transpose(2, 3), cfg), lambda: drf.rope(q.cpu(), cfg), lambda: drf.rope(q, cfg, lens=lens.long()), lambda: drf.rope(q, cfg, lens=lens[:1]),

@@ -122,6 +122,18 @@ def test_bad_attentions_are_refused():
     assert call(shape(slots=0), q=None, k=None, v=None, out=None, blocks=None) == call(shape(q_tokens=0), q=None, out=None) == 0
 
 
+def test_scratch_of_split_attentions():
+    L, t = drf.lib(), heads()
+    need = lambda s: L.drf_block_attention_scratch_bytes(None if s is None else C.byref(s))  # noqa: E731
+    long = dict(slots=1, q_tokens=1, kv_tokens=8192)
+    assert need(shape(**long)) == 4 * 8 * 32 * 68 * 4                              # a tile a head, eight workgroups each
+    assert need(shape(**dict(long, kv_tokens=1 << 20))) == 4 * 64 * 32 * 68 * 4    # a workgroup a CU
+    assert need(shape(**dict(long, kv_tokens=8191))) == need(shape(**dict(long, q_tokens=513))) == need(shape(**dict(long, dtype=0))) == 0
+    assert need(None) == need(shape(**dict(long, slots=0))) == need(shape(**dict(long, q_tokens=0))) == need(shape(**dict(long, head_dim=136))) == 0
+    call = lambda scratch, n: L.drf_block_attention_split(C.byref(shape(**long)), 64, 64, C.c_float(1.0), FAKE, *[C.byref(t)] * 4, scratch, n, None)  # noqa: E731
+    assert call(FAKE + 4, 1 << 30) == call(FAKE, 4 * 8 * 32 * 68 * 4 - 1) == call(FAKE, 0) == EINVAL
+
+
 @pytest.mark.parametrize("tokens", [2 ** 30 + 1, 2 ** 31 - 1])
 def test_more_tokens_than_are_counted_are_refused(tokens):
     """Sizes whose tiles, rounded up, would not fit 32 bits."""
