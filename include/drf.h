@@ -409,7 +409,7 @@ drf_status drf_block_attention(const drf_attn_shape* shape, int q_block, int kv_
 
 /*
  * The same where few queries attend to many keys (one token to a long context): several workgroups share a head's queries, leave their
- * parts in `scratch` and a second launch joins them.  scratch: DEVICE, 16-byte aligned, drf_block_attention_scratch_bytes() bytes of any
+ * parts in `scratch` and a second launch joins them.  Pays from about 1500 chosen keys a query block on.  scratch: DEVICE, 16-byte aligned, drf_block_attention_scratch_bytes() bytes of any
  * content, for one call at a time; NULL, or 0 of those bytes: exactly drf_block_attention.  Sums are formed in another order then.
  */
 size_t drf_block_attention_scratch_bytes(const drf_attn_shape* shape);

@@ -869,8 +869,8 @@ template <int P8, int QB, int W, int SH, bool SPLIT = false> drf_status launch_b
 }
 
 // Workgroups to a tile of 32 queries: where the tiles leave most CUs idle and the keys are many, since one CU's way to memory (some 43 bytes a ns) then
-// bounds the call.  1 query x 16 heads of 72 over 128 blocks of 64 of 16384 keys 22 us, 55 with a workgroup to a head.  The second launch and
-// the parts cost what they save from 2048 chosen keys a head down, so shorter contexts are left whole.
+// bounds the call.  1 query x 16 heads of 72, 8192 keys in blocks of 64, against a workgroup to a head, us: 128 blocks chosen 20.7 : 55.0, 64 15.9 : 29.8,
+// 32 12.7 : 16.7, 16 11.5 : 10.3, 4 11.3 : 5.6 (the second launch and the parts).  How many are chosen only the caller knows: who gives scratch wants it.
 int split_of(const drf_attn_shape& s)
 {
     if (s.dtype != DRF_BF16) return 1;

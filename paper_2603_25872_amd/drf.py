@@ -462,14 +462,15 @@ def block_select(q, k, q_block, kv_block, topk, q_lens=None, kv_lens=None, out=N
     return out
 
 
-def block_attention(q, k, v, blocks, q_block, kv_block, scale=None, q_lens=None, kv_lens=None, out=None):
+def block_attention(q, k, v, blocks, q_block, kv_block, scale=None, q_lens=None, kv_lens=None, out=None, split=False):
     """softmax(scale q k^T) v over the key blocks that the words `blocks` (as block_select gives them) name for each query block; scale
-    1 / sqrt(head_dim) by default.  Rows behind a slot's q length are left as they were: zeros in an output made here."""
+    1 / sqrt(head_dim) by default.  Rows behind a slot's q length are left as they were: zeros in an output made here.  split: several workgroups
+    share a head where its queries are few and its keys many (for lists from about 1500 keys on; see include/drf.h)."""
     import torch
     if out is None:
         out = (torch.empty if q_lens is None else torch.zeros)(q.shape, dtype=q.dtype, device=q.device)
     ops, scratch = _ops or _operators(), None
-    if k.shape[1] >= 8192:                                                      # (shorter contexts are never split)
+    if split:
         shape = AttnShape(BF16 if q.dtype == torch.bfloat16 else F32, q.shape[0], q.shape[1], k.shape[1], q.shape[2], k.shape[2], q.shape[3], None, None)
         n = _lib.drf_block_attention_scratch_bytes(C.byref(shape))
         scratch = torch.empty(n // 4, dtype=torch.float32, device=q.device) if n else None

@@ -315,11 +315,11 @@ def slack_of(dtype, d, mag, size):
     return mag * ((2.0 ** -8 if dtype == "bf16" else 0) + 2 * (d + 8) * 2.0 ** -24 * size + 2.0 ** -18)
 
 
-def attend(torch, drf, dtype, S, N, M, H, Hk, d, q_block, kv_block, mask, layout="rows", scale=None, scales=(1, 1, 1), q_lens=None, kv_lens=None, seed=0):
+def attend(torch, drf, dtype, S, N, M, H, Hk, d, q_block, kv_block, mask, layout="rows", scale=None, scales=(1, 1, 1), q_lens=None, kv_lens=None, seed=0, split=False):
     rng = np.random.default_rng(seed + N + M + d)
     (q, qv), (k, kv), (v, vv) = (tensor(torch, rng, (S, n, h, d), dtype, layout, f) for n, h, f in zip((N, M, M), (H, Hk, Hk), scales))
     dev = lambda a: None if a is None else torch.from_numpy(a).cuda()  # noqa: E731
-    got = drf.block_attention(q, k, v, pack(torch, mask), q_block, kv_block, scale, dev(q_lens), dev(kv_lens))
+    got = drf.block_attention(q, k, v, pack(torch, mask), q_block, kv_block, scale, dev(q_lens), dev(kv_lens), split=split)
     want, mag, size = attended(qv, kv, vv, mask, q_block, kv_block, d ** -0.5 if scale is None else scale, q_lens, kv_lens)
     check(got, want, dtype, slack_of(dtype, d, mag, size))
 
@@ -528,10 +528,10 @@ def test_block_attention_of_few_queries_over_many_keys(torch, drf, d, N, M, H, k
     kv_heads = 1 if H % 2 else H // 2
     mask = random_mask(rng, 1, H, N, M, 32, kv_block, share)
     mask[:, 0, 0] = 0
-    attend(torch, drf, "bf16", 1, N, M, H, kv_heads, d, 32, kv_block, mask, layout="rows")
+    attend(torch, drf, "bf16", 1, N, M, H, kv_heads, d, 32, kv_block, mask, layout="rows", split=True)
     mask[:, 0, 0, -1] = 1                                                       # one block, which the keys end inside of
     for length in (M - 1, 700, 1, 0):
-        attend(torch, drf, "bf16", 1, N, M, H, kv_heads, d, 32, kv_block, mask, layout="heads", kv_lens=np.array([length], np.int32))
+        attend(torch, drf, "bf16", 1, N, M, H, kv_heads, d, 32, kv_block, mask, layout="heads", kv_lens=np.array([length], np.int32), split=True)
 
 
 def test_block_attention_parts_in_a_replayed_graph_and_beside_the_unsplit_call(torch, drf):
@@ -539,7 +539,7 @@ def test_block_attention_parts_in_a_replayed_graph_and_beside_the_unsplit_call(t
     (q, qv), (k, kv), (v, vv) = (tensor(torch, rng, (2, n, 2, 64), "bf16", "plain") for n in (3, 8192, 8192))
     mask = random_mask(rng, 2, 2, 3, 8192, 32, 64, 0.4)
     words, lens, out = pack(torch, mask), torch.tensor([2, 3], dtype=torch.int32, device="cuda"), torch.full((2, 3, 2, 64), 7.0, dtype=q.dtype, device="cuda")
-    run = lambda: drf.block_attention(q, k, v, words, 32, 64, None, lens, out=out)  # noqa: E731
+    run = lambda: drf.block_attention(q, k, v, words, 32, 64, None, lens, out=out, split=True)  # noqa: E731
     want, mag, size = attended(qv, kv, vv, mask, 32, 64, 0.125, np.array([2, 3]))
     want[0, 2] = 7.0
     for t in (torch.cuda.current_stream(), torch.cuda.Stream()):
@@ -685,7 +685,7 @@ def test_both_marshallings_give_the_same(torch, drf, monkeypatch):
         monkeypatch.setattr(drf, "_ops", form)
         out = [drf.rope(q, cfg), drf.rope(f, cfg, positions=table, lens=lens), *chain(drf, x.clone(), cfg, gains, 32, 64, 1, lens),
                *drf.qk_norm_rope(q, k[:, :, :2], "layer", None, gains, gains, gains, gains, q_scale=2.0), drf.block_attention(q, k, v, words, 32, 32, scale=0.5),
-               drf.block_attention(q[:, :2], far, far, some, 32, 32)]
+               drf.block_attention(q[:, :2], far, far, some, 32, 32, split=True), drf.block_attention(q, k, v, words, 32, 32, split=True)]
         bad = []
         for call in (lambda: drf.rope(q, cfg, out=f), lambda: drf.rope(q, cfg, out=k[:, :69]), lambda: drf.rope(q[0], cfg), lambda: drf.rope(q.half(), cfg),
                      lambda: drf.rope(q.transpose(2, 3), cfg), lambda: drf.rope(q.cpu(), cfg), lambda: drf.rope(q, cfg, lens=lens.long()), lambda: drf.rope(q, cfg, lens=lens[:1]),
