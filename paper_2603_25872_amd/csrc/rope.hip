@@ -4,7 +4,8 @@
 // cosine and signed sine,
 //   y_c = (n_c g_c + b_c) C_c + (n_p g_p + b_p) S_c = n_c A_c + n_p B_c + D_c,    A_c = g_c C_c, B_c = g_p S_c, D_c = b_c C_c + b_p S_c,
 // so gains, biases, the scale of the queries and the angles come together in two or three numbers a column, which a lane forms once for its
-// token and its columns and holds in registers over the token's heads.  The angles of a workgroup's tokens are formed once, by all its threads
+// token and its columns and holds in registers over the token's heads.  A column that does not turn is n_c A_c + D_c alone: nothing times
+// zero, so that an infinity in it, or in a column beside it, stays where it is.  The angles of a workgroup's tokens are formed once, by all its threads
 // (in double precision: a position far from zero keeps its fraction of a turn), while the first heads are on their way.  What is left is a copy
 // with a sum over a head's columns and two multiply-adds a column: bound by memory.
 #include <type_traits>
@@ -184,6 +185,7 @@ __global__ void __launch_bounds__(kThreads) heads_kernel(const HeadsArgs a)
         for (int u = 0; u < U; ++u) t[u] = __shfl(t[u], lr * P, 64);
     };
     const float inv_d = 1.f / (float)d;
+    const int turning = a.r.columns - col;                          // of this lane's columns: the first so many turn
     float ka[E], kb[E], kd[E];
     int have = -1;                                                  // the side that they are for
     for (; ch < c1; ++ch) {
@@ -195,13 +197,13 @@ __global__ void __launch_bounds__(kThreads) heads_kernel(const HeadsArgs a)
 #pragma unroll
             for (int j = 0; j < E; ++j) {
                 float c = 1.f, s = 0.f;
-                if (ROPE != ROPE_NO && col + j < a.r.columns) {
+                if (ROPE != ROPE_NO && j < turning) {
                     c = tab[2 * (at * a.r.pairs + pc[j])];
                     s = tab[2 * (at * a.r.pairs + pc[j]) + 1];
                     if (ROPE == ROPE_IN_LANE ? j % 2 == 0 : oc[j] > col + j) s = -s;    // (the first of a pair is the lower)
                 }
                 ka[j] = g[j] * e.scale * c; kb[j] = go[j] * e.scale * s;
-                if constexpr (NORM == DRF_QK_LAYER) kd[j] = (b[j] * c + bo[j] * s) * e.scale;
+                if constexpr (NORM == DRF_QK_LAYER) kd[j] = (ROPE != ROPE_NO && j < turning ? b[j] * c + bo[j] * s : b[j]) * e.scale;
             }
         }
         const int h0 = (is_k ? ch - q_chunks : ch) * U;
@@ -237,7 +239,10 @@ __global__ void __launch_bounds__(kThreads) heads_kernel(const HeadsArgs a)
 #pragma unroll
                 for (int j = 0; j < E; ++j) {
                     float r = (to_f32(v[u][j]) - mean[u]) * ka[j];
-                    if constexpr (ROPE != ROPE_NO) r = fmaf(to_f32(ROPE == ROPE_IN_LANE ? v[u][j ^ 1] : w[u][j]) - mean[u], kb[j], r);
+                    if constexpr (ROPE != ROPE_NO) {
+                        const float turned = fmaf(to_f32(ROPE == ROPE_IN_LANE ? v[u][j ^ 1] : w[u][j]) - mean[u], kb[j], r);
+                        r = j < turning ? turned : r;
+                    }
                     if constexpr (NORM == DRF_QK_LAYER) r = fmaf(r, inv[u], kd[j]);
                     else if constexpr (NORM == DRF_QK_RMS) r *= inv[u];
                     out[j] = (T)r;

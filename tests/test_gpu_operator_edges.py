@@ -1,0 +1,80 @@
+"""The attention operators at the edges of what their calls allow, against their definitions in float64.
+
+Tolerances beyond those of test_gpu_operators.py stand at their tests; a rounding is off by at most half a step, 2^-8 of the value in bf16 and 2^-24 in
+fp32."""
+import numpy as np
+import pytest
+
+import test_gpu_operators as ops
+from paper_2603_25872_amd import drf as D_
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def torch():
+    import torch as t
+    assert t.cuda.is_available()
+    return t
+
+
+@pytest.fixture(scope="module")
+def drf():
+    D_.lib()
+    return D_
+
+
+# ---- rotations ------------------------------------------------------------------------------------------
+
+
+def same_bits(torch, a, b):
+    """Equal bit for bit, one NaN as good as another."""
+    as_int = torch.int16 if a.dtype == torch.bfloat16 else torch.int32
+    nan = torch.isnan(b)
+    return torch.equal(torch.isnan(a), nan) and torch.equal(a.contiguous().view(as_int)[~nan], b.contiguous().view(as_int)[~nan])
+
+
+UNTURNED = [((24,), "halves"), ((32, 8), "halves"), ((36,), "halves"), ((6, 10), "halves"), ((24,), "pairs"), ((36, 4), "pairs"), ((0, 0), "pairs")]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("dims,kind", UNTURNED)
+@pytest.mark.parametrize("layout", ["plain", "heads", "odd"])
+def test_columns_that_do_not_turn_are_left_as_they_are(torch, drf, dtype, dims, kind, layout):
+    """Infinities, NaN, zeros of both signs and the largest numbers among the columns behind the sections, on 16-byte and element accesses: bit for bit the
+    input's (a power of two times it for the queries with a scale), and nothing of them in the columns that turn."""
+    S, N, H, d, at = 2, 13, 5, 72, sum(dims)
+    rng = np.random.default_rng(at)
+    x, v = ops.tensor(torch, rng, (S, N, H, d), dtype, layout)
+    special = torch.tensor([float("inf"), float("-inf"), float("nan"), -0.0, 0.0, 1e38, -1e38, 1.5], device="cuda").to(x.dtype)
+    x[..., at:] = special[torch.from_numpy(rng.integers(0, 8, (S, N, H, d - at))).cuda()]
+    cfg = drf.rope_config(dims, (1, 4)[2 - len(dims):], layout=kind, origin=(5,) * len(dims))
+    want = ops.rotated(v, cfg)
+    lens = torch.tensor([N, 4], dtype=torch.int32, device="cuda")
+    for got, length in ((drf.rope(x, cfg), N), (drf.rope(x, cfg, lens=lens), 4), (drf.qk_norm_rope(x, x, "none", cfg, q_scale=0.5)[1], N)):
+        assert same_bits(torch, got[..., at:], x[..., at:])
+        ops.check(got[1, :length, :, :at], want[1, :length, :, :at], dtype, 2.0 ** -19 * np.abs(v).max())
+    assert same_bits(torch, drf.qk_norm_rope(x, x, "none", cfg, q_scale=0.5)[0][..., at:], (x * 0.5)[..., at:])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("dims,kind", UNTURNED)
+@pytest.mark.parametrize("layout", ["plain", "odd"])
+def test_infinite_parameters_of_columns_that_do_not_turn(torch, drf, dtype, dims, kind, layout):
+    """A gain and a bias that are infinite reach their own columns alone."""
+    S, N, H, d, at = 1, 9, 3, 72, sum(dims)
+    rng = np.random.default_rng(at + 1)
+    x, v = ops.tensor(torch, rng, (S, N, H, d), dtype, layout)
+    gain, bias = rng.uniform(0.5, 2, d).astype(np.float32), rng.uniform(-1, 1, d).astype(np.float32)
+    gain[at + 1], bias[at + 4] = np.inf, -np.inf
+    cfg = drf.rope_config(dims, (1, 4)[2 - len(dims):], layout=kind)
+    dev = lambda a: torch.from_numpy(a).cuda()  # noqa: E731
+    for norm, b in (("rms", None), ("layer", bias)):
+        y = ops.normed(v, norm, gain, b, 1e-6)
+        got = drf.qk_norm_rope(x, x, norm, cfg, dev(gain), dev(gain), None if b is None else dev(b), None if b is None else dev(b))
+        fine = np.isfinite(y)
+        for g in got:
+            g = g.double().cpu().numpy()
+            assert np.array_equal(g[~fine], y[~fine])
+            want = ops.rotated(np.where(fine, y, 0.0), cfg)
+            ops.check(torch.from_numpy(np.where(fine, g, 0.0)), want, dtype, 2.0 ** -19 * np.abs(want).max())
