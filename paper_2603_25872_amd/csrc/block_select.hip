@@ -1,9 +1,10 @@
-// The key blocks that each block of queries attends to: sums of the rows of every block in double precision, their products, and the topk
+// The key blocks that each block of queries attends to: means of the rows of every block in double precision, their products, and the topk
 // largest of each row of products.
 //
 // Which blocks are chosen must not depend on the order of a sum, so nothing before the comparison is narrower than 64 bits (a sum of
-// bf16 rows is then exact unless their exponents lie 37 apart), and equal scores go to the lower block.
-// The first launch reads q and k once and is bound by that; the sums, 1 / block of it, stay in the L2s for the second.
+// bf16 rows is then exact unless their exponents lie 37 apart), and equal scores go to the lower block.  Sums are divided by their rows before the
+// product, not after it: blocks of equal rows then have equal means and equal scores, however many rows the last of them holds.
+// The first launch reads q and k once and is bound by that; the means, 1 / block of it, stay in the L2s for the second.
 #include <type_traits>
 
 #include "common.h"
@@ -23,7 +24,7 @@ struct PoolSide {
     int64_t xs, xt, xh;
     int tokens, heads, block, blocks;
     const int32_t* lens;
-    double* out;        // [slot][head][blocks up to a multiple of 16][columns up to a multiple of 8]
+    double* out;        // means [slot][head][blocks up to a multiple of 16][columns up to a multiple of 8]
 };
 
 __device__ inline int slot_len(const int32_t* lens, int slot, int tokens)
@@ -35,7 +36,7 @@ __device__ inline int slot_len(const int32_t* lens, int slot, int tokens)
 
 // A wave takes a head of a block: 64 / P rows at a time in pieces of 16 bytes (VEC), or a row at a time, a column or two a lane.  Bound by the read
 // of q and k: 64 slots x 1024 tokens x 32 heads of 72 in bf16, 302 MB, 63 us (4.8 TB/s); 2 x 19344 x 16 heads of 64 in fp32, 158 MB, 39 us
-// (4.0) from memory and 16 out of the Infinity Cache.  Six rows in flight a lane, and a block's sums stored as one row: by columns, where 8 bytes of a line leave at a time, the first took 87 us.
+// (4.0) from memory and 16 out of the Infinity Cache.  Six rows in flight a lane, and a block's means stored as one row: by columns, where 8 bytes of a line leave at a time, the first took 87 us.
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(kThreads) pool_kernel(const PoolSide q, const PoolSide k, int d, int q_groups, int parts)
 {
@@ -51,6 +52,7 @@ __global__ void __launch_bounds__(kThreads) pool_kernel(const PoolSide q, const 
     const int slot = id / s.blocks, block = id - slot * s.blocks, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int len = slot_len(s.lens, slot, s.tokens), n0 = block * s.block, end = n0 + s.block < len ? n0 + s.block : len;
     const int width = (d + 7) / 8 * 8, padded = (s.blocks + 15) / 16 * 16;
+    const double rows = end > n0 ? end - n0 : 1;                // (of a block behind the length the mean is zero, and not compared)
     for (int h = part * kWaves + wave; h < s.heads; h += parts * kWaves) {
         const T* x = (const T*)s.x + slot * s.xs + h * s.xh;
         double* out = s.out + (((size_t)slot * s.heads + h) * padded + block) * width;
@@ -79,7 +81,7 @@ __global__ void __launch_bounds__(kThreads) pool_kernel(const PoolSide q, const 
                 double t = 0.0;
                 if (c < d)
                     for (int r = 0; r < rpw; ++r) t += mine[r * d + c];
-                out[c] = t;
+                out[c] = t / rows;
             }
             __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
         } else {
@@ -89,7 +91,7 @@ __global__ void __launch_bounds__(kThreads) pool_kernel(const PoolSide q, const 
                     if (lane + 64 * j < d) sum[j] += (double)(float)x[(int64_t)n * s.xt + lane + 64 * j];
 #pragma unroll
             for (int j = 0; j < 2; ++j)
-                if (lane + 64 * j < width) out[lane + 64 * j] = sum[j];
+                if (lane + 64 * j < width) out[lane + 64 * j] = sum[j] / rows;
         }
     }
 }
@@ -125,7 +127,7 @@ __global__ void __launch_bounds__(NW * 64) select_kernel(const SelectArgs a)
     extern __shared__ __attribute__((aligned(16))) double score[];          // [16][nk padded]
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int qtiles = (a.nq + 15) / 16, ktiles = (a.nk + 15) / 16, ld = ktiles * 16 + 2;
-    // the rows of one head on one XCD (ids are dealt round-robin over the 8 of them, each with its own L2): they read the same sums of keys
+    // the rows of one head on one XCD (ids are dealt round-robin over the 8 of them, each with its own L2): they read the same means of keys
     int id = blockIdx.x;
     {
         const int q8 = gridDim.x >> 3, rem = gridDim.x & 7, xcd = id & 7;
@@ -158,9 +160,8 @@ __global__ void __launch_bounds__(NW * 64) select_kernel(const SelectArgs a)
                 }
         }
         // lane l holds column l % 16 of rows l / 16 + 4 r
-        const int j = t * 16 + (lane & 15), left = kv_len - j * a.kv_block, count = left < a.kv_block ? left : a.kv_block;
 #pragma unroll
-        for (int r = 0; r < 4; ++r) score[((lane >> 4) + 4 * r) * ld + j] = count > 0 ? (acc[0][r] + acc[1][r]) / (double)count : 0.0;
+        for (int r = 0; r < 4; ++r) score[((lane >> 4) + 4 * r) * ld + t * 16 + (lane & 15)] = acc[0][r] + acc[1][r];
     }
     __syncthreads();
     for (int r = 0; r < R; ++r) {
@@ -310,9 +311,9 @@ extern "C" drf_status drf_block_select(const drf_attn_shape* shape, int q_block,
         vec = vec && (reinterpret_cast<uintptr_t>(t->data) & 15u) == 0 && t->slot_stride % unit == 0 && t->token_stride % unit == 0 && t->head_stride % unit == 0;
         return PoolSide{ t->data, t->slot_stride, t->token_stride, t->head_stride, tokens, heads, block, n, lens, out };
     };
-    double* q_sums = (double*)scratch;
-    double* k_sums = (double*)((char*)scratch + q_bytes);
-    const PoolSide qs = side(q, s.q_tokens, s.q_heads, q_block, nq, s.q_lens, q_sums), ks = side(k, s.kv_tokens, s.kv_heads, kv_block, nk, s.kv_lens, k_sums);
+    double* q_means = (double*)scratch;
+    double* k_means = (double*)((char*)scratch + q_bytes);
+    const PoolSide qs = side(q, s.q_tokens, s.q_heads, q_block, nq, s.q_lens, q_means), ks = side(k, s.kv_tokens, s.kv_heads, kv_block, nk, s.kv_lens, k_means);
     int parts = 1;                                                          // workgroups over the heads of a block
     while (parts * kWaves < s.q_heads && (long long)s.slots * (nq + nk) * parts < 2048) parts *= 2;
     const long long q_groups = (long long)s.slots * nq * parts, groups = q_groups + (long long)s.slots * nk * parts;
@@ -324,7 +325,7 @@ extern "C" drf_status drf_block_select(const drf_attn_shape* shape, int q_block,
     DRF_HIP(hipGetLastError());
 
     SelectArgs a{};
-    a.q = q_sums; a.k = k_sums; a.q_tokens = s.q_tokens; a.kv_tokens = s.kv_tokens; a.q_heads = s.q_heads; a.group = s.q_heads / s.kv_heads;
+    a.q = q_means; a.k = k_means; a.q_tokens = s.q_tokens; a.kv_tokens = s.kv_tokens; a.q_heads = s.q_heads; a.group = s.q_heads / s.kv_heads;
     a.q_block = q_block; a.kv_block = kv_block; a.nq = nq; a.nk = nk; a.pairs = (s.head_dim + 7) / 8; a.topk = topk;
     a.words = (int)drf_block_words(s.kv_tokens, kv_block); a.q_lens = s.q_lens; a.kv_lens = s.kv_lens; a.blocks = blocks;
     const size_t lds = (size_t)kRows * ((nk + 15) / 16 * 16 + 2) * sizeof(double);

@@ -35,7 +35,7 @@ struct Workspace {
     float *resid = nullptr, *mod = nullptr, *cact32 = nullptr, *cscratch = nullptr;
     void *hbuf = nullptr, *qkv = nullptr, *mid = nullptr, *ybuf = nullptr, *ybuf2 = nullptr, *cact = nullptr;
     void *xkv = nullptr, *ctx_act = nullptr;    // cross-attention K/V cache [L][rows][ctx_len][2D] and its staging
-    void* sel = nullptr;                        // sums that the choice of key blocks compares, then the chosen blocks' words
+    void* sel = nullptr;                        // means that the choice of key blocks compares, then the chosen blocks' words
     float* skpart = nullptr;                    // partial tiles of the split-K GEMM (bf16 path), or NULL: no split
 };
 
@@ -236,7 +236,7 @@ struct ProfScope {
 
 // Sizes (bytes) of the Workspace members for a pass of `slots` slots, `cond_rows` conditioning rows and
 // `ctx_rows` distinct text contexts: one table both the owned and the static workspace are built from.
-struct WorkspaceBytes { size_t resid, hbuf, qkv, mid, ybuf, ybuf2, mod, cact32, cscratch, cact, xkv, ctx_act, sel, sel_sums; };
+struct WorkspaceBytes { size_t resid, hbuf, qkv, mid, ybuf, ybuf2, mod, cact32, cscratch, cact, xkv, ctx_act, sel, sel_means; };
 WorkspaceBytes workspace_bytes(const drf_denoiser* d, size_t slots, size_t cond_rows, size_t ctx_rows)
 {
     const size_t M = slots * d->dm.T, D = (size_t)d->dm.D, act = d->bf16 ? 2 : 4;
@@ -251,8 +251,8 @@ WorkspaceBytes workspace_bytes(const drf_denoiser* d, size_t slots, size_t cond_
     }
     if (d->attn.topk > 0 && slots > 0) {
         const drf_attn_shape s = shape_of(&d->cfg, (int)slots);
-        b.sel_sums = drf_block_select_scratch_bytes(&s, d->attn.q_block, d->attn.kv_block);
-        b.sel = b.sel_sums + slots * d->dm.heads * ((d->dm.T + d->attn.q_block - 1) / d->attn.q_block) * drf_block_words(d->dm.T, d->attn.kv_block) * 4;
+        b.sel_means = drf_block_select_scratch_bytes(&s, d->attn.q_block, d->attn.kv_block);
+        b.sel = b.sel_means + slots * d->dm.heads * ((d->dm.T + d->attn.q_block - 1) / d->attn.q_block) * drf_block_words(d->dm.T, d->attn.kv_block) * 4;
     }
     return b;
 }
@@ -496,11 +496,11 @@ drf_status forward(drf_denoiser* d, const Workspace& ws, const float* x, const S
     };
     auto block_attention = [&]() -> drf_status {
         const drf_heads q = part_of_qkv(0), k = part_of_qkv(1), v = part_of_qkv(2), out = { ws.hbuf, (int64_t)dm.T * D, D, dm.d };
-        const size_t sums = drf_block_select_scratch_bytes(&shape, d->attn.q_block, d->attn.kv_block);
-        uint32_t* words = (uint32_t*)((char*)ws.sel + sums);
+        const size_t means = drf_block_select_scratch_bytes(&shape, d->attn.q_block, d->attn.kv_block);
+        uint32_t* words = (uint32_t*)((char*)ws.sel + means);
         {
             ProfScope ps(d, st, DRF_PROF_ELEMWISE, 2.0 * M * D * (double)act);
-            const drf_status r = drf_block_select(&shape, d->attn.q_block, d->attn.kv_block, d->attn.topk, &q, &k, ws.sel, sums, words, st);
+            const drf_status r = drf_block_select(&shape, d->attn.q_block, d->attn.kv_block, d->attn.topk, &q, &k, ws.sel, means, words, st);
             if (r != DRF_OK) return r;
         }
         ProfScope ps(d, st, DRF_PROF_ATTN, 4.0 * slots * dm.heads * (double)dm.T * std::min((double)d->attn.topk * d->attn.kv_block, (double)dm.T) * dm.d);

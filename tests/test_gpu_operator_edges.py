@@ -78,3 +78,22 @@ def test_infinite_parameters_of_columns_that_do_not_turn(torch, drf, dtype, dims
             assert np.array_equal(g[~fine], y[~fine])
             want = ops.rotated(np.where(fine, y, 0.0), cfg)
             ops.check(torch.from_numpy(np.where(fine, g, 0.0)), want, dtype, 2.0 ** -19 * np.abs(want).max())
+
+
+# ---- which blocks ---------------------------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [8, 64, 100, 128])
+@pytest.mark.parametrize("M,kv_block", [(3 * 64 + 37, 64), (70 * 32 + 31, 32), (2 * 128 + 1, 128)])
+def test_equal_keys_tie_in_a_block_that_is_not_full(torch, drf, dtype, d, M, kv_block):
+    """Every key row the same, of any values: every block has the same mean and score, the last one too that holds fewer rows (its sum of up to 128
+    equal fp32 rows is exact in 64 bits, and so is the mean), so the lowest blocks are chosen."""
+    rng = np.random.default_rng(d + M)
+    H, nk = 4, -(-M // kv_block)
+    for _ in range(12):
+        q, _ = ops.tensor(torch, rng, (1, 150, H, d), dtype, "plain")
+        k, _ = ops.tensor(torch, rng, (1, 1, H, d), dtype, "plain")
+        for topk in (1, 2, nk - 1):
+            got = ops.bits(torch, drf.block_select(q, k.expand(1, M, H, d), 32, kv_block, topk), nk)
+            assert np.array_equal(got, np.broadcast_to(np.arange(nk) < topk, got.shape)), topk
