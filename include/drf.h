@@ -402,7 +402,7 @@ drf_status drf_block_select(const drf_attn_shape* shape, int q_block, int kv_blo
  * caller's own choice as well as drf_block_select's; bits of blocks beyond the keys do not count).  A query with no key gives
  * zeros.  Rows of out behind a slot's q length are left as they were; keys and values behind its kv length, and of blocks
  * not chosen, are not looked at.  out overlaps no input.
- * head_dim <= 128, tokens <= 2^30; DRF_BF16: head_dim % 8 == 0, 16-byte aligned tensors, strides % 8 == 0.  token strides below 2^24.
+ * scale > 0, finite also times log2(e).  head_dim <= 128, tokens <= 2^30; DRF_BF16: head_dim % 8 == 0, 16-byte aligned tensors, strides % 8 == 0.  token strides below 2^24.
  */
 drf_status drf_block_attention(const drf_attn_shape* shape, int q_block, int kv_block, float scale, const uint32_t* blocks,
                                const drf_heads* q, const drf_heads* k, const drf_heads* v, const drf_heads* out, void* hip_stream);

@@ -147,6 +147,7 @@ __device__ inline void copy_pieces_of(uint32_t low, uint32_t high, uint32_t dst,
 constexpr float kTau = 8.f;                                     // lazy-rescale headroom of the online softmax, in log2 units
 constexpr float kNone = -3.4028235e38f;                         // no reference score yet
 constexpr float kFar = 1.8446744e19f;                           // 2^64: sums up to here (of a reference of weight 1) have lost nothing
+constexpr float kLargeReference = 1048576.f;                    // 2^20: a reference below is an exponent of two within 2^-4
 
 __device__ inline float max3(float a, float b, float c) { return __builtin_elementwise_maximum(__builtin_elementwise_maximum(a, b), c); }
 
@@ -305,7 +306,8 @@ __global__ void __launch_bounds__(64 * W * SH, P8 > 11 && QB == 2 ? 1 : 2) block
 
     f32x16 o[QB][DT1];
     f32x4 ot[QB][2];                                            // TAIL: rows 32 DT .. 32 DT + 15, queries 0-15 and 16-31 of block b
-    // Exponents are taken against a reference score m_run; ms: it in exponents of two (0 while there is none: then every score so far is -infinity).
+    // Exponents are taken against a reference score m_run; ms: it, in exponents of two where it stays (0 while there is none: then every score so far is
+    // -infinity).
     const float sl2 = a.scale_log2, tau = kTau / sl2;
     float m_run[QB], ms[QB], l_run[QB];
 
@@ -371,17 +373,18 @@ __global__ void __launch_bounds__(64 * W * SH, P8 > 11 && QB == 2 ? 1 : 2) block
         for (int r = 3; r < 15; r += 2) mx = max3(mx, s[b][r], s[b][r + 1]);
         return __builtin_elementwise_maximum(mx, s[b][15]);
     };
-    auto refer = [&](int b, float mx) {                         // to the largest of both halves' scores if that is more
+    auto refer = [&](auto lazy_c, int b, float mx) {            // to the largest of both halves' scores if that is more
         const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
         m_run[b] = max3(__uint_as_float(sw[0]), __uint_as_float(sw[1]), m_run[b]);
-        ms[b] = m_run[b] == kNone ? 0.f : m_run[b] * sl2;
+        ms[b] = m_run[b] == kNone ? 0.f : decltype(lazy_c)::value ? m_run[b] : m_run[b] * sl2;
     };
-    // The reference moves only when some query of the block would otherwise exceed 2^kTau.
+    // The reference moves only when some query of the block would otherwise exceed 2^kTau, or has none yet and a score to refer to (which may be the
+    // lowest number, and tau as large as the largest).
     auto settle = [&](int b) {
         const float mx = largest(b);
-        if (__any(mx - m_run[b] >= tau)) {
+        if (__any(mx - m_run[b] >= tau || (m_run[b] == kNone && mx > kNone))) {
             const float old = m_run[b];
-            refer(b, mx);
+            refer(std::true_type{}, b, mx);
             const float alpha = __builtin_amdgcn_exp2f((old - m_run[b]) * sl2);
             l_run[b] *= alpha;
 #pragma unroll
@@ -395,11 +398,17 @@ __global__ void __launch_bounds__(64 * W * SH, P8 > 11 && QB == 2 ? 1 : 2) block
             }
         }
     };
-    auto soft = [&](int b) {                                    // P of block b
+    // P of block b.  LAZY takes the difference first, which is exact where it matters, whatever the scores' size (0.2 us of a query's 10.3 over 1024 keys; by a
+    // branch for large references alone 0.3); otherwise one instruction does, and what the reference's rounding to an exponent of two leaves (2^-24 of it) is
+    // common to a query's weights.
+    auto soft = [&](auto lazy_c, int b) {
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) s[b][8 * c + e] = __builtin_amdgcn_exp2f(fmaf(s[b][8 * c + e], sl2, -ms[b]));
+            for (int e = 0; e < 8; ++e) {
+                const float x = s[b][8 * c + e];
+                s[b][8 * c + e] = __builtin_amdgcn_exp2f(decltype(lazy_c)::value ? (x - ms[b]) * sl2 : fmaf(x, sl2, -ms[b]));
+            }
             if constexpr (!C::ONES) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) l_run[b] += s[b][8 * c + e];
@@ -450,12 +459,12 @@ __global__ void __launch_bounds__(64 * W * SH, P8 > 11 && QB == 2 ? 1 : 2) block
         if constexpr (!LAZY && QB == 2) {
             qk(1, nothing);
             mask(1, n0);
-            refer(1, largest(1));
+            refer(lazy_c, 1, largest(1));
         }
         qk(0, nothing);
         mask(0, n0);
         if constexpr (LAZY) settle(0);
-        else refer(0, largest(0));
+        else refer(lazy_c, 0, largest(0));
         if constexpr (QB == 2) {                                // the first step finds nothing pending
             pf[1][0] = pf[1][1] = zero8;
 #pragma unroll
@@ -494,14 +503,14 @@ __global__ void __launch_bounds__(64 * W * SH, P8 > 11 && QB == 2 ? 1 : 2) block
                 qk(1, nothing);
                 if constexpr (MORE) load_k(buf ^ 1);
                 pin();
-                soft(0);
+                soft(lazy_c, 0);
                 pv(1, nothing);
                 load_v(buf);
                 pin();
                 if constexpr (!ISSUE) mask(1, n0);
                 if constexpr (LAZY) settle(1);
                 if constexpr (MORE) qk(0, refill);
-                soft(1);
+                soft(lazy_c, 1);
                 pv(0, [&](int m) { refill(KS + m); });
                 if constexpr (ISSUE) n3 = next_step();
                 if constexpr (MORE) {
@@ -512,7 +521,7 @@ __global__ void __launch_bounds__(64 * W * SH, P8 > 11 && QB == 2 ? 1 : 2) block
                 load_v(buf);
                 if constexpr (MORE) load_k(buf ^ 1);
                 pin();
-                soft(0);
+                soft(lazy_c, 0);
                 if constexpr (NM == 0) {
                     if constexpr (ISSUE) {
                         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
@@ -538,12 +547,13 @@ __global__ void __launch_bounds__(64 * W * SH, P8 > 11 && QB == 2 ? 1 : 2) block
         run(std::true_type{}, n0, n1);
     } else {
         run(std::false_type{}, n0, n1);
-        // Scores so far above the first step's that a sum overflows (or anything that is not a number, which stays what it is), or a first step
-        // that was all of -infinity and so no reference, below which all others may vanish: once more with a reference that follows them.
+        // Scores so far above the first step's that a sum overflows (or anything that is not a number, which stays what it is), a first step
+        // that was all of -infinity and so no reference, below which all others may vanish, or a reference so large that its rounding to an exponent of
+        // two is no small factor: once more with a reference that follows them.
         float top = 0.f;
 #pragma unroll
         for (int b = 0; b < QB; ++b) {
-            if (m_run[b] == kNone) top = INFINITY;
+            if (m_run[b] == kNone || !(fabsf(ms[b]) < kLargeReference)) top = INFINITY;
             if (!C::ONES) top = __builtin_elementwise_maximum(top, l_run[b]);
 #pragma unroll
             for (int t = 0; t < DT; ++t)
@@ -982,7 +992,7 @@ extern "C" drf_status drf_block_attention_split(const drf_attn_shape* shape, int
     if (s.q_heads % s.kv_heads) DRF_FAIL(DRF_ESHAPE, "%d query heads are no multiple of %d kv heads", s.q_heads, s.kv_heads);
     if (s.head_dim > kMaxD) DRF_FAIL(DRF_ESHAPE, "head_dim must be <= %d (got %d)", kMaxD, s.head_dim);
     if (!log2_of(q_block) || !log2_of(kv_block)) DRF_FAIL(DRF_EINVAL, "blocks of %d queries and %d keys: each must be 32, 64 or 128", q_block, kv_block);
-    if (!(scale > 0.f) || !std::isfinite(scale)) DRF_FAIL(DRF_EINVAL, "scale must be a positive number");
+    if (!(scale > 0.f) || !std::isfinite(1.4426950408889634f * scale)) DRF_FAIL(DRF_EINVAL, "scale must be a positive number (and below 2.3e38)");
     if (s.q_tokens > 1 << 30 || s.kv_tokens > 1 << 30) DRF_FAIL(DRF_ESHAPE, "more than 2^30 tokens");
     if (s.slots == 0 || s.q_tokens == 0) return DRF_OK;
     if (!q || !k || !v || !out || !q->data || !out->data || (s.kv_tokens > 0 && (!k->data || !v->data || !blocks))) DRF_FAIL(DRF_EINVAL, "NULL buffer");

@@ -97,3 +97,78 @@ def test_equal_keys_tie_in_a_block_that_is_not_full(torch, drf, dtype, d, M, kv_
         for topk in (1, 2, nk - 1):
             got = ops.bits(torch, drf.block_select(q, k.expand(1, M, H, d), 32, kv_block, topk), nk)
             assert np.array_equal(got, np.broadcast_to(np.arange(nk) < topk, got.shape)), topk
+
+
+# ---- attention ------------------------------------------------------------------------------------------
+
+
+FORMS = [("f32", 1), ("bf16", 1)] + [("bf16", t) for t in ops.TILES]
+
+
+def weighted_alike(torch, drf, dtype, q, k, v, mask, weighted, q_block, kv_block, tiles, scale):
+    """Attention whose weights are all alike over the keys `weighted` [tokens] of a list and zero over the others; where a list has none of them, over all its
+    keys.  What is left is the sum of as many values in fp32, 2^-24 of the mean of |v| for each at most, and in bf16 the weights' own rounding, half a step: they are alike
+    but need not be one (a power of two of any fraction, by what they are taken relative to), and the denominator sums them before it at widths of 32."""
+    S, N, H, d = q.shape
+    M = k.shape[1]
+    c = -(-tiles // (-(-N // 32) * H * S))
+    got = drf.block_attention(q.repeat(c, 1, 1, 1), k.repeat(c, 1, 1, 1), v.repeat(c, 1, 1, 1), ops.pack(torch, mask).repeat(c, 1, 1, 1), q_block, kv_block, scale)
+    vv = v.double().cpu().numpy()
+    want, mag = np.zeros((S, N, H, d)), np.zeros((S, N, H, d))
+    for h in range(H):
+        for i in range(mask.shape[2]):
+            keys = np.flatnonzero(np.repeat(mask[0, h, i], kv_block)[:M])
+            keys = keys[weighted[keys]] if weighted[keys].any() else keys
+            if keys.size:
+                want[0, i * q_block:(i + 1) * q_block, h] = vv[0, keys, h].mean(0)
+                mag[0, i * q_block:(i + 1) * q_block, h] = np.abs(vv[0, keys, h]).mean(0)
+    ops.check(got[:1], want, dtype, (M + 4) * 2.0 ** -24 * mag + (ops.HALF["bf16"] * np.abs(want) if dtype == "bf16" else 0.0))
+    assert (got == got[:1]).all()
+
+
+@pytest.mark.parametrize("dtype,tiles", FORMS)
+@pytest.mark.parametrize("d", [24, 64, 72, 128])
+@pytest.mark.parametrize("qb", [64, 128])
+@pytest.mark.parametrize("scale", [1e-20, 2e-38, 1e-38, 1e-42])
+def test_the_smallest_scales(torch, drf, dtype, tiles, d, qb, scale):
+    """Scores that the scale takes all difference from: the mean of the values."""
+    rng = np.random.default_rng(d)
+    (q, _), (k, _), (v, _) = (ops.tensor(torch, rng, (1, n, 2, d), dtype, "plain") for n in (96, 160, 160))
+    mask = ops.random_mask(rng, 1, 2, 96, 160, qb, 32, 0.7)
+    weighted_alike(torch, drf, dtype, q, k, v, mask, np.ones(160, bool), qb, 32, tiles, scale)
+
+
+@pytest.mark.parametrize("dtype,tiles", FORMS)
+@pytest.mark.parametrize("d", [24, 64, 72, 128])
+@pytest.mark.parametrize("qb", [64, 128])
+@pytest.mark.parametrize("scale", [1e-37, 0.125, 1.0, 30.0, 1e6])
+@pytest.mark.parametrize("value", [-3.3895313892515355e38, 3.3895313892515355e38])
+def test_scores_as_large_as_the_type_has(torch, drf, dtype, tiles, d, qb, scale, value):
+    """Keys that a column of them marks with the type's lowest value have no weight beside others and equal weights among themselves; with its
+    largest they have all of it (e^-33 is left at the smallest scale here).  Marked first, last, all and none."""
+    rng = np.random.default_rng(d)
+    N, M = 96, 160
+    (q, _), (k, _), (v, _) = (ops.tensor(torch, rng, (1, n, 2, d), dtype, "plain") for n in (N, M, M))
+    q.zero_()
+    q[..., 0] = 1.0
+    for marked in (np.arange(M) < 64, np.arange(M) >= 100, np.ones(M, bool), np.zeros(M, bool), rng.random(M) < 0.3):
+        k[..., 0] = torch.from_numpy(np.where(marked, value, 0.0)).to(k).view(1, M, 1)
+        mask = ops.random_mask(rng, 1, 2, N, M, qb, 32, 0.7)
+        mask[0, 0, 0, :3] = [1, 0, 1]
+        weighted_alike(torch, drf, dtype, q, k, v, mask, marked if value > 0 else ~marked, qb, 32, tiles, scale)
+
+
+def test_the_smallest_scales_and_largest_scores_in_parts(torch, drf):
+    """The same where several workgroups share a list."""
+    rng = np.random.default_rng(0)
+    M, d = 8192, 64
+    (q, _), (k, _), (v, _) = (ops.tensor(torch, rng, (1, n, 2, d), "bf16", "plain") for n in (3, M, M))
+    words = ops.pack(torch, np.ones((1, 2, 1, M // 64), bool))
+    vv = v.double().cpu().numpy()
+    ops.check(drf.block_attention(q, k, v, words, 32, 64, 1e-39, split=True), np.broadcast_to(vv.mean(1, keepdims=True), q.shape), "bf16", (M + 4) * 2.0 ** -24 * np.abs(vv).mean(1, keepdims=True))
+    q.zero_()
+    q[..., 0] = 1.0
+    for weighted, value in ((np.arange(M) >= 7000, -3.3895313892515355e38), (np.arange(M) == 4321, 3.3895313892515355e38)):
+        k[..., 0] = torch.from_numpy(np.where(weighted == (value > 0), value, 0.0)).to(k).view(1, M, 1)
+        want, mag = vv[:, weighted].mean(1, keepdims=True), np.abs(vv[:, weighted]).mean(1, keepdims=True)
+        ops.check(drf.block_attention(q, k, v, words, 32, 64, 1.0, split=True), np.broadcast_to(want, q.shape), "bf16", (M + 4) * 2.0 ** -24 * mag)
