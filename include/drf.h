@@ -353,7 +353,7 @@ typedef struct {
  *   positions   DEVICE fp32 or NULL: element (slot s, token n, axis a) at positions[s * positions_slot_stride +
  *               n * n_axes + a] (stride 0: one table for all slots); replaces the grid, origin and step
  *   out         may be x itself (the same address and strides); otherwise the two do not overlap
- * head_dim <= 128, tokens <= 2^30.  16-byte aligned tensors whose strides and head_dim are multiples of 16 bytes take 16-byte
+ * head_dim <= 128, heads <= 65535, tokens <= 2^30, and fewer than 2^31 workgroups (of some 4 KB of x or more each).  16-byte aligned tensors whose strides and head_dim are multiples of 16 bytes take 16-byte
  * accesses; all others one element at a time.
  */
 drf_status drf_rope(const drf_rope_config* rope, drf_dtype dtype, int slots, int tokens, int heads, int head_dim,

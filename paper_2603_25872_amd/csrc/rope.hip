@@ -46,6 +46,7 @@ struct HeadsArgs {
     const int32_t* lens;
     float eps;
     int tile, tiles, parts, head_waves;     // tokens a workgroup; its waves, head_waves of them over the heads, times `parts` workgroups
+    int first;                              // workgroup that this launch begins with
     Turns r;
 };
 
@@ -101,7 +102,7 @@ __global__ void __launch_bounds__(kThreads) heads_kernel(const HeadsArgs a)
     int id = blockIdx.x;
     {
         const int q8 = gridDim.x >> 3, rem = gridDim.x & 7, xcd = id & 7;
-        id = xcd * q8 + (xcd < rem ? xcd : rem) + (id >> 3);
+        id = a.first + xcd * q8 + (xcd < rem ? xcd : rem) + (id >> 3);
     }
     const int part = id % a.parts;
     id /= a.parts;
@@ -394,12 +395,16 @@ template <typename T> drf_status launch(HeadsArgs& a, int norm, int rope, bool v
     // and over several workgroups until there is one for every CU
     a.parts = 1;
     while (a.parts * 2 * a.head_waves <= chunks && groups * a.parts < 256) a.parts *= 2;
-    if (groups * a.parts > 0x7fffffLL) DRF_FAIL(DRF_ESHAPE, "too many tokens");
-    const unsigned grid = (unsigned)(groups * a.parts);
-    if (norm == DRF_QK_NONE) go<T, DRF_QK_NONE>(a, rope, grid, st);
-    else if (norm == DRF_QK_RMS) go<T, DRF_QK_RMS>(a, rope, grid, st);
-    else go<T, DRF_QK_LAYER>(a, rope, grid, st);
-    DRF_HIP(hipGetLastError());
+    const long long all_groups = groups * a.parts, most = 1 << 23;              // (a launch holds fewer than 2^32 threads)
+    if (all_groups > 0x7fffffffLL) DRF_FAIL(DRF_ESHAPE, "more than 2^31 workgroups");
+    for (long long first = 0; first < all_groups; first += most) {
+        a.first = (int)first;
+        const unsigned grid = (unsigned)(all_groups - first < most ? all_groups - first : most);
+        if (norm == DRF_QK_NONE) go<T, DRF_QK_NONE>(a, rope, grid, st);
+        else if (norm == DRF_QK_RMS) go<T, DRF_QK_RMS>(a, rope, grid, st);
+        else go<T, DRF_QK_LAYER>(a, rope, grid, st);
+        DRF_HIP(hipGetLastError());
+    }
     return DRF_OK;
 }
 

@@ -172,3 +172,19 @@ def test_the_smallest_scales_and_largest_scores_in_parts(torch, drf):
         k[..., 0] = torch.from_numpy(np.where(weighted == (value > 0), value, 0.0)).to(k).view(1, M, 1)
         want, mag = vv[:, weighted].mean(1, keepdims=True), np.abs(vv[:, weighted]).mean(1, keepdims=True)
         ops.check(drf.block_attention(q, k, v, words, 32, 64, 1.0, split=True), np.broadcast_to(want, q.shape), "bf16", (M + 4) * 2.0 ** -24 * mag)
+
+
+def test_rotation_of_more_rows_than_one_launch_takes(torch, drf):
+    """34 GB of rows in place, as 16-byte accesses: each turns once, by its own position."""
+    d, tokens = 128, 8 * 2 ** 23 + 13
+    if torch.cuda.mem_get_info()[0] < 60 * 2 ** 30:
+        pytest.skip("needs 60 GB")
+    x = torch.ones(1, tokens, 1, d, device="cuda")
+    drf.rope(x, drf.rope_config((2,), (1,), theta=1.0), out=x)
+    for a in range(0, tokens, 2 ** 22):
+        part = x[0, a:a + 2 ** 22, 0]
+        phi = torch.arange(a, a + part.shape[0], device="cuda", dtype=torch.float64)
+        want = torch.stack([phi.cos() - phi.sin(), phi.sin() + phi.cos()], 1)
+        assert (part[:, :2] - want).abs().max() <= 2.0 ** -19 and (part[:, 2:] == 1).all()
+    del x, part
+    torch.cuda.empty_cache()

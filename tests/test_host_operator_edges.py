@@ -15,3 +15,8 @@ def attend(s, scale=0.125, **over):
 @pytest.mark.parametrize("scale", [2.4e38, 3.4e38])
 def test_a_scale_that_is_no_number_in_exponents_of_two_is_refused(scale):
     assert attend(shape(), scale) == EINVAL
+
+
+def test_more_workgroups_than_are_numbered_are_refused():
+    x, rc = heads(), config()
+    assert drf.lib().drf_rope(C.byref(rc), drf.BF16, 1 << 20, 1 << 30, 4, 64, None, None, 0, C.byref(x), C.byref(x), None) == ESHAPE
