@@ -996,17 +996,19 @@ extern "C" drf_status drf_block_attention_split(const drf_attn_shape* shape, int
     if (s.q_tokens > 1 << 30 || s.kv_tokens > 1 << 30) DRF_FAIL(DRF_ESHAPE, "more than 2^30 tokens");
     if (s.slots == 0 || s.q_tokens == 0) return DRF_OK;
     if (!q || !k || !v || !out || !q->data || !out->data || (s.kv_tokens > 0 && (!k->data || !v->data || !blocks))) DRF_FAIL(DRF_EINVAL, "NULL buffer");
-    for (const drf_heads* t : { q, k, v, out }) {
-        if (s.dtype == DRF_BF16 && ((reinterpret_cast<uintptr_t>(t->data) & 15u) || t->slot_stride % 8 || t->token_stride % 8 || t->head_stride % 8))
+    const drf_heads tq = used_strides(*q, s.slots, s.q_tokens, s.q_heads), to = used_strides(*out, s.slots, s.q_tokens, s.q_heads);
+    const drf_heads tk = used_strides(*k, s.slots, s.kv_tokens, s.kv_heads), tv = used_strides(*v, s.slots, s.kv_tokens, s.kv_heads);
+    for (const drf_heads& t : { tq, tk, tv, to }) {
+        if (s.dtype == DRF_BF16 && ((reinterpret_cast<uintptr_t>(t.data) & 15u) || t.slot_stride % 8 || t.token_stride % 8 || t.head_stride % 8))
             DRF_FAIL(DRF_ESHAPE, "bf16 needs 16-byte aligned tensors with strides %% 8 == 0");
-        if (t->token_stride < 0 || t->token_stride >= 1 << 24) DRF_FAIL(DRF_ESHAPE, "token stride %lld outside [0, 2^24)", (long long)t->token_stride);
+        if (t.token_stride < 0 || t.token_stride >= 1 << 24) DRF_FAIL(DRF_ESHAPE, "token stride %lld outside [0, 2^24)", (long long)t.token_stride);
     }
     if (s.dtype == DRF_BF16 && s.head_dim % 8) DRF_FAIL(DRF_ESHAPE, "bf16 needs head_dim %% 8 == 0 (got %d)", s.head_dim);
     BlockArgs a{};
-    a.q = { q->data, q->slot_stride, q->token_stride, q->head_stride };
-    a.k = { k->data, k->slot_stride, k->token_stride, k->head_stride };
-    a.v = { v->data, v->slot_stride, v->token_stride, v->head_stride };
-    a.out = out->data; a.out_slot = out->slot_stride; a.out_token = out->token_stride; a.out_head = out->head_stride;
+    a.q = { tq.data, tq.slot_stride, tq.token_stride, tq.head_stride };
+    a.k = { tk.data, tk.slot_stride, tk.token_stride, tk.head_stride };
+    a.v = { tv.data, tv.slot_stride, tv.token_stride, tv.head_stride };
+    a.out = to.data; a.out_slot = to.slot_stride; a.out_token = to.token_stride; a.out_head = to.head_stride;
     a.blocks = blocks; a.q_lens = s.q_lens; a.kv_lens = s.kv_lens;
     a.slots = s.slots; a.nq = s.q_tokens; a.nk = s.kv_tokens; a.q_heads = s.q_heads; a.group = s.q_heads / s.kv_heads; a.d = s.head_dim;
     a.q_shift = log2_of(q_block); a.kv_shift = log2_of(kv_block);

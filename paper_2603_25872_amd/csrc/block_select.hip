@@ -307,9 +307,10 @@ extern "C" drf_status drf_block_select(const drf_attn_shape* shape, int q_block,
 
     const int unit = s.dtype == DRF_BF16 ? 8 : 4;
     bool vec = s.head_dim % unit == 0;
-    auto side = [&](const drf_heads* t, int tokens, int heads, int block, int n, const int32_t* lens, double* out) {
-        vec = vec && (reinterpret_cast<uintptr_t>(t->data) & 15u) == 0 && t->slot_stride % unit == 0 && t->token_stride % unit == 0 && t->head_stride % unit == 0;
-        return PoolSide{ t->data, t->slot_stride, t->token_stride, t->head_stride, tokens, heads, block, n, lens, out };
+    auto side = [&](const drf_heads* x, int tokens, int heads, int block, int n, const int32_t* lens, double* out) {
+        const drf_heads t = used_strides(*x, s.slots, tokens, heads);
+        vec = vec && (reinterpret_cast<uintptr_t>(t.data) & 15u) == 0 && t.slot_stride % unit == 0 && t.token_stride % unit == 0 && t.head_stride % unit == 0;
+        return PoolSide{ t.data, t.slot_stride, t.token_stride, t.head_stride, tokens, heads, block, n, lens, out };
     };
     double* q_means = (double*)scratch;
     double* k_means = (double*)((char*)scratch + q_bytes);

@@ -83,6 +83,13 @@ enum { NOISE_NONE = 0, NOISE_EXPLICIT = 1, NOISE_PHILOX = 2 };
 drf_status set_noise_source(UpdateArgs* a, const drf_noise* noise);
 drf_status launch_update(const UpdateArgs& a, hipStream_t st);
 
+// ---- attention operators ---------------------------------------------------------
+// A tensor with a stride of zero where a dimension has one element: nothing is checked or chosen by what is never used.
+inline drf_heads used_strides(const drf_heads& t, int slots, int tokens, int heads)
+{
+    return { t.data, slots > 1 ? t.slot_stride : 0, tokens > 1 ? t.token_stride : 0, heads > 1 ? t.head_stride : 0 };
+}
+
 // ---- DiT kernels ------------------------------------------------------------------
 typedef __bf16 bf16_t;
 

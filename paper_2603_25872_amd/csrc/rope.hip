@@ -350,16 +350,17 @@ drf_status fill_turns(const drf_rope_config* rc, int head_dim, const float* posi
     return DRF_OK;
 }
 
-drf_status fill_side(const char* what, const drf_heads* x, const drf_heads* y, int heads, bool* vec, int unit, Side* s)
+drf_status fill_side(const char* what, const drf_heads* in, const drf_heads* out, int slots, int tokens, int heads, bool* vec, int unit, Side* s)
 {
-    if (!x || !y || !x->data || !y->data) DRF_FAIL(DRF_EINVAL, "%s: NULL tensor", what);
-    if (x->data == y->data && (x->slot_stride != y->slot_stride || x->token_stride != y->token_stride || x->head_stride != y->head_stride))
+    if (!in || !out || !in->data || !out->data) DRF_FAIL(DRF_EINVAL, "%s: NULL tensor", what);
+    const drf_heads x = used_strides(*in, slots, tokens, heads), y = used_strides(*out, slots, tokens, heads);
+    if (x.data == y.data && (x.slot_stride != y.slot_stride || x.token_stride != y.token_stride || x.head_stride != y.head_stride))
         DRF_FAIL(DRF_EINVAL, "%s: input and output share an address but not their strides", what);
-    s->x = x->data; s->xs = x->slot_stride; s->xt = x->token_stride; s->xh = x->head_stride;
-    s->y = y->data; s->ys = y->slot_stride; s->yt = y->token_stride; s->yh = y->head_stride;
+    s->x = x.data; s->xs = x.slot_stride; s->xt = x.token_stride; s->xh = x.head_stride;
+    s->y = y.data; s->ys = y.slot_stride; s->yt = y.token_stride; s->yh = y.head_stride;
     s->heads = heads;
-    for (const drf_heads* t : { x, y })
-        *vec = *vec && (reinterpret_cast<uintptr_t>(t->data) & 15u) == 0 && t->slot_stride % unit == 0 && t->token_stride % unit == 0 && t->head_stride % unit == 0;
+    for (const drf_heads& t : { x, y })
+        *vec = *vec && (reinterpret_cast<uintptr_t>(t.data) & 15u) == 0 && t.slot_stride % unit == 0 && t.token_stride % unit == 0 && t.head_stride % unit == 0;
     return DRF_OK;
 }
 
@@ -451,7 +452,7 @@ extern "C" drf_status drf_rope(const drf_rope_config* rope, drf_dtype dtype, int
     if ((rc = fill_turns(rope, head_dim, positions, positions_slot_stride, &a.r)) != DRF_OK) return rc;
     if (slots == 0 || tokens == 0) return DRF_OK;
     bool vec = true;
-    if ((rc = fill_side("x", x, out, heads, &vec, dtype == DRF_BF16 ? 8 : 4, &a.q)) != DRF_OK) return rc;
+    if ((rc = fill_side("x", x, out, slots, tokens, heads, &vec, dtype == DRF_BF16 ? 8 : 4, &a.q)) != DRF_OK) return rc;
     a.q.scale = 1.f;
     a.k = a.q; a.k.heads = 0;
     a.slots = slots; a.tokens = tokens; a.d = head_dim; a.lens = lens;
@@ -478,8 +479,8 @@ extern "C" drf_status drf_qk_norm_rope(const drf_qk_config* cfg, const drf_rope_
     if (s.slots == 0 || s.q_tokens == 0) return DRF_OK;
     bool vec = true;
     const int unit = s.dtype == DRF_BF16 ? 8 : 4;
-    if ((rc = fill_side("q", q, q_out, s.q_heads, &vec, unit, &a.q)) != DRF_OK) return rc;
-    if ((rc = fill_side("k", k, k_out, s.kv_heads, &vec, unit, &a.k)) != DRF_OK) return rc;
+    if ((rc = fill_side("q", q, q_out, s.slots, s.q_tokens, s.q_heads, &vec, unit, &a.q)) != DRF_OK) return rc;
+    if ((rc = fill_side("k", k, k_out, s.slots, s.kv_tokens, s.kv_heads, &vec, unit, &a.k)) != DRF_OK) return rc;
     a.q.scale = cfg->q_scale; a.k.scale = 1.f;
     a.q.gain = cfg->q_gain; a.q.bias = cfg->q_bias; a.k.gain = cfg->k_gain; a.k.bias = cfg->k_bias;
     a.slots = s.slots; a.tokens = s.q_tokens; a.d = s.head_dim; a.lens = s.q_lens; a.eps = (float)cfg->eps;

@@ -188,3 +188,31 @@ def test_rotation_of_more_rows_than_one_launch_takes(torch, drf):
         assert (part[:, :2] - want).abs().max() <= 2.0 ** -19 and (part[:, 2:] == 1).all()
     del x, part
     torch.cuda.empty_cache()
+
+
+# ---- layouts --------------------------------------------------------------------------------------------
+
+
+def with_odd_unused_strides(torch, x):
+    """The same memory with strides that no multiple of 16 bytes is, where a dimension has one element."""
+    strides = [s if n > 1 else 2 ** 24 + 3 for n, s in zip(x.shape[:3], x.stride())]
+    return torch.as_strided(x, x.shape, (*strides, 1), x.storage_offset())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("S,N,M,H,Hk", [(1, 1, 100, 1, 1), (1, 40, 100, 2, 1), (2, 1, 1, 2, 2), (1, 1, 1, 4, 1), (2, 33, 33, 1, 1)])
+def test_strides_of_one_element_are_not_used(torch, drf, dtype, S, N, M, H, Hk):
+    rng = np.random.default_rng(N)
+    d = 64
+    q, k, v = (ops.tensor(torch, rng, (S, n, h, d), dtype, "plain")[0] for n, h in ((N, H), (M, Hk), (M, Hk)))
+    cfg, odd = drf.rope_config((32, 32), (1, 9)), lambda t: with_odd_unused_strides(torch, t)  # noqa: E731
+    words = drf.block_select(q, k, 32, 32, 2)
+    assert torch.equal(drf.block_select(odd(q), odd(k), 32, 32, 2), words)
+    assert torch.equal(drf.rope(odd(q), cfg, out=odd(torch.empty_like(q))), drf.rope(q, cfg))
+    if N == M:
+        got = drf.qk_norm_rope(odd(q), odd(k), "rms", cfg, q_out=odd(torch.empty_like(q)), k_out=odd(torch.empty_like(k)))
+        assert all(torch.equal(a, b) for a, b in zip(got, drf.qk_norm_rope(q, k, "rms", cfg)))
+    want = drf.block_attention(q, k, v, words, 32, 32)
+    assert torch.equal(drf.block_attention(odd(q), odd(k), odd(v), words, 32, 32, out=odd(torch.empty_like(q))), want)
+    same = odd(q.clone())
+    assert torch.equal(drf.rope(same, cfg, out=torch.as_strided(same, q.shape, q.stride())), drf.rope(q, cfg))      # in place
