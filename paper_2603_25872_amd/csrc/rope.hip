@@ -73,11 +73,19 @@ __device__ inline double position(const Turns& r, int slot, int n, int axis)
     return p;
 }
 
-// cos and sin of a turn of p units of position
+// cos and sin of a turn of p units of position.  The angle is in double precision until a quarter turn at most is left of it, whose rounding to a float is
+// in proportion to a sine or cosine that is small (of half a turn it is as large where a sine is near zero as elsewhere).
 __device__ inline void turn(double p, double turns, float* c, float* s)
 {
     p *= turns;
-    sincospif(2.f * (float)(p - rint(p)), s, c);
+    p = 4.0 * (p - rint(p));
+    const double quarter = rint(p);                                 // -2 .. 2
+    float c0, s0;
+    sincospif(0.5f * (float)(p - quarter), &s0, &c0);
+    const int k = (int)quarter & 3;
+    const float x = k & 1 ? s0 : c0, y = k & 1 ? c0 : s0;
+    *c = k == 1 || k == 2 ? -x : x;
+    *s = k >= 2 ? -y : y;
 }
 
 template <typename T> __device__ inline float to_f32(T v) { return (float)v; }

@@ -216,3 +216,23 @@ def test_strides_of_one_element_are_not_used(torch, drf, dtype, S, N, M, H, Hk):
     assert torch.equal(drf.block_attention(odd(q), odd(k), odd(v), words, 32, 32, out=odd(torch.empty_like(q))), want)
     same = odd(q.clone())
     assert torch.equal(drf.rope(same, cfg, out=torch.as_strided(same, q.shape, q.stride())), drf.rope(q, cfg))      # in place
+
+
+@pytest.mark.parametrize("layout", ["plain", "odd"])
+@pytest.mark.parametrize("kind", ["pairs", "halves"])
+def test_angles_are_right_where_a_sine_or_cosine_is_small(torch, drf, layout, kind):
+    """(1, 0) turns to the cosine and sine of the angle.  A position below 4096 is at most 652 turns, of which double precision keeps 652 2^-51 (frequency, product,
+    rest), 2 pi times that together with the oracle's own below 2^-37 rad.  The rest of a quarter turn is rounded to fp32, half a step, of which sine and cosine
+    have at most as much; each of them is off by at most 4 steps of 2^-23; the products with 1 and 0 are exact."""
+    rng = np.random.default_rng(3)
+    S, N, H, d, dims = 1, 3000, 1, 64, (40, 24)
+    cfg = drf.rope_config(dims, (1, 1), layout=kind)
+    x, v = ops.tensor(torch, rng, (S, N, H, d), "f32", layout, 0.0)
+    _, first, second = ops.angles(cfg, S, N)
+    x[..., torch.from_numpy(first).cuda()] = 1.0
+    p = np.where(rng.random((N, 2)) < 0.5, rng.integers(-4096, 4096, (N, 2)), rng.uniform(-40, 40, (N, 2))).astype(np.float32)
+    phi, _, _ = ops.angles(cfg, S, N, p)
+    got = drf.rope(x, cfg, positions=torch.from_numpy(p).cuda()).double().cpu().numpy()[:, :, 0]
+    for columns, want in ((first, np.cos(phi)), (second, np.sin(phi))):
+        off = np.abs(got[..., columns] - want)
+        assert (off <= (2.0 ** -24 + 4 * 2.0 ** -23) * np.abs(want) + 2.0 ** -37).all(), float((off / np.abs(want)).max() * 2.0 ** 23)
