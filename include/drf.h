@@ -410,8 +410,10 @@ drf_status drf_block_attention(const drf_attn_shape* shape, int q_block, int kv_
 
 /*
  * The same where few queries attend to many keys (one token to a long context): several workgroups share a head's queries, leave their
- * parts in `scratch` and a second launch joins them.  Pays from about 1500 chosen keys a query block on.  scratch: DEVICE, 16-byte aligned, drf_block_attention_scratch_bytes() bytes of any
- * content, for one call at a time; NULL, or 0 of those bytes: exactly drf_block_attention.  Sums are formed in another order then.
+ * parts in `scratch` and a second launch joins them; sums are formed in another order then.  Pays from about 1500 chosen keys a query block on.
+ *   scratch   DEVICE, 16-byte aligned, at least drf_block_attention_scratch_bytes() bytes of any content, for one call at a time; fewer are DRF_EINVAL.
+ *             NULL, or a shape for which that gives 0: exactly drf_block_attention, and scratch and scratch_bytes are not looked at.
+ * It gives 0 for DRF_F32, for fewer than 8192 kv_tokens and for more than 64 tiles (of up to 32 queries of one head).
  */
 size_t drf_block_attention_scratch_bytes(const drf_attn_shape* shape);
 drf_status drf_block_attention_split(const drf_attn_shape* shape, int q_block, int kv_block, float scale, const uint32_t* blocks,

@@ -1016,8 +1016,8 @@ extern "C" drf_status drf_block_attention_split(const drf_attn_shape* shape, int
     a.words = (int)drf_block_words(s.kv_tokens, kv_block);
     a.scale_log2 = 1.4426950408889634f * scale;
     a.split = 1;
-    if (scratch) {
-        const int split = split_of(s);
+    const int split = scratch ? split_of(s) : 1;
+    if (split > 1) {
         if (reinterpret_cast<uintptr_t>(scratch) & 15u) DRF_FAIL(DRF_EINVAL, "scratch must be 16-byte aligned");
         if (scratch_bytes < parts_bytes(s, split)) DRF_FAIL(DRF_EINVAL, "scratch of %zu bytes, %zu are needed", scratch_bytes, parts_bytes(s, split));
         a.split = split;

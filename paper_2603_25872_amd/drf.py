@@ -465,7 +465,7 @@ def block_select(q, k, q_block, kv_block, topk, q_lens=None, kv_lens=None, out=N
 def block_attention(q, k, v, blocks, q_block, kv_block, scale=None, q_lens=None, kv_lens=None, out=None, split=False):
     """softmax(scale q k^T) v over the key blocks that the words `blocks` (as block_select gives them) name for each query block; scale
     1 / sqrt(head_dim) by default.  Rows behind a slot's q length are left as they were: zeros in an output made here.  split: several workgroups
-    share a head where its queries are few and its keys many (for lists from about 1500 keys on; see include/drf.h)."""
+    share a head where its queries are few and its keys many (for lists from about 1500 keys on, in bf16 over 8192 tokens or more; other calls are as without)."""
     import torch
     if out is None:
         out = (torch.empty if q_lens is None else torch.zeros)(q.shape, dtype=q.dtype, device=q.device)

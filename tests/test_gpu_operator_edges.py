@@ -236,3 +236,17 @@ def test_angles_are_right_where_a_sine_or_cosine_is_small(torch, drf, layout, ki
     for columns, want in ((first, np.cos(phi)), (second, np.sin(phi))):
         off = np.abs(got[..., columns] - want)
         assert (off <= (2.0 ** -24 + 4 * 2.0 ** -23) * np.abs(want) + 2.0 ** -37).all(), float((off / np.abs(want)).max() * 2.0 ** 23)
+
+
+def test_scratch_that_a_call_has_no_use_for_is_not_looked_at(torch, drf):
+    """Where drf_block_attention_scratch_bytes() is 0, the call with scratch, of any size and alignment, is the one without."""
+    torch.manual_seed(0)
+    for dtype, kind in ((torch.bfloat16, drf.BF16), (torch.float32, drf.F32)):
+        q, k, v = (torch.randn(1, n, 2, 64, device="cuda").to(dtype) for n in (5, 300, 300))
+        words, out = drf.block_select(q, k, 32, 32, 3), torch.empty_like(q)
+        shape = drf.AttnShape(kind, 1, 5, 300, 2, 2, 64, None, None)
+        assert drf.lib().drf_block_attention_scratch_bytes(drf.C.byref(shape)) == 0
+        scratch = torch.empty(16, device="cuda")
+        rc = drf.lib().drf_block_attention_split(drf.C.byref(shape), 32, 32, 0.125, words.data_ptr(), *[drf.C.byref(drf._heads(t)) for t in (q, k, v, out)],
+                                                 scratch.data_ptr() + 4, 0, drf._current(q))
+        assert rc == 0 and torch.equal(out, drf.block_attention(q, k, v, words, 32, 32, scale=0.125))
