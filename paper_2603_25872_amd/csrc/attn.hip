@@ -494,11 +494,8 @@ drf_status launch_bf16_cfg(const AttnArgs& a, float scale_log2, hipStream_t st)
     constexpr size_t smem = ((size_t)2 * (KC * LDKS + (VTR ? KC : DT * 32) * LDV) + (size_t)NW * 32 * (DT * 32 + 8)) * sizeof(bf16_t);
     static_assert(smem <= 160 * 1024 && smem % 16 == 0, "LDS budget");
     auto kern = attn_bf16_kernel<KS, DT, NW, KC, PERSIST, VTR>;
-    static bool attr_set = false;
-    if (!attr_set) {
-        DRF_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
-        attr_set = true;
-    }
+    static std::atomic<uint64_t> lds_allowed{ 0 };
+    DRF_HIP(allow_lds(reinterpret_cast<const void*>(kern), (int)smem, lds_allowed));
     const int nqb = (a.Nq + NW * 32 - 1) / (NW * 32);
     const long long n_items = (long long)nqb * a.heads * a.slots;
     if (n_items > 0x7fffffffLL) DRF_FAIL(DRF_ESHAPE, "attention: too many (query block, head, slot) items");

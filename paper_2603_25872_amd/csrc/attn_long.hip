@@ -411,11 +411,8 @@ __global__ void __launch_bounds__(kWaves * 64, 2) attn_long_kernel(const AttnArg
 template <int P8, bool PRE> drf_status launch_inst(const AttnArgs& a, hipStream_t st)
 {
     auto kern = attn_long_kernel<P8, PRE>;
-    static bool attr_set = false;
-    if (!attr_set) {
-        DRF_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, LongCfg<P8>::SMEM));
-        attr_set = true;
-    }
+    static std::atomic<uint64_t> lds_allowed{ 0 };
+    DRF_HIP(allow_lds(reinterpret_cast<const void*>(kern), LongCfg<P8>::SMEM, lds_allowed));
     const int nqb = (a.Nq + kQpg - 1) / kQpg;
     const long long n_items = (long long)nqb * a.heads * a.slots;
     if (n_items > 0x7fffffffLL) DRF_FAIL(DRF_ESHAPE, "attention: too many (query block, head, slot) items");

@@ -544,11 +544,8 @@ template <int NI, int MI, bool ATT> drf_status launch_inst(const ChainArgs& a, h
 {
     using C = ChainCfg<NI, MI>;
     auto kern = block_chain_kernel<NI, MI, ATT>;
-    static bool attr_set = false;
-    if (!attr_set) {
-        DRF_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, C::SMEM));
-        attr_set = true;
-    }
+    static std::atomic<uint64_t> lds_allowed{ 0 };
+    DRF_HIP(allow_lds(reinterpret_cast<const void*>(kern), C::SMEM, lds_allowed));
     const int tiles = (a.tokens + C::ROWS - 1) / C::ROWS;
     hipLaunchKernelGGL(kern, dim3((unsigned)(a.slots * tiles * a.parts)), dim3(kChainWaves * 64), C::SMEM, st, a, tiles);
     DRF_HIP(hipGetLastError());

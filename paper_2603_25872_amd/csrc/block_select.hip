@@ -259,11 +259,8 @@ size_t side_bytes(int slots, int heads, int blocks, int d)
 template <int NK, int NW> drf_status launch_select(const SelectArgs& a, unsigned grid, size_t lds, hipStream_t st)
 {
     auto kern = select_kernel<NK, NW>;
-    static bool attr_set = false;
-    if (!attr_set) {
-        DRF_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, kRows * (64 * NK + 2) * (int)sizeof(double)));
-        attr_set = true;
-    }
+    static std::atomic<uint64_t> lds_allowed{ 0 };
+    DRF_HIP(allow_lds(reinterpret_cast<const void*>(kern), kRows * (64 * NK + 2) * (int)sizeof(double), lds_allowed));
     hipLaunchKernelGGL(kern, dim3(grid), dim3(NW * 64), lds, st, a);
     DRF_HIP(hipGetLastError());
     return DRF_OK;

@@ -8,6 +8,7 @@
 #include <vector>
 
 #include "../../include/drf.h"
+#include "lds_limit.h"
 
 namespace drf {
 

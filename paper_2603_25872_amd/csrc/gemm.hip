@@ -523,13 +523,10 @@ drf_status launch_bf16_xl(const bf16_t* A, const bf16_t* W, int M, int N, int K,
 {
     constexpr size_t smem = (size_t)NS * WK * (BM + BN) * BK * sizeof(bf16_t) + epi_lds_bytes(BN) + 256;
     static_assert(smem <= 160 * 1024, "LDS of a CU");
-    static bool attr_set = false;
+    static std::atomic<uint64_t> lds_allowed{ 0 };
     auto kern = gemm_bf16_xl_kernel<BM, BN, BK, NS, WM, WN, WK, false, RS>;
     if (K % (BK * WK) != 0) DRF_FAIL(DRF_ESHAPE, "bf16 GEMM tile needs K %% %d == 0 (K=%d)", BK * WK, K);
-    if (!attr_set) {
-        DRF_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
-        attr_set = true;
-    }
+    DRF_HIP(allow_lds(reinterpret_cast<const void*>(kern), (int)smem, lds_allowed));
     const int tiles_m = (M - m_first + BM - 1) / BM, tiles_n = (N + BN - 1) / BN;
     hipLaunchKernelGGL(kern, dim3(tiles_m * tiles_n), dim3(WM * WN * WK * 64), smem, st, A, W, M, N, K, e, tiles_m, tiles_n, m_first, SplitK{});
     DRF_HIP(hipGetLastError());
@@ -543,15 +540,12 @@ drf_status launch_bf16_splitk(const bf16_t* A, const bf16_t* W, int M, int N, in
 {
     constexpr size_t smem = (size_t)NS * WK * (BM + BN) * BK * sizeof(bf16_t) + epi_lds_bytes(BN) + 256;
     static_assert(smem <= 160 * 1024, "LDS of a CU");
-    static bool attr_set = false;
+    static std::atomic<uint64_t> lds_allowed{ 0 };
     auto kern = gemm_bf16_xl_kernel<BM, BN, BK, NS, WM, WN, WK, true>;
     const int tiles_m = (M + BM - 1) / BM, tiles_n = (N + BN - 1) / BN;
     if (!part || K % (BK * WK) != 0 || K / (BK * WK) < splits || (size_t)tiles_m * tiles_n * splits * BM * BN > kSplitKScratchFloats)
         DRF_FAIL(DRF_ESHAPE, "split-K GEMM of %d parts does not fit (M=%d N=%d K=%d)", splits, M, N, K);
-    if (!attr_set) {
-        DRF_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
-        attr_set = true;
-    }
+    DRF_HIP(allow_lds(reinterpret_cast<const void*>(kern), (int)smem, lds_allowed));
     SplitK sk{ splits, tiles_n, part };
     hipLaunchKernelGGL(kern, dim3(tiles_m * tiles_n * splits), dim3(WM * WN * WK * 64), smem, st, A, W, M, N, K, e, tiles_m, tiles_n * splits, 0, sk);
     DRF_HIP(hipGetLastError());

@@ -208,12 +208,9 @@ drf_status launch_pair(const bf16_t* A, const bf16_t* W, int M, int N, int K, co
 {
     constexpr size_t smem = pair_lds_rows_at(BM, BN, NS) + epi_lds_bytes(BN) + 256;
     static_assert(smem <= 160 * 1024, "LDS of a CU");
-    static bool attr_set = false;
+    static std::atomic<uint64_t> lds_allowed{ 0 };
     auto kern = gemm_bf16_pair_kernel<BM, BN, NS>;
-    if (!attr_set) {
-        DRF_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
-        attr_set = true;
-    }
+    DRF_HIP(allow_lds(reinterpret_cast<const void*>(kern), (int)smem, lds_allowed));
     const int tiles_m = (M - m_first + BM - 1) / BM, tiles_n = (N + BN - 1) / BN;
     hipLaunchKernelGGL(kern, dim3(tiles_m * tiles_n), dim3(256), smem, st, A, W, M, N, K, e, tiles_m, tiles_n, m_first);
     DRF_HIP(hipGetLastError());
