@@ -315,7 +315,7 @@ drf_status drf_plan_build(const drf_sched_config* sched, drf_mode mode, int n, i
  * data + s * slot_stride + n * token_stride + h * head_stride + c, strides in elements.  A column range
  * of a qkv Linear's rows (token_stride = row width, head_stride = head_dim) and planes stored head by
  * head (head_stride = tokens * head_dim, token_stride = head_dim) are both such tensors.  The stride of a dimension of one element is not used
- * and may be anything.
+ * and may be anything.  Inputs may have strides of zero (one row for all); an output whose rows lie on one another is DRF_EINVAL.
  */
 typedef struct { void* data; int64_t slot_stride, token_stride, head_stride; } drf_heads;
 

@@ -1000,6 +1000,7 @@ extern "C" drf_status drf_block_attention_split(const drf_attn_shape* shape, int
             DRF_FAIL(DRF_ESHAPE, "bf16 needs 16-byte aligned tensors with strides %% 8 == 0");
         if (t.token_stride < 0 || t.token_stride >= 1 << 24) DRF_FAIL(DRF_ESHAPE, "token stride %lld outside [0, 2^24)", (long long)t.token_stride);
     }
+    if (rows_overlap(to, s.slots, s.q_tokens, s.q_heads, s.head_dim)) DRF_FAIL(DRF_EINVAL, "rows of the output lie on one another");
     if (s.dtype == DRF_BF16 && s.head_dim % 8) DRF_FAIL(DRF_ESHAPE, "bf16 needs head_dim %% 8 == 0 (got %d)", s.head_dim);
     BlockArgs a{};
     a.q = { tq.data, tq.slot_stride, tq.token_stride, tq.head_stride };

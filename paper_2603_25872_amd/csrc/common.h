@@ -90,6 +90,12 @@ inline drf_heads used_strides(const drf_heads& t, int slots, int tokens, int hea
 {
     return { t.data, slots > 1 ? t.slot_stride : 0, tokens > 1 ? t.token_stride : 0, heads > 1 ? t.head_stride : 0 };
 }
+// Whether two rows of such a tensor that differ in one index alone lie on one another (an expanded tensor): nothing to write to.
+inline bool rows_overlap(const drf_heads& t, int slots, int tokens, int heads, int head_dim)
+{
+    auto near = [&](int n, int64_t stride) { return n > 1 && stride > -(int64_t)head_dim && stride < head_dim; };
+    return near(slots, t.slot_stride) || near(tokens, t.token_stride) || near(heads, t.head_stride);
+}
 
 // ---- DiT kernels ------------------------------------------------------------------
 typedef __bf16 bf16_t;

@@ -358,12 +358,13 @@ drf_status fill_turns(const drf_rope_config* rc, int head_dim, const float* posi
     return DRF_OK;
 }
 
-drf_status fill_side(const char* what, const drf_heads* in, const drf_heads* out, int slots, int tokens, int heads, bool* vec, int unit, Side* s)
+drf_status fill_side(const char* what, const drf_heads* in, const drf_heads* out, int slots, int tokens, int heads, int head_dim, bool* vec, int unit, Side* s)
 {
     if (!in || !out || !in->data || !out->data) DRF_FAIL(DRF_EINVAL, "%s: NULL tensor", what);
     const drf_heads x = used_strides(*in, slots, tokens, heads), y = used_strides(*out, slots, tokens, heads);
     if (x.data == y.data && (x.slot_stride != y.slot_stride || x.token_stride != y.token_stride || x.head_stride != y.head_stride))
         DRF_FAIL(DRF_EINVAL, "%s: input and output share an address but not their strides", what);
+    if (rows_overlap(y, slots, tokens, heads, head_dim)) DRF_FAIL(DRF_EINVAL, "%s: rows of the output lie on one another", what);
     s->x = x.data; s->xs = x.slot_stride; s->xt = x.token_stride; s->xh = x.head_stride;
     s->y = y.data; s->ys = y.slot_stride; s->yt = y.token_stride; s->yh = y.head_stride;
     s->heads = heads;
@@ -460,7 +461,7 @@ extern "C" drf_status drf_rope(const drf_rope_config* rope, drf_dtype dtype, int
     if ((rc = fill_turns(rope, head_dim, positions, positions_slot_stride, &a.r)) != DRF_OK) return rc;
     if (slots == 0 || tokens == 0) return DRF_OK;
     bool vec = true;
-    if ((rc = fill_side("x", x, out, slots, tokens, heads, &vec, dtype == DRF_BF16 ? 8 : 4, &a.q)) != DRF_OK) return rc;
+    if ((rc = fill_side("x", x, out, slots, tokens, heads, head_dim, &vec, dtype == DRF_BF16 ? 8 : 4, &a.q)) != DRF_OK) return rc;
     a.q.scale = 1.f;
     a.k = a.q; a.k.heads = 0;
     a.slots = slots; a.tokens = tokens; a.d = head_dim; a.lens = lens;
@@ -487,8 +488,8 @@ extern "C" drf_status drf_qk_norm_rope(const drf_qk_config* cfg, const drf_rope_
     if (s.slots == 0 || s.q_tokens == 0) return DRF_OK;
     bool vec = true;
     const int unit = s.dtype == DRF_BF16 ? 8 : 4;
-    if ((rc = fill_side("q", q, q_out, s.slots, s.q_tokens, s.q_heads, &vec, unit, &a.q)) != DRF_OK) return rc;
-    if ((rc = fill_side("k", k, k_out, s.slots, s.kv_tokens, s.kv_heads, &vec, unit, &a.k)) != DRF_OK) return rc;
+    if ((rc = fill_side("q", q, q_out, s.slots, s.q_tokens, s.q_heads, s.head_dim, &vec, unit, &a.q)) != DRF_OK) return rc;
+    if ((rc = fill_side("k", k, k_out, s.slots, s.kv_tokens, s.kv_heads, s.head_dim, &vec, unit, &a.k)) != DRF_OK) return rc;
     a.q.scale = cfg->q_scale; a.k.scale = 1.f;
     a.q.gain = cfg->q_gain; a.q.bias = cfg->q_bias; a.k.gain = cfg->k_gain; a.k.bias = cfg->k_bias;
     a.slots = s.slots; a.tokens = s.q_tokens; a.d = s.head_dim; a.lens = s.q_lens; a.eps = (float)cfg->eps;

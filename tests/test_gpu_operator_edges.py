@@ -250,3 +250,23 @@ def test_scratch_that_a_call_has_no_use_for_is_not_looked_at(torch, drf):
         rc = drf.lib().drf_block_attention_split(drf.C.byref(shape), 32, 32, 0.125, words.data_ptr(), *[drf.C.byref(drf._heads(t)) for t in (q, k, v, out)],
                                                  scratch.data_ptr() + 4, 0, drf._current(q))
         assert rc == 0 and torch.equal(out, drf.block_attention(q, k, v, words, 32, 32, scale=0.125))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_expanded_inputs_and_outputs(torch, drf, dtype):
+    """Tensors expanded over slots, tokens or heads are inputs like others; as outputs they are refused."""
+    rng = np.random.default_rng(9)
+    S, N, H, d = 2, 33, 3, 64
+    cfg = drf.rope_config((32, 32), (1, 9))
+    for size in ((1, N, H, d), (S, 1, H, d), (S, N, 1, d)):
+        x, v = ops.tensor(torch, rng, size, dtype, "plain")
+        wide, v = x.expand(S, N, H, d), np.broadcast_to(v, (S, N, H, d))
+        whole = wide.contiguous()
+        ops.check(drf.rope(wide, cfg), ops.rotated(v, cfg), dtype, 2.0 ** -19 * np.abs(v).max())
+        words = drf.block_select(wide, wide, 32, 32, 1)
+        assert torch.equal(words, drf.block_select(whole, whole, 32, 32, 1))
+        assert torch.equal(drf.block_attention(wide, wide, wide, words, 32, 32), drf.block_attention(whole, whole, whole, words, 32, 32))
+        for call in (lambda: drf.rope(whole, cfg, out=wide), lambda: drf.qk_norm_rope(whole, whole, "rms", cfg, k_out=wide),
+                     lambda: drf.block_attention(whole, whole, whole, words, 32, 32, out=wide)):
+            with pytest.raises(drf.DrfError):
+                call()

@@ -20,3 +20,17 @@ def test_a_scale_that_is_no_number_in_exponents_of_two_is_refused(scale):
 def test_more_workgroups_than_are_numbered_are_refused():
     x, rc = heads(), config()
     assert drf.lib().drf_rope(C.byref(rc), drf.BF16, 1 << 20, 1 << 30, 4, 64, None, None, 0, C.byref(x), C.byref(x), None) == ESHAPE
+
+
+@pytest.mark.parametrize("over", [dict(slot=0), dict(token=0), dict(head=0), dict(head=32), dict(token=-56), dict(slot=8)])
+@pytest.mark.parametrize("dtype", [drf.BF16, drf.F32])
+def test_outputs_whose_rows_lie_on_one_another_are_refused(over, dtype):
+    """(Every row would be written by several workgroups at once.)  As inputs they are calls like others; of a dimension of one element no stride counts."""
+    L, x, y, rc, s = drf.lib(), heads(), heads(2 * FAKE, **over), config(), shape(dtype=dtype)
+    ref = C.byref
+    assert L.drf_rope(ref(rc), dtype, 2, 64, 4, 64, None, None, 0, ref(x), ref(y), None) == EINVAL
+    cfg = drf.QkConfig(drf.QK_RMS, 1e-6, 1.0)
+    for outs in ((y, x), (x, y)):
+        assert L.drf_qk_norm_rope(ref(cfg), ref(rc), ref(s), None, 0, ref(x), ref(x), ref(outs[0]), ref(outs[1]), None) == EINVAL
+    assert attend(s, out=y) == (ESHAPE if over.get("token", 0) < 0 else EINVAL)
+    assert L.drf_rope(ref(rc), dtype, 0, 64, 4, 64, None, None, 0, ref(x), ref(y), None) == 0
