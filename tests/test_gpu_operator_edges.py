@@ -252,6 +252,35 @@ def test_scratch_that_a_call_has_no_use_for_is_not_looked_at(torch, drf):
         assert rc == 0 and torch.equal(out, drf.block_attention(q, k, v, words, 32, 32, scale=0.125))
 
 
+@pytest.mark.parametrize("dtype,S,N,M,H,Hk,d,kv_block,share,split", [
+    ("bf16", 1, 1, 20000, 2, 1, 128, 32, 0.7, True), ("bf16", 1, 33, 14000, 2, 2, 64, 32, 0.3, True), ("bf16", 1, 1, 9000, 16, 2, 72, 128, 1.0, True),
+    ("bf16", 1, 5, 8255, 1, 1, 128, 64, 0.05, True), ("bf16", 2, 64, 16384, 1, 1, 96, 128, 0.4, True), ("bf16", 1, 1, 9001, 2, 1, 64, 32, 1.0, False),
+    ("bf16", 1, 33, 5000, 2, 1, 128, 64, 0.4, False), ("bf16", 4, 300, 3001, 16, 1, 72, 32, 0.3, False), ("bf16", 4, 700, 3001, 16, 1, 128, 64, 0.5, False),
+    ("bf16", 2, 700, 3001, 32, 1, 128, 128, 0.5, False), ("f32", 1, 1, 9001, 2, 1, 128, 32, 0.6, False), ("f32", 2, 70, 4000, 2, 1, 64, 64, 1.0, False)])
+def test_every_step_of_a_list_counts_once(torch, drf, dtype, S, N, M, H, Hk, d, kv_block, share, split):
+    """Queries of zeros weigh the keys of a list alike, and column c of the values is one on the 32 keys of one step alone: the result is that step's share of the
+    list, nothing if a step is missed, twice as much if it is taken twice.  Every step of the keys is a column's in turn.  Weights and sums are whole numbers,
+    exact in fp32; the quotient and product with its inverse are off by 2^-22."""
+    rng = np.random.default_rng(M + d)
+    q_block = 128 if N == 700 and kv_block == 128 else 64 if N > 64 else 32
+    mask = ops.random_mask(rng, S, H, N, M, q_block, kv_block, share)
+    q, k = torch.zeros(S, N, H, d, device="cuda"), torch.randn(S, M, Hk, d, device="cuda")
+    chosen = np.repeat(mask, kv_block, axis=-1)[..., :M]                        # [slots, heads, query blocks, keys]
+    steps = -(-M // 32)
+    a_step = np.add.reduceat(chosen, np.arange(0, M, 32), axis=-1, dtype=np.int64)
+    share_of = a_step / np.maximum(chosen.sum(-1, keepdims=True), 1)            # [slots, heads, query blocks, steps]
+    q, k, words = q.to(ops.dtype_of(torch, dtype)), k.to(ops.dtype_of(torch, dtype)), ops.pack(torch, mask)
+    step_of = torch.arange(M, device="cuda") // 32
+    row_block = np.arange(N) // q_block
+    for first in range(0, steps, d):
+        v = (step_of[:, None] == first + torch.arange(d, device="cuda")).to(q.dtype).view(1, M, 1, d).expand(S, M, Hk, d).contiguous()
+        got = drf.block_attention(q, k, v, words, q_block, kv_block, split=split)
+        want = np.zeros((S, H, len(row_block), d))
+        want[..., :min(d, steps - first)] = share_of[:, :, row_block, first:first + d]
+        want = want.transpose(0, 2, 1, 3)
+        ops.check(got, want, dtype, 2.0 ** -22 * want)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_expanded_inputs_and_outputs(torch, drf, dtype):
     """Tensors expanded over slots, tokens or heads are inputs like others; as outputs they are refused."""
