@@ -38,13 +38,6 @@ struct BlockArgs {
     float* parts;                               // [tile][split][32][d + 4]: O, and m and l behind it
 };
 
-__device__ inline int slot_len(const int32_t* lens, int slot, int tokens)
-{
-    if (!lens) return tokens;
-    const int n = lens[slot];
-    return n < 0 ? 0 : n < tokens ? n : tokens;
-}
-
 // The steps of 32 keys of a query block's list, W of them passed over after each.  All of it is scalar arithmetic.
 template <int W> struct Walk {
     typedef const __attribute__((address_space(4))) uint32_t* scalar_ptr;
@@ -171,12 +164,7 @@ __global__ void __launch_bounds__(64 * W * SH, P8 > 11 && QB == 2 ? 1 : 2) block
     static_assert(SH == 1 || (W == 1 && QB == 2), "two waves of 64 queries share their keys");
     const int wave = W * SH > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0;
     unsigned char* mem = smem + (SH > 1 ? 0 : wave * C::WAVE);
-    // consecutive items (query tiles of one head) on one XCD: ids are dealt round-robin over the 8 of them, each with its own L2
-    int item = blockIdx.x;
-    {
-        const int q8 = n_items >> 3, rem = n_items & 7, xcd = item & 7;
-        item = xcd * q8 + (xcd < rem ? xcd : rem) + (item >> 3);
-    }
+    int item = item_by_xcd(blockIdx.x, n_items);                // query tiles of one head on one XCD
     const int part = SPLIT ? item % a.split : 0;
     if (SPLIT) item /= a.split;
     const int tile = item % q_tiles, sh = item / q_tiles, slot = sh / a.q_heads, h = sh - slot * a.q_heads;

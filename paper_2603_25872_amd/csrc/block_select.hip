@@ -27,13 +27,6 @@ struct PoolSide {
     double* out;        // means [slot][head][blocks up to a multiple of 16][columns up to a multiple of 8]
 };
 
-__device__ inline int slot_len(const int32_t* lens, int slot, int tokens)
-{
-    if (!lens) return tokens;
-    const int n = lens[slot];
-    return n < 0 ? 0 : n < tokens ? n : tokens;
-}
-
 // A wave takes a head of a block: 64 / P rows at a time in pieces of 16 bytes (VEC), or a row at a time, a column or two a lane.  Bound by the read
 // of q and k: 64 slots x 1024 tokens x 32 heads of 72 in bf16, 302 MB, 63 us (4.8 TB/s); 2 x 19344 x 16 heads of 64 in fp32, 158 MB, 39 us
 // (4.0) from memory and 16 out of the Infinity Cache.  Six rows in flight a lane, and a block's means stored as one row: by columns, where 8 bytes of a line leave at a time, the first took 87 us.
@@ -127,12 +120,8 @@ __global__ void __launch_bounds__(NW * 64) select_kernel(const SelectArgs a)
     extern __shared__ __attribute__((aligned(16))) double score[];          // [16][nk padded]
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int qtiles = (a.nq + 15) / 16, ktiles = (a.nk + 15) / 16, ld = ktiles * 16 + 2;
-    // the rows of one head on one XCD (ids are dealt round-robin over the 8 of them, each with its own L2): they read the same means of keys
-    int id = blockIdx.x;
-    {
-        const int q8 = gridDim.x >> 3, rem = gridDim.x & 7, xcd = id & 7;
-        id = xcd * q8 + (xcd < rem ? xcd : rem) + (id >> 3);
-    }
+    // the rows of one head on one XCD: they read the same means of keys
+    const int id = item_by_xcd(blockIdx.x, gridDim.x);
     const int qt = id % qtiles, sh = id / qtiles, slot = sh / a.q_heads, h = sh - slot * a.q_heads;
     const int q_len = slot_len(a.q_lens, slot, a.q_tokens), kv_len = slot_len(a.kv_lens, slot, a.kv_tokens);
     const int n_valid = (kv_len + a.kv_block - 1) / a.kv_block;             // key blocks that hold a key

@@ -90,6 +90,21 @@ inline drf_heads used_strides(const drf_heads& t, int slots, int tokens, int hea
 {
     return { t.data, slots > 1 ? t.slot_stride : 0, tokens > 1 ? t.token_stride : 0, heads > 1 ? t.head_stride : 0 };
 }
+// Tokens of a slot that exist.
+__device__ inline int slot_len(const int32_t* lens, int slot, int tokens)
+{
+    if (!lens) return tokens;
+    const int n = lens[slot];
+    return n < 0 ? 0 : n < tokens ? n : tokens;
+}
+
+// Work item of workgroup id of n: consecutive items on one XCD (ids are dealt round-robin over the 8 of them, each with its own L2).
+__device__ inline int item_by_xcd(int id, int n)
+{
+    const int q8 = n >> 3, rem = n & 7, xcd = id & 7;
+    return xcd * q8 + (xcd < rem ? xcd : rem) + (id >> 3);
+}
+
 // Whether two rows of such a tensor that differ in one index alone lie on one another (an expanded tensor): nothing to write to.
 inline bool rows_overlap(const drf_heads& t, int slots, int tokens, int heads, int head_dim)
 {

@@ -50,13 +50,6 @@ struct HeadsArgs {
     Turns r;
 };
 
-__device__ inline int slot_len(const int32_t* lens, int slot, int tokens)
-{
-    if (!lens) return tokens;
-    const int n = lens[slot];
-    return n < 0 ? 0 : n < tokens ? n : tokens;
-}
-
 // position of token n of a slot on axis `axis`
 __device__ inline double position(const Turns& r, int slot, int n, int axis)
 {
@@ -106,12 +99,8 @@ __global__ void __launch_bounds__(kThreads) heads_kernel(const HeadsArgs a)
     typedef T half_piece __attribute__((ext_vector_type(E / 2)));
     extern __shared__ __attribute__((aligned(16))) float tab[];     // [token][pair](cos, sin)
     const int d = a.d, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    // consecutive tiles on one XCD (ids are dealt round-robin over the 8 of them, each with its own L2): they share the lines that a tile ends inside of
-    int id = blockIdx.x;
-    {
-        const int q8 = gridDim.x >> 3, rem = gridDim.x & 7, xcd = id & 7;
-        id = a.first + xcd * q8 + (xcd < rem ? xcd : rem) + (id >> 3);
-    }
+    // consecutive tiles on one XCD: they share the lines that a tile ends inside of
+    int id = a.first + item_by_xcd(blockIdx.x, gridDim.x);
     const int part = id % a.parts;
     id /= a.parts;
     const int slot = id / a.tiles, t0 = (id - slot * a.tiles) * a.tile, left = slot_len(a.lens, slot, a.tokens) - t0;
