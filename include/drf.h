@@ -391,7 +391,7 @@ drf_status drf_qk_norm_rope(const drf_qk_config* cfg, const drf_rope_config* rop
  *            bit j % 32 of word j / 32 of row i: query block i attends to key block j.  A query block with no query
  *            inside its slot's length has none.
  *   scratch  DEVICE, 16-byte aligned, drf_block_select_scratch_bytes() bytes of any content
- * head_dim <= 128, at most 1024 key blocks.  drf_block_words and .._scratch_bytes give 0 for sizes that are refused.
+ * head_dim <= 128, at most 1024 key blocks, slots * (query blocks + key blocks) < 2^23 and slots * q_heads * ceil(query blocks / 16) < 2^21.  drf_block_words and .._scratch_bytes give 0 for sizes that are refused.
  */
 size_t drf_block_words(int kv_tokens, int kv_block);
 size_t drf_block_select_scratch_bytes(const drf_attn_shape* shape, int q_block, int kv_block);
@@ -403,7 +403,8 @@ drf_status drf_block_select(const drf_attn_shape* shape, int q_block, int kv_blo
  * caller's own choice as well as drf_block_select's; bits of blocks beyond the keys do not count).  A query with no key gives
  * zeros.  Rows of out behind a slot's q length are left as they were; keys and values behind its kv length, and of blocks
  * not chosen, are not looked at.  out overlaps no input.
- * scale > 0, finite also times log2(e).  head_dim <= 128, tokens <= 2^30; DRF_BF16: head_dim % 8 == 0, 16-byte aligned tensors, strides % 8 == 0.  token strides below 2^24.
+ * scale > 0, finite also times log2(e).  head_dim <= 128, tokens <= 2^30, and over all slots and heads fewer than 2^25 tiles of 32 queries
+ * (DRF_F32: 2^23 tiles of 16); DRF_BF16: head_dim % 8 == 0, 16-byte aligned tensors, strides % 8 == 0.  token strides below 2^24.
  */
 drf_status drf_block_attention(const drf_attn_shape* shape, int q_block, int kv_block, float scale, const uint32_t* blocks,
                                const drf_heads* q, const drf_heads* k, const drf_heads* v, const drf_heads* out, void* hip_stream);

@@ -849,11 +849,11 @@ template <int P8, int QB, int W, int SH, bool SPLIT = false> drf_status launch_b
     constexpr int smem = W * (W > 1 && C::JOIN > C::WAVE ? C::JOIN : C::WAVE) + (SH > 1 ? 16 : 0);
     static_assert(smem <= 160 * 1024, "LDS of a CU");
     auto kern = block_attn_kernel<P8, QB, W, SH, SPLIT>;
-    static std::atomic<uint64_t> lds_allowed{ 0 };
-    DRF_HIP(allow_lds(reinterpret_cast<const void*>(kern), smem, lds_allowed));
     const int q_tiles = (a.nq + 32 * QB * SH - 1) / (32 * QB * SH);
     const long long items = (long long)q_tiles * a.q_heads * a.slots * (SPLIT ? a.split : 1);
     if (items > 0x1ffffffLL / (W * SH)) DRF_FAIL(DRF_ESHAPE, "too many queries");
+    static std::atomic<uint64_t> lds_allowed{ 0 };
+    DRF_HIP(allow_lds(reinterpret_cast<const void*>(kern), smem, lds_allowed));
     hipLaunchKernelGGL(kern, dim3((unsigned)items), dim3(64 * W * SH), smem, st, a, q_tiles, (int)items);
     if constexpr (SPLIT) {
         DRF_HIP(hipGetLastError());

@@ -34,3 +34,15 @@ def test_outputs_whose_rows_lie_on_one_another_are_refused(over, dtype):
         assert L.drf_qk_norm_rope(ref(cfg), ref(rc), ref(s), None, 0, ref(x), ref(x), ref(outs[0]), ref(outs[1]), None) == EINVAL
     assert attend(s, out=y) == (ESHAPE if over.get("token", 0) < 0 else EINVAL)
     assert L.drf_rope(ref(rc), dtype, 0, 64, 4, 64, None, None, 0, ref(x), ref(y), None) == 0
+
+
+def test_more_tiles_than_a_launch_has_are_refused():
+    """On the host, before a device is asked for anything."""
+    L, t = drf.lib(), heads(slot=64 * 4 * 128, token=4 * 128, head=128)
+    for q_block in (32, 64, 128):
+        for dtype, tokens in ((drf.BF16, 1 << 26), (drf.F32, 1 << 23)):
+            for head_dim in (8, 64, 72, 128):
+                s = shape(dtype=dtype, slots=1 << 7, q_tokens=tokens, head_dim=head_dim)
+                assert L.drf_block_attention(C.byref(s), q_block, 64, C.c_float(1.0), FAKE, *[C.byref(t)] * 4, None) == ESHAPE
+    for s in (shape(slots=1 << 23), shape(slots=1 << 19, q_heads=16, kv_heads=16), shape(q_tokens=1 << 30)):
+        assert L.drf_block_select(C.byref(s), 32, 64, 4, C.byref(t), C.byref(t), FAKE, 1 << 62, FAKE, None) == ESHAPE
