@@ -307,7 +307,9 @@ drf_status drf_plan_build(const drf_sched_config* sched, drf_mode mode, int n, i
  * by drf_denoiser_create_attn runs them in every block; a caller with a predictor of its own calls them
  * on its own tensors.  They allocate nothing, keep nothing between calls and need no handle; every call
  * may be captured into a HIP graph.  All arithmetic is fp32 or wider; results are rounded once, to the
- * tensors' type (the attention's probabilities are rounded to the type of the values too).
+ * tensors' type.  One thing is rounded before: the attention's probabilities, to the type of the values, for their
+ * product with them (in bf16 the sum that divides it is of the unrounded ones for a head_dim that is a multiple of 32,
+ * of the rounded ones otherwise).  None of the calls records anything for a gradient.
  */
 
 /*
@@ -335,7 +337,7 @@ typedef struct {
  * DRF_ROPE_PAIRS: x and y are columns 2i and 2i + 1 of the section; DRF_ROPE_HALVES: i and i + dim / 2.
  * Position of token n on axis a: origin[a] + step[a] * (its coordinate in the row-major grid of extent[0] x
  * extent[1] x .., the first axis slowest and not limited by its extent), or table entry [n][a] where a call gives a table.
- * Angles are formed in double precision.  Negated origins and steps turn back.
+ * Angles are formed in double precision, to within a quarter turn.  Negated origins and steps turn back.
  */
 #define DRF_ROPE_AXES 3
 typedef enum { DRF_ROPE_PAIRS = 0, DRF_ROPE_HALVES = 1 } drf_rope_layout;

@@ -112,7 +112,9 @@ template <int P8> struct Cfg {
     static constexpr int DT = TAIL ? d / 32 : (d + 31) / 32, DT1 = DT > 0 ? DT : 1;     // 32-row tiles of O^T
     static constexpr bool ONES = d % 32 != 0;                   // O^T has a padding row: it accumulates the denominator
     static constexpr int KP = P8 | 1;                           // 16-byte pieces per K row in LDS: odd, rows on different banks
-    static constexpr int VP = P8 + (P8 % 4 == 2 ? 0 : P8 % 4 == 3 ? 3 : 2 - P8 % 4);     // and per V row: the four rows of a transposing read on different banks
+    // and per V row: two modulo four, which keeps the four rows of a transposing read half apart (34 to 38 % of the LDS cycles are still conflicts, widths 72
+    // and 128; 20 pieces a row of 128 have none and are 1 - 2 % slower, for what they add to the copies)
+    static constexpr int VP = P8 + (P8 % 4 == 2 ? 0 : P8 % 4 == 3 ? 3 : 2 - P8 % 4);
     static constexpr int KI = (kStep * KP + 63) / 64, VI = (kStep * VP + 63) / 64;      // copy instructions a step
     static constexpr int KBYTES = kStep * KP * 16, BUF = KBYTES + kStep * VP * 16;
     // 16 bytes of zeros: K in the spare columns of the last k-step, V in those behind the head width but for the first, which is one: 1, 0, 0, 0
@@ -153,7 +155,7 @@ __device__ inline float max3(float a, float b, float c) { return __builtin_eleme
 // Bound by the matrix instructions and, beside them, the exponentials and the way of K and V into LDS: 4 slots x 16384 queries x 12 heads of 128
 // over 16 of 128 blocks of 128, 825 GFLOP, 0.89 ms, 0.93 PFLOP/s (a large library product reaches 1.23 here, the instruction by itself 1.94; by
 // waves of their own 0.94 ms, of which the copies were 0.2 and their waits nothing).  6 x 4096 x 16 of 72 over 8 of 64 blocks of 64, 58 GFLOP over
-// 226 MB of q, k, v and result, 82 us, 97 with nothing of them in the caches: half of it is that read.
+// 226 MB of q, k, v and result, 83 us, 97 with nothing of them in the caches: 24 us and 7.4 a block (1 block 34, 2 43, 4 54, 16 143, 32 263).
 template <int P8, int QB, int W, int SH, bool SPLIT>
 __global__ void __launch_bounds__(64 * W * SH, P8 > 11 && QB == 2 ? 1 : 2) block_attn_kernel(const BlockArgs a, int q_tiles, int n_items)
 {
@@ -386,7 +388,10 @@ __global__ void __launch_bounds__(64 * W * SH, P8 > 11 && QB == 2 ? 1 : 2) block
             }
         }
     };
-    // P of block b.  LAZY takes the difference first, which is exact where it matters, whatever the scores' size (0.2 us of a query's 10.3 over 1024 keys; by a
+    // P of block b, rounded to bf16 for the matrix instruction (its fp32 form has a sixteenth of the rate): half a step of a weight at most, which takes
+    // the error of a result from 0.0017 of its size, what its own rounding leaves, to 0.0018.  The denominator sums the weights before that rounding
+    // where the head width is a multiple of 32, and in the matrix instruction, after it, where O^T has a row to spare.
+    // LAZY takes the difference first, which is exact where it matters, whatever the scores' size (0.2 us of a query's 10.3 over 1024 keys; by a
     // branch for large references alone 0.3); otherwise one instruction does, and what the reference's rounding to an exponent of two leaves (2^-24 of it) is
     // common to a query's weights.
     auto soft = [&](auto lazy_c, int b) {
@@ -864,8 +869,9 @@ template <int P8, int QB, int W, int SH, bool SPLIT = false> drf_status launch_b
 }
 
 // Workgroups to a tile of 32 queries: where the tiles leave most CUs idle and the keys are many, since one CU's way to memory (some 43 bytes a ns) then
-// bounds the call.  1 query x 16 heads of 72, 8192 keys in blocks of 64, against a workgroup to a head, us: 128 blocks chosen 20.7 : 55.0, 64 15.9 : 29.8,
-// 32 12.7 : 16.7, 16 11.5 : 10.3, 4 11.3 : 5.6 (the second launch and the parts).  How many are chosen only the caller knows: who gives scratch wants it.
+// bounds the call.  1 query x 16 heads of 72, 8192 keys in blocks of 64, against a workgroup to a head, us: 128 blocks chosen 21.7 : 55.9, 64 15.5 : 30.0,
+// 32 12.9 : 17.0, 16 11.6 : 10.5, 4 11.4 : 5.7 (the second launch and the parts).  How many are chosen only the caller knows: who gives scratch wants it.
+// The rule sees the tokens alone, and below 8192 of them nothing has been measured.
 int split_of(const drf_attn_shape& s)
 {
     if (s.dtype != DRF_BF16) return 1;

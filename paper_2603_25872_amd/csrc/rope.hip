@@ -89,7 +89,7 @@ enum { ROPE_NO = 0, ROPE_IN_LANE = 1, ROPE_PIECE = 2, ROPE_HALF_PIECE = 3, ROPE_
 // A row (one head of one token) is P = d / E pieces of 16 bytes, one a lane, and a wave takes 64 / P tokens, so that all but the last few lanes
 // work at any head width, and U heads of them at a time.  NORM: a drf_qk_norm.  Bound by memory: 4 slots x 16384 tokens x 16 heads of 72 in bf16
 // turned, 302 MB, 68.5 us (4.4 TB/s, where a copy of 1 GiB reaches 5.05); q and k of 6 x 4096 x 16 of 72 with RMS norms, 226 MB, 53 us (4.3); the sums of
-// four heads are formed beside one another (83 us with a head's shuffles behind the last one's).  One token: 3.7 us, a launch and three dependent reads.
+// four heads are formed beside one another (83 us with a head's shuffles behind the last one's).  One token: 3.9 us, a launch and three dependent reads.
 constexpr int kHeads = 4;
 template <typename T, int NORM, int ROPE>
 __global__ void __launch_bounds__(kThreads) heads_kernel(const HeadsArgs a)

@@ -294,6 +294,7 @@ def refine_step(sched, x, eps, s_from, out=None):
 
 
 # ---- attention operators: what _native does, where that module is not there ----
+# (Like every call of this module they work on the tensors' memory and are unknown to autograd: results require no gradient.)
 
 def _heads(t, like=None, same=False):
     """(drf_heads, dtype, shape) of a device tensor [slots, tokens, heads, head_dim] whose head columns are contiguous."""
@@ -427,7 +428,8 @@ def rope_config(dims, extents, theta=10000.0, layout="pairs", origin=None, step=
 
 def rope(x, config, positions=None, lens=None, out=None):
     """x [slots, tokens, heads, head_dim] (any strides but the last) with its columns turned by their positions; out may be x.  Rows behind a
-    slot's length are left as they were: those of x in an output made here."""
+    slot's length are left as they were: those of x in an output made here.  No gradient is recorded; that of x is the result's, turned back by the
+    rotation with origin and step negated."""
     import torch
     if out is None:
         out = torch.empty_like(x) if lens is None else x.clone()
@@ -438,7 +440,7 @@ def rope(x, config, positions=None, lens=None, out=None):
 def qk_norm_rope(q, k, norm, config=None, q_gain=None, k_gain=None, q_bias=None, k_bias=None, eps=1e-6, q_scale=1.0, positions=None, lens=None,
                  q_out=None, k_out=None):
     """Norm ("none", "rms", "layer") of every head of q and k [slots, tokens, heads, head_dim], then the rotation; returns (q_out, k_out).  Outputs may
-    be their inputs; rows behind a slot's length as in rope()."""
+    be their inputs; rows behind a slot's length as in rope().  No gradient is recorded."""
     import torch
     if q_out is None:
         q_out = torch.empty_like(q) if lens is None else q.clone()
@@ -464,7 +466,7 @@ def block_select(q, k, q_block, kv_block, topk, q_lens=None, kv_lens=None, out=N
 
 def block_attention(q, k, v, blocks, q_block, kv_block, scale=None, q_lens=None, kv_lens=None, out=None, split=False):
     """softmax(scale q k^T) v over the key blocks that the words `blocks` (as block_select gives them) name for each query block; scale
-    1 / sqrt(head_dim) by default.  Rows behind a slot's q length are left as they were: zeros in an output made here.  split: several workgroups
+    1 / sqrt(head_dim) by default.  No gradient is recorded.  Rows behind a slot's q length are left as they were: zeros in an output made here.  split: several workgroups
     share a head where its queries are few and its keys many (for lists from about 1500 keys on, in bf16 over 8192 tokens or more; other calls are as without)."""
     import torch
     if out is None:
