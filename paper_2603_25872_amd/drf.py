@@ -432,7 +432,7 @@ def rope(x, config, positions=None, lens=None, out=None):
     rotation with origin and step negated."""
     import torch
     if out is None:
-        out = torch.empty_like(x) if lens is None else x.clone()
+        out = torch.empty_like(x) if lens is None else x.detach().clone()
     _check((_ops or _operators()).rope(x, out, C.addressof(config), positions, lens))
     return out
 
@@ -443,9 +443,9 @@ def qk_norm_rope(q, k, norm, config=None, q_gain=None, k_gain=None, q_bias=None,
     be their inputs; rows behind a slot's length as in rope().  No gradient is recorded."""
     import torch
     if q_out is None:
-        q_out = torch.empty_like(q) if lens is None else q.clone()
+        q_out = torch.empty_like(q) if lens is None else q.detach().clone()
     if k_out is None:
-        k_out = torch.empty_like(k) if lens is None else k.clone()
+        k_out = torch.empty_like(k) if lens is None else k.detach().clone()
     _check((_ops or _operators()).qk_norm_rope(q, k, q_out, k_out, _QK[norm], float(eps), float(q_scale), q_gain, q_bias, k_gain, k_bias,
                                                None if config is None else C.addressof(config), positions, lens))
     return q_out, k_out

@@ -299,3 +299,14 @@ def test_expanded_inputs_and_outputs(torch, drf, dtype):
                      lambda: drf.block_attention(whole, whole, whole, words, 32, 32, out=wide)):
             with pytest.raises(drf.DrfError):
                 call()
+
+
+def test_results_are_unknown_to_autograd(torch, drf):
+    """Of inputs that require gradients too: no result carries a gradient that is not the operator's."""
+    x = torch.randn(2, 40, 2, 64, device="cuda", requires_grad=True)
+    lens, cfg = torch.tensor([40, 7], dtype=torch.int32, device="cuda"), drf.rope_config((32, 32), (1, 9))
+    for n in (None, lens):
+        words = drf.block_select(x, x, 32, 32, 1, q_lens=n, kv_lens=n)
+        out = [drf.rope(x, cfg, lens=n), *drf.qk_norm_rope(x, x, "rms", cfg, lens=n), drf.block_attention(x, x, x, words, 32, 32, q_lens=n, kv_lens=n)]
+        assert not any(t.requires_grad for t in out)
+        assert torch.equal(out[0], drf.rope(x.detach(), cfg, lens=n))
