@@ -356,7 +356,8 @@ typedef struct {
  *   positions   DEVICE fp32 or NULL: element (slot s, token n, axis a) at positions[s * positions_slot_stride +
  *               n * n_axes + a] (stride 0: one table for all slots); replaces the grid, origin and step
  *   out         may be x itself (the same address and strides); otherwise the two do not overlap
- * head_dim <= 128, heads <= 65535, tokens <= 2^30, and fewer than 2^31 workgroups (of some 4 KB of x or more each).  16-byte aligned tensors whose strides and head_dim are multiples of 16 bytes take 16-byte
+ * head_dim <= 128, heads <= 65535, tokens <= 2^30, and fewer than 2^31 workgroups (of some 4 KB of x or more each).
+ * 16-byte aligned tensors whose strides and head_dim are multiples of 16 bytes take 16-byte
  * accesses; all others one element at a time.
  */
 drf_status drf_rope(const drf_rope_config* rope, drf_dtype dtype, int slots, int tokens, int heads, int head_dim,
@@ -393,7 +394,8 @@ drf_status drf_qk_norm_rope(const drf_qk_config* cfg, const drf_rope_config* rop
  *            bit j % 32 of word j / 32 of row i: query block i attends to key block j.  A query block with no query
  *            inside its slot's length has none.
  *   scratch  DEVICE, 16-byte aligned, drf_block_select_scratch_bytes() bytes of any content
- * head_dim <= 128, at most 1024 key blocks, slots * (query blocks + key blocks) < 2^23 and slots * q_heads * ceil(query blocks / 16) < 2^21.  drf_block_words and .._scratch_bytes give 0 for sizes that are refused.
+ * head_dim <= 128, at most 1024 key blocks, slots * (query blocks + key blocks) < 2^23 and slots * q_heads *
+ * ceil(query blocks / 16) < 2^21.  drf_block_words and .._scratch_bytes give 0 for block sizes, types and head_dims that are refused.
  */
 size_t drf_block_words(int kv_tokens, int kv_block);
 size_t drf_block_select_scratch_bytes(const drf_attn_shape* shape, int q_block, int kv_block);
