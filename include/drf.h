@@ -369,7 +369,7 @@ drf_status drf_rope(const drf_rope_config* rope, drf_dtype dtype, int slots, int
  *   DRF_QK_RMS     y = x / sqrt(mean(x^2) + eps) * gain
  *   DRF_QK_LAYER   y = (x - mean(x)) / sqrt(var(x) + eps) * gain + bias
  *   DRF_QK_NONE    y = x                                             (gains and biases NULL)
- * and the queries times q_scale (a softmax scale, or 1).  Gains and biases: DEVICE fp32 [head_dim], or NULL:
+ * (squares and their sum in fp32: values up to 1e18) and the queries times q_scale (a softmax scale, or 1).  Gains and biases: DEVICE fp32 [head_dim], or NULL:
  * ones and zeros; biases only with DRF_QK_LAYER.  q and k have the same tokens (shape->kv_tokens == q_tokens) and lengths
  * (shape->q_lens; kv_lens is NULL or the same address).  q_out may be q itself, k_out k itself; otherwise as in drf_rope.
  */

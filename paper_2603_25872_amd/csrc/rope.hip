@@ -8,6 +8,7 @@
 // zero, so that an infinity in it, or in a column beside it, stays where it is.  The angles of a workgroup's tokens are formed once, by all its threads
 // (in double precision: a position far from zero keeps its fraction of a turn), while the first heads are on their way.  What is left is a copy
 // with a sum over a head's columns and two multiply-adds a column: bound by memory.
+#include <algorithm>
 #include <type_traits>
 
 #include "common.h"
@@ -481,6 +482,7 @@ extern "C" drf_status drf_qk_norm_rope(const drf_qk_config* cfg, const drf_rope_
     if ((rc = fill_side("k", k, k_out, s.slots, s.kv_tokens, s.kv_heads, s.head_dim, &vec, unit, &a.k)) != DRF_OK) return rc;
     a.q.scale = cfg->q_scale; a.k.scale = 1.f;
     a.q.gain = cfg->q_gain; a.q.bias = cfg->q_bias; a.k.gain = cfg->k_gain; a.k.bias = cfg->k_bias;
-    a.slots = s.slots; a.tokens = s.q_tokens; a.d = s.head_dim; a.lens = s.q_lens; a.eps = (float)cfg->eps;
+    a.slots = s.slots; a.tokens = s.q_tokens; a.d = s.head_dim; a.lens = s.q_lens;
+    a.eps = cfg->eps > 0.0 ? std::max((float)cfg->eps, 1.17549435e-38f) : 0.f;     // (one that fp32 does not hold is still no zero: a row of zeros stays one)
     return run_heads(a, rope, s.dtype, cfg->norm, vec, (hipStream_t)hip_stream);
 }

@@ -310,3 +310,20 @@ def test_results_are_unknown_to_autograd(torch, drf):
         out = [drf.rope(x, cfg, lens=n), *drf.qk_norm_rope(x, x, "rms", cfg, lens=n), drf.block_attention(x, x, x, words, 32, 32, q_lens=n, kv_lens=n)]
         assert not any(t.requires_grad for t in out)
         assert torch.equal(out[0], drf.rope(x.detach(), cfg, lens=n))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("layout", ["plain", "odd"])
+@pytest.mark.parametrize("eps", [1e-300, 1e-46, 1e-30, 1e30])
+def test_norms_of_rows_of_zeros(torch, drf, dtype, layout, eps):
+    """Zeros over the root of any eps above zero are zeros, biases stay; the rows beside them are what they are."""
+    rng = np.random.default_rng(12)
+    x, v = ops.tensor(torch, rng, (1, 9, 3, 40), dtype, layout)
+    x[:, ::2] = 0.0
+    v[:, ::2] = 0.0
+    bias = rng.uniform(-1, 1, 40).astype(np.float32)
+    for norm, b in (("rms", None), ("layer", bias)):
+        want = ops.normed(v, norm, None, b, eps)
+        dev = None if b is None else torch.from_numpy(b).cuda()
+        for got in drf.qk_norm_rope(x, x, norm, q_bias=dev, k_bias=dev, eps=eps):
+            ops.check(got, want, dtype, 2.0 ** -19 * np.abs(want).max())
