@@ -448,6 +448,89 @@ size_t drf_denoiser_weight_count_attn(const drf_dit_config* cfg, const drf_attn_
 drf_status drf_denoiser_create_attn(const drf_dit_config* cfg, const drf_attn_config* attn, const float* host_weights, size_t count,
                                     void* hip_stream, drf_denoiser** out);
 
+/* ---- operators around the Linears of a block -------------------------------------------------------
+ * The rest of a transformer denoiser's block beside its attention: the update of the residual stream with the norms before and after it,
+ * the gated feed-forward block, and a projection that many requests share while each has a low-rank adapter of its own.  As above: nothing is
+ * allocated, kept between calls or recorded for a gradient, every call may be captured into a HIP graph, sums are fp32 and results are rounded once, to
+ * their tensors' type.  A scratch buffer may be of any content and belongs to one call at a time.  slots * tokens and tokens <= 2^30.
+ */
+
+/*
+ * A tensor [slots][tokens][columns], DEVICE: element (s, n, c) at data + s * slot_stride + n * token_stride + c, strides in elements.  Strides of a
+ * dimension of one element, strides of zero and outputs whose rows lie on one another as in drf_heads.
+ */
+typedef struct { void* data; int64_t slot_stride, token_stride; } drf_rows;
+
+/*
+ * z = x_scale x + y_scale gate * after(y),  h = before(z) (1 + scale) + shift: what follows one branch of a block and precedes the next.
+ *   after, before   norms of a row, as in drf_qk_norm_rope over `width` columns; gains and biases DEVICE fp32 [width] or NULL
+ *   gate, shift, scale   fp32, rows of a slot (token_stride 0) or of every token; data NULL: 1, 0 and 0
+ *   x, out          of type stream; y, h of type branch (DRF_BF16 with a DRF_BF16 stream)
+ *   out NULL: z is not stored.  h NULL: no h.  y NULL: z = x_scale x, and out has to be NULL; after, gate and y_scale are not looked at.
+ * h is formed from z as it is before its rounding to the stream's type.  Norms add their squares in fp32: values up to 1e18.  Rows behind a slot's
+ * length (lens, DEVICE int32 [slots] or NULL) are neither read nor written.  out may be x itself and h y itself (address and strides), otherwise
+ * no output overlaps another tensor.  1 <= width <= 16384.  16-byte aligned tensors whose strides and width are multiples of 16
+ * bytes take 16-byte accesses; all others one element at a time.
+ */
+typedef struct {
+    drf_qk_norm norm;
+    double eps;                     /* >= 0 */
+    const float *gain, *bias;
+} drf_row_norm;
+typedef struct {
+    drf_dtype stream, branch;
+    int slots, tokens, width;
+    const int32_t* lens;
+    float x_scale, y_scale;         /* finite */
+    drf_row_norm after, before;
+    drf_rows gate, shift, scale;
+} drf_residual_config;
+drf_status drf_residual_norm(const drf_residual_config* cfg, const drf_rows* x, const drf_rows* y, const drf_rows* out, const drf_rows* h,
+                             void* hip_stream);
+
+/*
+ * out = (act(x Wg^T + bg) * (x Wv^T + bv)) Wo^T + bo: the gated feed-forward block.
+ *   w_in    DEVICE [2 hidden][width]: the rows of Wg, then those of Wv; b_in fp32 [2 hidden] (bg, then bv) or NULL
+ *   w_out   DEVICE [out_width][hidden]; b_out fp32 [out_width] or NULL
+ *   act     DRF_GLU_SILU a / (1 + e^-a) | DRF_GLU_GELU the tanh form of the DiT above
+ *   scratch DEVICE, 16-byte aligned, drf_gated_ffn_scratch_bytes() bytes
+ * x, the weights and out are of one type.  DRF_BF16: the product of act and value is rounded to bf16, the operand type of the second product; x and weights
+ * 16-byte aligned, width and hidden % 8 == 0, strides of x % 8 == 0; out: any.  DRF_F32: any sizes and alignment.  Strides of x and out >= 0, token strides below
+ * 2^22; width, hidden and out_width <= 2^20.  Rows behind a slot's length are left as they were.  out overlaps no input.
+ * .._scratch_bytes gives 0 for sizes that are refused and where there is nothing to do.
+ */
+typedef enum { DRF_GLU_SILU = 0, DRF_GLU_GELU = 1 } drf_glu;
+typedef struct {
+    drf_dtype dtype;
+    drf_glu act;
+    int slots, tokens, width, hidden, out_width;
+    const int32_t* lens;
+    const void *w_in, *w_out;
+    const float *b_in, *b_out;
+} drf_gated_ffn_config;
+size_t drf_gated_ffn_scratch_bytes(const drf_gated_ffn_config* cfg);
+drf_status drf_gated_ffn(const drf_gated_ffn_config* cfg, const drf_rows* x, const drf_rows* out, void* scratch, size_t scratch_bytes, void* hip_stream);
+
+/*
+ * out = x W^T + bias + scales[i] (x A_i^T) B_i^T with i = which[slot]: a Linear that all slots share, and a low-rank adapter of each slot's own.
+ *   w       DEVICE [out_width][width]; bias fp32 [out_width] or NULL
+ *   a, b    DEVICE [adapters][rank][width] and [adapters][out_width][rank]; scales fp32 [adapters] or NULL: ones
+ *   which   DEVICE int32 [slots]; an index below 0 or from `adapters` on: the slot has none
+ *   scratch DEVICE, 16-byte aligned, drf_linear_adapters_scratch_bytes() bytes
+ * x A^T is kept in fp32, in DRF_BF16 as the sum of two bf16 operands (16 bits of it).  Types, alignment, strides, lengths and sizes as in drf_gated_ffn;
+ * w and a 16-byte aligned and width % 8 == 0 in DRF_BF16, b, rank and out_width any; 1 <= rank <= 256, adapters >= 0 (0: a and b may be NULL).
+ */
+typedef struct {
+    drf_dtype dtype;
+    int slots, tokens, width, out_width, rank, adapters;
+    const int32_t *lens, *which;
+    const void *w, *a, *b;
+    const float *bias, *scales;
+} drf_adapters_config;
+size_t drf_linear_adapters_scratch_bytes(const drf_adapters_config* cfg);
+drf_status drf_linear_adapters(const drf_adapters_config* cfg, const drf_rows* x, const drf_rows* out, void* scratch, size_t scratch_bytes,
+                               void* hip_stream);
+
 /* HOST, thread-local, valid until the next failing call on this thread. */
 const char* drf_last_error(void);
 

@@ -22,6 +22,8 @@ DDIM, DDPM, EULER = 0, 1, 2
 ROPE_PAIRS, ROPE_HALVES = 0, 1
 QK_NONE, QK_RMS, QK_LAYER = 0, 1, 2
 _QK = {"none": QK_NONE, "rms": QK_RMS, "layer": QK_LAYER}
+GLU_SILU, GLU_GELU = 0, 1
+_GLU = {"silu": GLU_SILU, "gelu": GLU_GELU}
 _LAYOUTS = {"pairs": ROPE_PAIRS, "halves": ROPE_HALVES}
 
 # include/drf.h: the method's calls
@@ -30,7 +32,8 @@ SYMBOLS = ["drf_denoiser_weight_count", "drf_denoiser_create", "drf_denoiser_des
            "drf_skip_transition_noise", "drf_normal_fill", "drf_sample_noise", "drf_noise_count",
            "drf_plan_build", "drf_last_error",
            "drf_rope", "drf_qk_norm_rope", "drf_block_words", "drf_block_select_scratch_bytes", "drf_block_select", "drf_block_attention", "drf_block_attention_scratch_bytes", "drf_block_attention_split",
-           "drf_denoiser_weight_count_attn", "drf_denoiser_create_attn"]
+           "drf_denoiser_weight_count_attn", "drf_denoiser_create_attn",
+           "drf_residual_norm", "drf_gated_ffn_scratch_bytes", "drf_gated_ffn", "drf_linear_adapters_scratch_bytes", "drf_linear_adapters"]
 # include/drf_measure.h: test and measurement hooks
 MEASURE_SYMBOLS = ["drf_eps_trace", "drf_profile_enable", "drf_profile_read", "drf_probe_gemm_bf16",
                    "drf_probe_attn_bf16", "drf_probe_cross_attn_bf16", "drf_probe_attn_route", "drf_probe_gemm_route", "drf_probe_block_route", "drf_probe_update_fused", "drf_graph_stats", "drf_calibrate_mfma_bf16", "drf_calibrate_copy"]
@@ -72,6 +75,29 @@ class QkConfig(C.Structure):
 class AttnConfig(C.Structure):
     _fields_ = [("qk_norm", C.c_int), ("norm_eps", C.c_double), ("rope_dim", C.c_int * 2), ("rope_theta", C.c_double), ("rope_layout", C.c_int),
                 ("additive_pos", C.c_int), ("q_block", C.c_int), ("kv_block", C.c_int), ("topk", C.c_int)]
+
+
+class Rows(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("slot_stride", C.c_int64), ("token_stride", C.c_int64)]
+
+
+class RowNorm(C.Structure):
+    _fields_ = [("norm", C.c_int), ("eps", C.c_double), ("gain", C.c_void_p), ("bias", C.c_void_p)]
+
+
+class ResidualConfig(C.Structure):
+    _fields_ = [(k, C.c_int) for k in ("stream", "branch", "slots", "tokens", "width")] + [
+        ("lens", C.c_void_p), ("x_scale", C.c_float), ("y_scale", C.c_float), ("after", RowNorm), ("before", RowNorm), ("gate", Rows), ("shift", Rows), ("scale", Rows)]
+
+
+class GatedFfnConfig(C.Structure):
+    _fields_ = [(k, C.c_int) for k in ("dtype", "act", "slots", "tokens", "width", "hidden", "out_width")] + [
+        (k, C.c_void_p) for k in ("lens", "w_in", "w_out", "b_in", "b_out")]
+
+
+class AdaptersConfig(C.Structure):
+    _fields_ = [(k, C.c_int) for k in ("dtype", "slots", "tokens", "width", "out_width", "rank", "adapters")] + [
+        (k, C.c_void_p) for k in ("lens", "which", "w", "a", "b", "bias", "scales")]
 
 
 class DrfError(RuntimeError):
@@ -143,6 +169,10 @@ def lib():
         L.drf_block_attention_scratch_bytes.argtypes = [C.c_void_p]
         L.drf_block_attention_scratch_bytes.restype = C.c_size_t
         L.drf_block_attention_split.argtypes = [C.c_void_p, C.c_int, C.c_int, C.c_float] + [C.c_void_p] * 6 + [C.c_size_t, C.c_void_p]
+        L.drf_residual_norm.argtypes = [C.c_void_p] * 6
+        L.drf_gated_ffn_scratch_bytes.restype = L.drf_linear_adapters_scratch_bytes.restype = C.c_size_t
+        L.drf_gated_ffn_scratch_bytes.argtypes = L.drf_linear_adapters_scratch_bytes.argtypes = [C.c_void_p]
+        L.drf_gated_ffn.argtypes = L.drf_linear_adapters.argtypes = [C.c_void_p] * 4 + [C.c_size_t, C.c_void_p]
         try:
             from . import _native               # built beside the library
             _native.bind(C.cast(L.drf_skip_transition_noise, C.c_void_p).value)
@@ -395,6 +425,47 @@ class _OperatorsCtypes:
                                               _vector(scratch, torch.float32, n // 4, q, "scratch"), n, _current(q))
 
 
+def _rows(t, like=None, shape=None, dtype=None):
+    """drf_rows of a device tensor [slots, tokens, columns] whose columns are contiguous."""
+    import torch
+    assert t.is_cuda and t.dim() == 3, "need a device tensor [slots, tokens, columns]"
+    ss, ts, cs = t.stride()
+    assert cs == 1 or t.shape[2] < 2, "a row's columns must be contiguous"
+    assert t.dtype in (torch.bfloat16, torch.float32), "expected bfloat16 or float32"
+    assert max(t.shape) < 2 ** 31, "a size that does not fit 32 bits"
+    if like is not None:
+        assert t.device == like.device, "tensors on two devices"
+    assert dtype is None or t.dtype == dtype, "tensors of two types"
+    assert shape is None or tuple(t.shape) == tuple(shape), "expected a tensor of shape %s" % (tuple(shape),)
+    return Rows(t.data_ptr(), ss, ts)
+
+
+def _modulation(t, x, what):
+    """drf_rows of fp32 rows [slots, columns] or [slots, tokens, columns] for x, or of none."""
+    import torch
+    if t is None:
+        return Rows(None, 0, 0)
+    assert t.is_cuda and t.dtype == torch.float32, "%s: need a float32 device tensor" % what
+    assert t.device == x.device, "tensors on two devices"
+    S, N, D = x.shape
+    assert tuple(t.shape) in ((S, D), (S, N, D)), "%s must be [slots, columns] or [slots, tokens, columns]" % what
+    assert t.stride(-1) == 1 or D < 2, "a row's columns must be contiguous"
+    return Rows(t.data_ptr(), t.stride(0), t.stride(1) if t.dim() == 3 else 0)
+
+
+def _weights(t, x, shape, what):
+    """Device pointer of contiguous weights of x's type."""
+    assert tuple(t.shape) == tuple(shape), "%s must be %s" % (what, tuple(shape))
+    p = _dev(t, x.dtype)
+    assert t.device == x.device, "tensors on two devices"
+    return p
+
+
+def _dtype_of(t):
+    import torch
+    return BF16 if t.dtype == torch.bfloat16 else F32
+
+
 _ops = None             # _native or _OperatorsCtypes, at the first operator
 
 
@@ -477,6 +548,81 @@ def block_attention(q, k, v, blocks, q_block, kv_block, scale=None, q_lens=None,
         n = _lib.drf_block_attention_scratch_bytes(C.byref(shape))
         scratch = torch.empty(n // 4, dtype=torch.float32, device=q.device) if n else None
     _check(ops.block_attention(q, k, v, blocks, out, q_block, kv_block, q.shape[3] ** -0.5 if scale is None else scale, q_lens, kv_lens, scratch))
+    return out
+
+
+# ---- operators around the Linears of a block ----
+
+
+def residual_norm(x, y=None, gate=None, after="none", after_gain=None, after_bias=None, x_scale=1.0, y_scale=1.0, before="layer", before_gain=None, before_bias=None,
+                  shift=None, scale=None, eps=1e-6, lens=None, out=None, h_out=None):
+    """The step between two branches of a block: z = x_scale x + y_scale gate * after(y), h = before(z) (1 + scale) + shift; returns (z, h).
+    x [slots, tokens, columns] the residual stream, y the branch's output (None: z = x_scale x is not stored, and x returned for it); norms "none", "rms", "layer",
+    before None: no h.  gate, shift, scale: fp32 [slots, columns] or [slots, tokens, columns].  h is of y's type (x's without y).  out may be x, h_out y.
+    Rows behind a slot's length are left as they were: those of x in a z made here, zeros in an h.  No gradient is recorded."""
+    import torch
+    L = _lib or lib()
+    rx, D = _rows(x), x.shape[2]
+    like = x if y is None else y
+    assert y is not None or out is None, "a stream is stored where a branch is added to it"
+    assert before is not None or h_out is None, "an output for a norm that is not asked for"
+    if y is not None and out is None:
+        out = torch.empty_like(x) if lens is None else x.detach().clone()
+    if before is not None and h_out is None:
+        h_out = (torch.empty if lens is None else torch.zeros)(x.shape, dtype=like.dtype, device=x.device)
+    ry = None if y is None else _rows(y, x, x.shape)
+    ro = None if y is None else _rows(out, x, x.shape, x.dtype)
+    rh = None if before is None else _rows(h_out, x, x.shape, like.dtype if y is not None else None)
+    vec = lambda t: _vector(t, torch.float32, D, x, "a norm's parameters")  # noqa: E731
+    cfg = ResidualConfig(_dtype_of(x), _dtype_of(h_out if y is None else y), *x.shape, _vector(lens, torch.int32, x.shape[0], x, "lens"), float(x_scale), float(y_scale),
+                         RowNorm(_QK[after], float(eps), vec(after_gain), vec(after_bias)), RowNorm(_QK[before or "none"], float(eps), vec(before_gain), vec(before_bias)),
+                         _modulation(gate, x, "gate"), _modulation(shift, x, "shift"), _modulation(scale, x, "scale"))
+    ref = lambda r: None if r is None else C.byref(r)  # noqa: E731
+    _check(L.drf_residual_norm(C.byref(cfg), C.byref(rx), ref(ry), ref(ro), ref(rh), _current(x)))
+    return (x if y is None else out), h_out
+
+
+def gated_ffn(x, w_in, w_out, b_in=None, b_out=None, act="silu", lens=None, out=None):
+    """(act(x Wg^T + bg) * (x Wv^T + bv)) Wo^T + bo of x [slots, tokens, columns]: w_in [2 hidden, columns] holds Wg's rows and then Wv's, w_out is
+    [out columns, hidden], biases fp32; act "silu" or "gelu" (the tanh form).  Rows behind a slot's length are left as they were: zeros in an output made here.  No
+    gradient is recorded."""
+    import torch
+    L = _lib or lib()
+    rx = _rows(x)
+    S, N, D = x.shape
+    assert w_in.dim() == 2 and w_out.dim() == 2 and w_in.shape[0] == 2 * w_out.shape[1], "w_in must have twice the rows that w_out has columns"
+    O, F = w_out.shape
+    if out is None:
+        out = (torch.empty if lens is None else torch.zeros)((S, N, O), dtype=x.dtype, device=x.device)
+    ro = _rows(out, x, (S, N, O), x.dtype)
+    cfg = GatedFfnConfig(_dtype_of(x), _GLU[act], S, N, D, F, O, _vector(lens, torch.int32, S, x, "lens"), _weights(w_in, x, (2 * F, D), "w_in"),
+                         _weights(w_out, x, (O, F), "w_out"), _vector(b_in, torch.float32, 2 * F, x, "b_in"), _vector(b_out, torch.float32, O, x, "b_out"))
+    n = L.drf_gated_ffn_scratch_bytes(C.byref(cfg))
+    scratch = torch.empty(n, dtype=torch.uint8, device=x.device)
+    _check(L.drf_gated_ffn(C.byref(cfg), C.byref(rx), C.byref(ro), scratch.data_ptr(), n, _current(x)))
+    return out
+
+
+def linear_adapters(x, w, a, b, which, bias=None, scales=None, lens=None, out=None):
+    """x W^T + bias + scales[i] (x A_i^T) B_i^T, i = which[slot], of x [slots, tokens, columns]: w [out columns, columns] for all slots, a [adapters, rank, columns]
+    and b [adapters, out columns, rank], which int32 [slots] (an index outside of the adapters: none), bias and scales fp32.  Rows behind a slot's length are left as
+    they were: zeros in an output made here.  No gradient is recorded."""
+    import torch
+    L = _lib or lib()
+    rx = _rows(x)
+    S, N, D = x.shape
+    assert w.dim() == 2 and a.dim() == 3, "need w [out columns, columns] and a [adapters, rank, columns]"
+    O, (n_ad, R) = w.shape[0], a.shape[:2]
+    if out is None:
+        out = (torch.empty if lens is None else torch.zeros)((S, N, O), dtype=x.dtype, device=x.device)
+    ro = _rows(out, x, (S, N, O), x.dtype)
+    assert which is not None, "which must have %d elements" % S
+    cfg = AdaptersConfig(_dtype_of(x), S, N, D, O, R, n_ad, _vector(lens, torch.int32, S, x, "lens"), _vector(which, torch.int32, S, x, "which"),
+                         _weights(w, x, (O, D), "w"), _weights(a, x, (n_ad, R, D), "a"), _weights(b, x, (n_ad, O, R), "b"),
+                         _vector(bias, torch.float32, O, x, "bias"), _vector(scales, torch.float32, n_ad, x, "scales"))
+    n = L.drf_linear_adapters_scratch_bytes(C.byref(cfg))
+    scratch = torch.empty(n, dtype=torch.uint8, device=x.device) if n else None
+    _check(L.drf_linear_adapters(C.byref(cfg), C.byref(rx), C.byref(ro), None if scratch is None else scratch.data_ptr(), n, _current(x)))
     return out
 
 
