@@ -1,0 +1,179 @@
+// Device code and arguments shared by the kernels of the Linears around a block (linear.hip, linear_tile.h).
+#pragma once
+#include <algorithm>
+#include <type_traits>
+
+#include "gemm_device.h"
+#include "rows.h"
+
+namespace drf {
+
+enum { LIN_STORE = 0, LIN_GLU = 1, LIN_ADAPT = 2 };
+
+struct LinArgs {
+    drf_rows x, out;
+    const void* w;                      // [N][K]; LIN_GLU: [2 N][K], gates and then values
+    const float* bias;                  // [N] (LIN_GLU: [2 N]) or NULL
+    const int32_t* lens;
+    int slots, tokens, N, K;
+    uint32_t tok_magic; int tok_shift;
+    int slot_rows;                      // rows that are counted together: tokens (tiles do not cross slots) or slots * tokens
+    int tiles_m, tiles_n;               // tiles of all rows; tiles of columns
+    int slot_tiles;                     // tiles of rows that are counted together
+    long long first, tiles;             // tile that this launch begins with; all of them
+    int act, out_vec, in_vec;
+    // adapters
+    const int32_t* which;
+    const float* scales;
+    const void* a;                      // [adapters][rank][K]
+    const void* b;                      // [adapters][N][rank]
+    void* low;                          // x A^T of every row, scaled: fp32 [rank]; for bf16 operands [2][low_cols], upper and lower 8 bits, zeros from rank on
+    int adapters, rank, low_cols, b_vec;
+    int in_loop;                        // bf16: tiles keep to a slot and B's rows are 16-byte pieces, the adapter is steps of the product's loop
+};
+
+namespace {
+
+__device__ inline float glu(float a, float v, int act)
+{
+    if (act == DRF_GLU_GELU) return gelu_tanh(a) * v;
+    return a * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-1.4426950408889634f * a)) * v;
+}
+
+__device__ inline int adapter_of(const LinArgs& a, int slot)
+{
+    const int i = a.adapters ? a.which[slot] : -1;
+    return i >= 0 && i < a.adapters ? i : -1;
+}
+
+// Row m of the rows that are counted together, of group `group` of them: its slot and token; false where it is not there or behind its slot's length.
+__device__ inline bool locate_row(const LinArgs& a, int group, int m, int& slot, int& token)
+{
+    if (a.slot_rows == a.tokens) { slot = group; token = m; }
+    else { slot = fast_div(m, a.tok_magic, a.tok_shift); token = m - slot * a.tokens; }
+    return m < a.slot_rows && token < slot_len(a.lens, slot, a.tokens);
+}
+
+typedef bf16_t bf16x8 __attribute__((ext_vector_type(8)));
+__device__ inline f32x4 mma_bf16(const u32x4& w, const u32x4& x, const f32x4& c)
+{
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w), __builtin_bit_cast(bf16x8, x), c, 0, 0, 0);
+}
+
+// 16 bytes of a row of n elements from element k on, zeros behind its end
+template <typename T> __device__ inline u32x4 load16(const T* row, int k, int n, bool vec)
+{
+    constexpr int E = 16 / sizeof(T);
+    if (vec) return k < n ? *reinterpret_cast<const u32x4*>(row + k) : (u32x4){ 0, 0, 0, 0 };
+    T v[E];
+#pragma unroll
+    for (int j = 0; j < E; ++j) v[j] = k + j < n ? row[k + j] : (T)0.f;
+    u32x4 r;
+    __builtin_memcpy(&r, v, 16);
+    return r;
+}
+
+// What the adapters add to a wave's tile: acc[i][j][r] is (row mw + 16 j + l16, column nw + 16 i + 4 quarter + r) of the group's rows.
+// A slot's product goes into sums of its own, of which its rows take theirs: an infinite weight of one adapter is nothing to the rows of another.  Where slots
+// are shorter than a tile's sixteen rows a lane adds up its elements one by one, each row from its own adapter, read once.
+template <int MI, int NI>
+__device__ __forceinline__ void add_adapters(f32x4 (&acc)[NI][MI], const LinArgs& a, int group, int mw, int nw)
+{
+    const int lane = threadIdx.x & 63, l16 = lane & 15, quarter = lane >> 4, LC = a.low_cols;
+    if (!a.adapters) return;
+    if (a.tokens < 16) {
+#pragma unroll
+        for (int j = 0; j < MI; ++j) {
+            int slot, token;
+            if (!locate_row(a, group, mw + 16 * j + l16, slot, token)) continue;
+            const int ad = adapter_of(a, slot);
+            if (ad < 0) continue;
+            const bf16_t* t = (const bf16_t*)a.low + ((size_t)slot * a.tokens + token) * 2 * LC;
+#pragma unroll
+            for (int i = 0; i < NI; ++i) {
+                const int n = nw + 16 * i + 4 * quarter;
+                const bf16_t* b[4];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) b[r] = (const bf16_t*)a.b + ((size_t)ad * a.N + (n + r < a.N ? n + r : a.N - 1)) * a.rank;
+                for (int k = 0; k < a.rank; k += 8) {
+                    const bf16x8 hi = *reinterpret_cast<const bf16x8*>(t + k), lo = *reinterpret_cast<const bf16x8*>(t + LC + k);
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const bf16x8 f = __builtin_bit_cast(bf16x8, load16(b[r], k, a.rank, a.b_vec));
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) acc[i][j][r] = fmaf((float)hi[e] + (float)lo[e], (float)f[e], acc[i][j][r]);
+                    }
+                }
+            }
+        }
+        return;
+    }
+    auto slot_of = [&](int m) { return a.slot_rows == a.tokens ? group : fast_div(m < a.slot_rows ? m : a.slot_rows - 1, a.tok_magic, a.tok_shift); };
+    auto low_row = [&](int m) {                                     // (a row that is not there: some row's, its result is not stored)
+        int slot, token;
+        if (!locate_row(a, group, m, slot, token)) { slot = slot_of(m); token = 0; }
+        return (const bf16_t*)a.low + ((size_t)slot * a.tokens + token) * 2 * LC;
+    };
+    auto b_frag = [&](int ad, int i, int k) {
+        int n = nw + 16 * i + l16;
+        n = n < a.N ? n : a.N - 1;
+        return load16((const bf16_t*)a.b + ((size_t)ad * a.N + n) * a.rank, k + 8 * quarter, a.rank, a.b_vec);
+    };
+    if (slot_of(mw) == slot_of(mw + 16 * MI - 1)) {                 // one slot: straight into the tile's sums
+        const int ad = adapter_of(a, slot_of(mw));
+        if (ad < 0) return;
+        const bf16_t* t[MI];
+#pragma unroll
+        for (int j = 0; j < MI; ++j) t[j] = low_row(mw + 16 * j + l16) + 8 * quarter;
+        for (int k = 0; k < LC; k += 32) {
+            u32x4 hi[MI], lo[MI];
+#pragma unroll
+            for (int j = 0; j < MI; ++j) {
+                hi[j] = *reinterpret_cast<const u32x4*>(t[j] + k);
+                lo[j] = *reinterpret_cast<const u32x4*>(t[j] + LC + k);
+            }
+#pragma unroll
+            for (int i = 0; i < NI; ++i) {
+                const u32x4 f = b_frag(ad, i, k);
+#pragma unroll
+                for (int j = 0; j < MI; ++j) acc[i][j] = mma_bf16(f, lo[j], mma_bf16(f, hi[j], acc[i][j]));
+            }
+        }
+        return;
+    }
+#pragma unroll
+    for (int j = 0; j < MI; ++j) {
+        const int m = mw + 16 * j, last = slot_of(m + 15), mine = slot_of(m + l16);
+        for (int s = slot_of(m); s <= last; ++s) {
+            const int ad = adapter_of(a, s);
+            if (ad < 0) continue;
+            const bf16_t* t = low_row(m + l16) + 8 * quarter;
+            constexpr int NG = NI < 4 ? NI : 4;                     // pieces at a time
+#pragma unroll
+            for (int i0 = 0; i0 < NI; i0 += NG) {
+                f32x4 sum[NG];
+#pragma unroll
+                for (int i = 0; i < NG; ++i) sum[i] = (f32x4){ 0.f, 0.f, 0.f, 0.f };
+                for (int k = 0; k < LC; k += 32) {
+                    const u32x4 hi = *reinterpret_cast<const u32x4*>(t + k), lo = *reinterpret_cast<const u32x4*>(t + LC + k);
+#pragma unroll
+                    for (int i = 0; i < NG; ++i) {
+                        const u32x4 f = b_frag(ad, i0 + i, k);
+                        sum[i] = mma_bf16(f, lo, mma_bf16(f, hi, sum[i]));
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < NG; ++i)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) acc[i0 + i][j][r] += mine == s ? sum[i][r] : 0.f;
+            }
+        }
+    }
+}
+
+}  // namespace
+
+// The tiles of linear_tile.h, by KIND (one file each); `first` counts tiles.
+template <int KIND> drf_status launch_linear_tile(int tile, const LinArgs& a, hipStream_t st);
+
+}  // namespace drf

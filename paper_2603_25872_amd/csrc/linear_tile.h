@@ -1,0 +1,298 @@
+// bf16 products of rows [slots][tokens][K] with weights, for the feed-forward block and the projections with adapters: BM x BN tiles, operands by direct
+// copies to LDS NS - 1 steps of 64 of the inner axis ahead, 16x16x32 matrix instructions, waves as WM x WN.
+//
+// The loop is that of the framework's other products: the matrix instructions of a step in groups of one weight fragment, whose LDS read is issued
+// R - 1 groups ahead, one barrier a step that far before its end, one copy instruction a group.  What is this kernel's own:
+//  - rows by slot and token with strides: a lane's copies have 32-bit offsets from its workgroup's first slot (or first row, where tiles keep to a slot);
+//  - an inner axis that is a multiple of 8 only: the last step's copies repeat the row's last 16 bytes, and zeros are written over them once they have
+//    landed (in both operands: nothing times an infinity that lies beside);
+//  - LIN_GLU: rows of a weight tile are 16 of the gate, 16 of the value, and so on, so that a lane ends with both of a column; half the columns go out;
+//  - LIN_ADAPT: where a tile keeps to a slot its adapter is more steps of the loop, 32 columns of the rank each: 64 columns of a row are the upper and
+//    the lower halves of its x A^T, those of a weight row twice the same of B.  Elsewhere the adapters are added to the finished sums (add_adapters);
+//  - the result goes out in whole rows through the idle stages, rows that are not there left out.
+#pragma once
+#include "linear_device.h"
+
+namespace drf {
+
+namespace {
+
+template <int BM, int BN, int NS, int WM, int WN, int KIND>
+__global__ void __launch_bounds__(WM * WN * 64) linear_tile_kernel(const LinArgs a)
+{
+    constexpr int NW = WM * WN, TM = BM / WM, TN = BN / WN, MI = TM / 16, NI = TN / 16;
+    constexpr int STAGE = (BM + BN) * 128, SEG = (BM + BN) / 8, LPT = SEG / NW, GROUP_M = 8;
+    constexpr int ON = KIND == LIN_GLU ? TN / 2 : TN, PITCH = ON * 2 + 16, CH = ON / 8;        // columns of a wave's result; its rows in LDS, in 16-byte pieces
+    constexpr int PASS = NW * TM * PITCH <= NS * STAGE ? TM : 32;     // rows of it at a time
+    static_assert(SEG % NW == 0 && LPT % 2 == 0 && BM <= NW * 64 && BN <= NW * 64 && NW * PASS * PITCH <= NS * STAGE, "tile shape");
+    extern __shared__ __attribute__((aligned(128))) unsigned char smem[];   // stages | bias of the tile's weight rows | where its rows go
+    float* bias = reinterpret_cast<float*>(smem + NS * STAGE);
+    uint32_t* out_at = reinterpret_cast<uint32_t*>(bias + BN);
+
+    const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, quarter = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave % WM, wn = wave / WM;
+    int tm, tn;
+    {
+        // tiles in groups of GROUP_M rows of them, consecutive ones on one XCD
+        const int nb = gridDim.x;
+        const long long idx = a.first + item_by_xcd(blockIdx.x, nb);
+        const long long per_group = (long long)GROUP_M * a.tiles_n, group = idx / per_group;
+        const int in = (int)(idx - group * per_group), first_m = (int)group * GROUP_M;
+        const int gsz = a.tiles_m - first_m < GROUP_M ? a.tiles_m - first_m : GROUP_M;
+        tm = first_m + in % gsz;
+        tn = in / gsz;
+    }
+    const int group = tm / a.slot_tiles, row0 = (tm - group * a.slot_tiles) * BM, n0 = tn * (KIND == LIN_GLU ? BN / 2 : BN);
+    const int nk = (a.K + 63) / 64, chunks = (a.K & 63) / 8;        // pieces of the last step; 0: all eight
+    const int ad = KIND == LIN_ADAPT && a.in_loop ? __builtin_amdgcn_readfirstlane(adapter_of(a, group)) : -1;
+    const int nt = nk + (ad >= 0 ? a.low_cols / 32 : 0), bound = KIND == LIN_ADAPT ? nt : nk;   // steps of the product and of the adapter
+    int slot0, token0;
+    const bool some = locate_row(a, group, row0, slot0, token0);
+    if (a.slot_rows == a.tokens) {
+        if (!some) return;                                          // the slot ends before this tile
+    } else token0 = 0;
+    const char* x0 = (const char*)a.x.data + (slot0 * a.x.slot_stride + token0 * a.x.token_stride) * 2;
+    char* out0 = (char*)a.out.data + (slot0 * a.out.slot_stride + token0 * a.out.token_stride) * 2;
+
+    // A wave's copies: LPT instructions of 8 rows; chunk c of row r sits at position c ^ ((r / 2) % 8).
+    const int prow = lane >> 3, ppos = lane & 7;
+    uint32_t voff[LPT], over[2];
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+        const int chunk = ppos ^ ((p * 4 + prow / 2) & 7);
+        over[p] = chunks && chunk >= chunks ? (uint32_t)(chunk - chunks + 1) * 16u : 0u;
+    }
+#pragma unroll
+    for (int i = 0; i < LPT; ++i) {
+        const int r = (wave * LPT + i) * 8 + prow, chunk = ppos ^ ((r / 2) & 7);
+        if ((wave * LPT + i) * 8 < BM) {
+            int slot, token;
+            if (!locate_row(a, group, row0 + r, slot, token)) { slot = slot0; token = token0; }
+            voff[i] = (uint32_t)(((slot - slot0) * a.x.slot_stride + (token - token0) * a.x.token_stride) * 2) + (uint32_t)chunk * 16u;
+        } else {
+            int n = r - BM;
+            if constexpr (KIND == LIN_GLU) n = n / 32 * 16 + n % 16;
+            n = n0 + n < a.N ? n : a.N - 1 - n0;
+            voff[i] = (uint32_t)n * (uint32_t)a.K * 2u + (uint32_t)chunk * 16u;
+        }
+    }
+    const char* w0 = (const char*)a.w + (size_t)n0 * a.K * 2;
+    const char* w1 = KIND == LIN_GLU ? w0 + (size_t)a.N * a.K * 2 : w0;
+    const char* low0 = (const char*)a.low + ((size_t)slot0 * a.tokens + row0) * a.low_cols * 4;
+    const char* b0 = (const char*)a.b + ((size_t)(ad < 0 ? 0 : ad) * a.N + n0) * a.rank * 2;
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(DRF_LDS_AS unsigned char*)smem;
+    auto issue_one = [&](auto ic, int kt, int stage) __attribute__((always_inline)) {
+        constexpr int i = decltype(ic)::value;
+        const int g = wave * LPT + i;
+        if (KIND == LIN_ADAPT && kt >= nk) {
+            const int r = g * 8 + prow, chunk = ppos ^ ((r / 2) & 7), e = kt - nk, left = (a.rank - 32 * e) / 8;
+            const char* src;
+            if (g * 8 < BM) {
+                const int row = row0 + r < a.tokens ? r : 0;
+                src = low0 + (size_t)row * a.low_cols * 4 + (chunk & 3) * 16 + (chunk & 4 ? a.low_cols * 2 : 0) + e * 64;
+            } else {
+                const int n = n0 + r - BM < a.N ? r - BM : a.N - 1 - n0, c = (chunk & 3) < left ? chunk & 3 : left - 1;
+                src = b0 + (size_t)n * a.rank * 2 + c * 16 + e * 64;
+            }
+            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" :: "s"(lds0 + (uint32_t)(stage * STAGE + g * 1024)), "v"(src) : "memory");
+            return;
+        }
+        const char* base = (g * 8 < BM ? x0 : (g - BM / 8) & 2 ? w1 : w0) + (size_t)kt * 128;
+        const uint32_t dst = lds0 + (uint32_t)(stage * STAGE + g * 1024);
+        const uint32_t vo = voff[i] - (kt == nk - 1 ? over[i & 1] : 0u);
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" :: "s"(dst), "v"(vo), "s"(base) : "memory");
+    };
+    auto issue = [&](int kt, int stage) __attribute__((always_inline)) { static_for<0, LPT>([&](auto ic) { issue_one(ic, kt, stage); }); };
+    // step kt has landed for every wave: zeros behind the end of its rows, if they end in it
+    auto cut = [&](int kt, int stage) __attribute__((always_inline)) {
+        const bool low = KIND == LIN_ADAPT && kt >= nk;
+        const int from = low ? (a.rank - 32 * (kt - nk)) / 8 : chunks;
+        if (low ? from >= 4 : !chunks || kt != nk - 1) return;
+        for (int r = tid + (low ? BM : 0); r < BM + BN; r += NW * 64)
+            for (int c = from; c < (low ? 4 : 8); ++c) {
+                *reinterpret_cast<u32x4*>(smem + stage * STAGE + r * 128 + (c ^ ((r / 2) & 7)) * 16) = (u32x4){ 0, 0, 0, 0 };
+                if (low) *reinterpret_cast<u32x4*>(smem + stage * STAGE + r * 128 + ((c + 4) ^ ((r / 2) & 7)) * 16) = (u32x4){ 0, 0, 0, 0 };
+            }
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    };
+
+    f32x4 acc[NI][MI];
+#pragma unroll
+    for (int i = 0; i < NI; ++i)
+#pragma unroll
+        for (int j = 0; j < MI; ++j) acc[i][j] = (f32x4){ 0.f, 0.f, 0.f, 0.f };
+
+    constexpr int G = 2 * NI;
+    constexpr int R = G % 6 == 0 && NI >= 6 ? 6 : G % 4 == 0 && NI >= 4 ? 4 : 2, D = R - 1;
+    static_assert(G % R == 0 && D < NI && D + MI <= 15, "ring size");
+    constexpr int HEAD0 = D < LPT ? D : LPT;
+    constexpr bool kSpread = NS == 2 && LPT - HEAD0 <= G - D;
+    constexpr int HEAD = kSpread ? HEAD0 : LPT, TAIL = LPT - HEAD;
+    u32x4 fa[2][MI], fw[R];
+    uint32_t a_addr[2], w_addr[2];
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks) {
+        const uint32_t pos = (uint32_t)(l16 * 128 + (((ks * 4 + quarter) ^ ((l16 / 2) & 7)) * 16));
+        a_addr[ks] = lds0 + (uint32_t)(wm * TM * 128) + pos;
+        w_addr[ks] = lds0 + (uint32_t)((BM + wn * TN) * 128) + pos;
+    }
+    auto fetch = [&](auto pc, const uint32_t (&aa)[2], const uint32_t (&wa)[2]) {
+        constexpr int p = decltype(pc)::value, ks = p / NI, i = p % NI;
+        if constexpr (i == 0)
+            static_for<0, MI>([&](auto jc) {
+                constexpr int j = decltype(jc)::value;
+                lds_read16<j * 2048>(fa[ks & 1][j], aa[ks]);
+            });
+        lds_read16<i * 2048>(fw[p % R], wa[ks]);
+    };
+
+#pragma unroll
+    for (int t = 0; t < NS - 1; ++t)
+        if (t < bound) issue(t, t);
+    if (tid < BN) {
+        int n = tid;
+        if constexpr (KIND == LIN_GLU) n = n / 32 * 16 + n % 16;
+        n += n0;
+        n = n < a.N ? n : a.N - 1;
+        if constexpr (KIND == LIN_GLU) n += tid / 16 % 2 ? a.N : 0;
+        bias[tid] = a.bias ? a.bias[n] : 0.f;
+    }
+    if (tid < BM) {
+        int slot, token;
+        const bool live = locate_row(a, group, row0 + tid, slot, token);
+        out_at[tid] = live ? (uint32_t)(((slot - slot0) * a.out.slot_stride + (token - token0) * a.out.token_stride) * 2) : 0xffffffffu;
+    }
+    if (NS > 2 && bound >= NS - 1) wait_vmcnt<LPT * (NS - 2)>(); else wait_vmcnt<0>();
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    cut(0, 0);
+    static_for<0, NI * MI>([&](auto pc) { constexpr int p = decltype(pc)::value; hold_acc<false>(acc[p / MI][p % MI]); });
+    settle_mfma();
+    if (NS - 1 < bound) issue(NS - 1, NS - 1);
+    static_for<0, D>([&](auto pc) { fetch(pc, a_addr, w_addr); });
+    int cs = 0;                                     // stage of step kt
+    for (int kt = 0; kt < bound; ++kt) {
+        const int ns = cs + 1 == NS ? 0 : cs + 1;
+        const uint32_t co = (uint32_t)cs * (uint32_t)STAGE, no = (uint32_t)ns * (uint32_t)STAGE;
+        uint32_t ca[2], cw[2], na[2], nw[2];
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks) { ca[ks] = a_addr[ks] + co; cw[ks] = w_addr[ks] + co; na[ks] = a_addr[ks] + no; nw[ks] = w_addr[ks] + no; }
+        static_for<0, G>([&](auto gc) {
+            constexpr int g = decltype(gc)::value;
+            if constexpr (g + D == G) {
+                // step kt + 1 has landed and this wave's reads of step kt are complete, for every wave after the barrier: kt's stage may be filled again
+                if (NS > 2 && kt + NS - 1 < bound) wait_vmcnt<LPT * (NS - 2)>(); else wait_vmcnt<0>();
+                asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+                if (kt + 1 < bound) cut(kt + 1, ns);
+                if constexpr (!kSpread) {
+                    if (kt + NS < bound) issue(kt + NS, cs);
+                }
+            }
+            if constexpr (kSpread) {
+                if constexpr (g >= G - D && g - (G - D) < HEAD) {
+                    if (kt + NS < bound) issue_one(std::integral_constant<int, g - (G - D)>{}, kt + NS, cs);
+                } else if constexpr (g < G - D && g < TAIL) {
+                    if (kt >= 1 && kt + 1 < bound) issue_one(std::integral_constant<int, HEAD + g>{}, kt + 1, ns);
+                }
+            }
+            // (in the last step the positions beyond it read the idle stage: LDS that is there, values unused)
+            if constexpr (g + D < G) fetch(std::integral_constant<int, g + D>{}, ca, cw);
+            else fetch(std::integral_constant<int, g + D - G>{}, na, nw);
+            __builtin_amdgcn_sched_barrier(0);
+            constexpr int later = D + (((g + D) / NI) != (g / NI) ? MI : 0);     // reads issued behind this group's
+            if constexpr (g % NI == 0) wait_frags<later, MI>(fw[g % R], fa[(g / NI) & 1]);
+            else wait_frag<later>(fw[g % R]);
+            static_for<0, MI>([&](auto jc) {
+                constexpr int j = (g & 1) ? MI - 1 - decltype(jc)::value : decltype(jc)::value;
+                mfma<false>(acc[g % NI][j], fw[g % R], fa[(g / NI) & 1][j]);
+            });
+            __builtin_amdgcn_sched_barrier(0);
+        });
+        cs = ns;
+    }
+    // the last look-ahead reads are on their way into the fragment registers: they pass through the wait
+    wait_frag<0>(fw[0]);
+    settle_mfma();
+    static_for<0, NI * MI>([&](auto pc) { constexpr int p = decltype(pc)::value; hold_acc<false>(acc[p / MI][p % MI]); });
+#pragma unroll
+    for (int r = 1; r < R; ++r) hold_frag(fw[r]);
+#pragma unroll
+    for (int j = 0; j < MI; ++j) { hold_frag(fa[0][j]); hold_frag(fa[1][j]); }
+
+    if constexpr (KIND == LIN_ADAPT && BM < 256) {
+        if (!a.in_loop) add_adapters(acc, a, group, row0 + wm * TM, n0 + wn * TN);
+    }
+
+    // ---- bias and activation, then in whole rows through LDS of the wave's own: acc[i][j][r] is (row 16 j + l16, weight row 16 i + 4 quarter + r)
+    asm volatile("s_barrier" ::: "memory");         // every wave has read its last fragments
+    unsigned char* wbuf = smem + wave * (PASS * PITCH);
+    const int nc = n0 + wn * ON;
+#pragma unroll
+    for (int p = 0; p < TM / PASS; ++p) {
+#pragma unroll
+        for (int i = 0; i < NI; i += KIND == LIN_GLU ? 2 : 1) {
+            const f32x4 b0 = *reinterpret_cast<const f32x4*>(bias + wn * TN + i * 16 + 4 * quarter);
+            f32x4 b1 = b0;
+            if constexpr (KIND == LIN_GLU) b1 = *reinterpret_cast<const f32x4*>(bias + wn * TN + (i + 1) * 16 + 4 * quarter);
+#pragma unroll
+            for (int jj = 0; jj < PASS / 16; ++jj) {
+                const int j = p * (PASS / 16) + jj;
+                __builtin_amdgcn_sched_barrier(0);  // (pieces computed far ahead of their stores would spill)
+                f32x4 v = acc[i][j] + b0;
+                if constexpr (KIND == LIN_GLU) {
+                    const f32x4 u = acc[i + 1][j] + b1;
+                    if (a.act == DRF_GLU_GELU)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) v[r] = glu(v[r], u[r], DRF_GLU_GELU);
+                    else
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) v[r] = glu(v[r], u[r], DRF_GLU_SILU);
+                }
+                const bf16x4 o = { (bf16_t)v[0], (bf16_t)v[1], (bf16_t)v[2], (bf16_t)v[3] };
+                *reinterpret_cast<bf16x4*>(wbuf + (jj * 16 + l16) * PITCH + (KIND == LIN_GLU ? i / 2 : i) * 32 + quarter * 8) = o;
+            }
+        }
+#pragma unroll 4
+        for (int id = lane; id < PASS * CH; id += 64) {
+            const int r = id / CH, c = id - r * CH, n = nc + c * 8;
+            const uint32_t at = out_at[wm * TM + p * PASS + r];
+            const u32x4 v = *reinterpret_cast<const u32x4*>(wbuf + r * PITCH + c * 16);
+            if (at == 0xffffffffu || n >= a.N) continue;
+            bf16_t* o = reinterpret_cast<bf16_t*>(out0 + at) + n;
+            if (a.out_vec && n + 8 <= a.N) *reinterpret_cast<u32x4*>(o) = v;
+            else {
+                const bf16x8 e = __builtin_bit_cast(bf16x8, v);
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    if (n + k < a.N) o[k] = e[k];
+            }
+        }
+    }
+}
+
+template <int BM, int BN, int NS, int WM, int WN, int KIND> drf_status launch_tile_shape(LinArgs a, hipStream_t st)
+{
+    constexpr size_t smem = (size_t)NS * (BM + BN) * 128 + BN * 4 + BM * 4;
+    static_assert(smem <= 160 * 1024, "LDS of a CU");
+    static std::atomic<uint64_t> lds_allowed{ 0 };
+    auto kern = linear_tile_kernel<BM, BN, NS, WM, WN, KIND>;
+    DRF_HIP(allow_lds(reinterpret_cast<const void*>(kern), (int)smem, lds_allowed));
+    const long long most = 1 << 22;                                 // (a launch holds fewer than 2^32 threads)
+    for (a.first = 0; a.first < a.tiles; a.first += most) {
+        hipLaunchKernelGGL(kern, dim3((unsigned)std::min(most, a.tiles - a.first)), dim3(WM * WN * 64), smem, st, a);
+        DRF_HIP(hipGetLastError());
+    }
+    return DRF_OK;
+}
+
+}  // namespace
+
+template <int KIND> drf_status launch_linear_tile(int tile, const LinArgs& a, hipStream_t st)
+{
+    switch (tile) {
+    case 0: return launch_tile_shape<256, 256, 2, 4, 2, KIND>(a, st);
+    case 1: return launch_tile_shape<128, 128, 4, 4, 2, KIND>(a, st);
+    default: return launch_tile_shape<64, 64, 4, 2, 2, KIND>(a, st);
+    }
+}
+
+}  // namespace drf

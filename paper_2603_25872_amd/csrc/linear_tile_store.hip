@@ -1,0 +1,8 @@
+// The tiles of linear_tile.h for LIN_STORE (a file of their own: the kinds compile beside one another).
+#include "linear_tile.h"
+
+namespace drf {
+
+template drf_status launch_linear_tile<LIN_STORE>(int, const LinArgs&, hipStream_t);
+
+}  // namespace drf
