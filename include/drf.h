@@ -469,8 +469,7 @@ typedef struct { void* data; int64_t slot_stride, token_stride; } drf_rows;
  *   out NULL: z is not stored.  h NULL: no h.  y NULL: z = x_scale x, and out has to be NULL; after, gate and y_scale are not looked at.
  * h is formed from z as it is before its rounding to the stream's type.  Norms add their squares in fp32: values up to 1e18.  Rows behind a slot's
  * length (lens, DEVICE int32 [slots] or NULL) are neither read nor written.  out may be x itself and h y itself (address and strides), otherwise
- * no output overlaps another tensor.  1 <= width <= 16384.  16-byte aligned tensors whose strides and width are multiples of 16
- * bytes take 16-byte accesses; all others one element at a time.
+ * no output overlaps another tensor.  1 <= width <= 16384.
  */
 typedef struct {
     drf_qk_norm norm;

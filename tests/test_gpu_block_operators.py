@@ -184,14 +184,14 @@ def test_residual_norm_parts_of_it(torch, drf, stream, branch, D):
 
 
 @pytest.mark.parametrize("stream,branch", TYPES)
-@pytest.mark.parametrize("D", [72, 131, 2500])
-def test_residual_norm_lengths(torch, drf, stream, branch, D):
+@pytest.mark.parametrize("N,D", [(11, 72), (11, 131), (11, 2500), (600, 72), (600, 131), (500, 1153)])
+def test_residual_norm_lengths(torch, drf, stream, branch, N, D):
     """Rows behind a slot's length are neither read (they are NaN) nor written; lengths of none, one, all, fewer than none and more than all."""
     rng = np.random.default_rng(D)
-    S, N = 6, 11
+    S = 6
     x, y, a, r = residual_case(torch, rng, S, N, D, stream, branch, "layer", "rms", "plain")
     zz, ez, hh, eh = residual(f64(x), f64(y), r)
-    lens = [0, 1, 11, -5, 100, 6]
+    lens = [0, 1, N, -5, N + 100, N // 2 + 1]
     for j, n in enumerate(lens):
         n = min(max(n, 0), N)
         x[j, n:] = float("nan")
