@@ -101,6 +101,12 @@ int drf_probe_block_route(int slots, int tokens, int hidden, int heads, int mlp_
 drf_status drf_graph_stats(drf_denoiser* den, int* captured, int* failed, long long* replays);
 
 /*
+ * The bf16 products of drf_gated_ffn and drf_linear_adapters called on this thread from now on run on tile `tile` (0 ..) where that tile can take them; -1: by choice.
+ * Returns the number of tiles.  Host only.
+ */
+int drf_probe_linear_tile(int tile);
+
+/*
  * Measurement hook: ONE launch of the fused update kernel in the shape drf_sample gives it after a
  * draft pass: guidance combine of the pass's noise fields (g = 2: eps = eps_null + w (eps_cond -
  * eps_null); g = 1: none), the chain of n_chain standard updates s_from -> s_from - 1 -> ... starting

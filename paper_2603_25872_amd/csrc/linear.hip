@@ -8,6 +8,7 @@
 // This file has the entry points, the choice of a tile, x A^T and all of fp32; bf16 products run on the tiles of linear_tile.h.  The weights are the matrix
 // instruction's first operand throughout: a lane ends with four consecutive columns of one row.
 #include "linear_device.h"
+#include "../../include/drf_measure.h"
 
 namespace drf {
 
@@ -271,7 +272,10 @@ constexpr int kMaxTokenStride = 1 << 22;           // 256 rows within 2^31 bytes
 
 // Tiles and a time model of a launch of each: rounds of 256 (x per_cu) workgroups of `round` + steps * lat us.
 struct Tile { int bm, bn, per_cu; double base, round, lat; };
-const Tile kLinTiles[] = { { 256, 256, 1, 0.0, 8.0, 1.31 }, { 128, 128, 1, 1.3, 2.95, 0.48 }, { 64, 64, 2, 1.9, 1.4, 0.24 } };
+const Tile kLinTiles[] = { { 256, 256, 1, 0.0, 8.0, 1.31 }, { 256, 128, 1, 0.24, 4.29, 0.85 }, { 128, 128, 1, 1.3, 2.95, 0.48 }, { 128, 128, 2, 1.0, 2.65, 0.51 },
+                           { 128, 64, 2, 1.5, 2.1, 0.32 }, { 64, 128, 2, 1.5, 2.1, 0.32 }, { 64, 64, 2, 1.9, 1.4, 0.24 } };
+constexpr int kTiles = sizeof(kLinTiles) / sizeof(kLinTiles[0]);
+thread_local int g_forced_tile = -1;                    // see drf_probe_linear_tile
 
 // Whether tiles of up to 256 rows may cross slots: offsets within one from its first slot on stay below 2^31 bytes.
 bool may_cross(const drf_rows& t, int tokens)
@@ -294,9 +298,9 @@ template <int KIND> drf_status launch_bf16(LinArgs a, hipStream_t st)
     a.out_vec = rows_aligned(a.out, 8);
     const bool cross = a.slots > 1 && may_cross(a.x, a.tokens) && may_cross(a.out, a.tokens);
     const int weight_rows = KIND == LIN_GLU ? 2 * a.N : a.N, steps = (a.K + 63) / 64;
-    int best = 2;
+    int best = kTiles - 1;
     double best_us = 1e300;
-    for (int t = 0; t < 3; ++t) {
+    for (int t = 0; t < kTiles; ++t) {
         const Tile& m = kLinTiles[t];
         const long long tn = (weight_rows + m.bn - 1) / m.bn, by_slot = (long long)a.slots * ((a.tokens + m.bm - 1) / m.bm);
         // (the largest tile has adapters as steps of its loop only, which keeps to a slot)
@@ -304,6 +308,7 @@ template <int KIND> drf_status launch_bf16(LinArgs a, hipStream_t st)
         if (KIND == LIN_ADAPT && t == 0 && a.adapters && !a.b_vec) continue;
         const long long tm = keep ? by_slot : std::min(by_slot, ((long long)a.slots * a.tokens + m.bm - 1) / m.bm);
         const double us = m.base + std::ceil((double)(tm * tn) / (256 * m.per_cu)) * (m.round + steps * m.lat * m.per_cu);
+        if (t == g_forced_tile) { best = t; break; }
         if (us < best_us) { best_us = us; best = t; }
     }
     const Tile& m = kLinTiles[best];
@@ -464,4 +469,10 @@ extern "C" drf_status drf_linear_adapters(const drf_adapters_config* cfg, const 
         DRF_FAIL(DRF_EINVAL, "scratch is NULL, not 16-byte aligned or too small");
     a.lens = c.lens;
     return run_adapters(c, a, scratch, (hipStream_t)hip_stream);
+}
+
+extern "C" int drf_probe_linear_tile(int tile)
+{
+    g_forced_tile = tile;
+    return kTiles;
 }

@@ -77,7 +77,7 @@ __global__ void __launch_bounds__(WM * WN * 64) linear_tile_kernel(const LinArgs
         }
     }
     const char* w0 = (const char*)a.w + (size_t)n0 * a.K * 2;
-    const char* w1 = KIND == LIN_GLU ? w0 + (size_t)a.N * a.K * 2 : w0;
+    const ptrdiff_t to_x = (ptrdiff_t)((uintptr_t)x0 - (uintptr_t)w0), to_value = (ptrdiff_t)a.N * a.K * 2;
     const char* low0 = (const char*)a.low + ((size_t)slot0 * a.tokens + row0) * a.low_cols * 4;
     const char* b0 = (const char*)a.b + ((size_t)(ad < 0 ? 0 : ad) * a.N + n0) * a.rank * 2;
     const uint32_t lds0 = (uint32_t)(uintptr_t)(DRF_LDS_AS unsigned char*)smem;
@@ -97,12 +97,14 @@ __global__ void __launch_bounds__(WM * WN * 64) linear_tile_kernel(const LinArgs
             asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" :: "s"(lds0 + (uint32_t)(stage * STAGE + g * 1024)), "v"(src) : "memory");
             return;
         }
-        const char* base = (g * 8 < BM ? x0 : (g - BM / 8) & 2 ? w1 : w0) + (size_t)kt * 128;
+        // (sums: a choice between the three addresses would keep them, and everything beside them, in memory)
+        const bool of_x = g * 8 < BM, second = KIND == LIN_GLU && !of_x && ((g - BM / 8) & 2);
+        const char* base = w0 + (of_x ? to_x : 0) + (second ? to_value : 0) + (size_t)kt * 128;
         const uint32_t dst = lds0 + (uint32_t)(stage * STAGE + g * 1024);
         const uint32_t vo = voff[i] - (kt == nk - 1 ? over[i & 1] : 0u);
         asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" :: "s"(dst), "v"(vo), "s"(base) : "memory");
     };
-    auto issue = [&](int kt, int stage) __attribute__((always_inline)) { static_for<0, LPT>([&](auto ic) { issue_one(ic, kt, stage); }); };
+    auto issue = [&](int kt, int stage) __attribute__((always_inline)) { static_for<0, LPT>([&](auto ic) __attribute__((always_inline)) { issue_one(ic, kt, stage); }); };
     // step kt has landed for every wave: zeros behind the end of its rows, if they end in it
     auto cut = [&](int kt, int stage) __attribute__((always_inline)) {
         const bool low = KIND == LIN_ADAPT && kt >= nk;
@@ -136,10 +138,10 @@ __global__ void __launch_bounds__(WM * WN * 64) linear_tile_kernel(const LinArgs
         a_addr[ks] = lds0 + (uint32_t)(wm * TM * 128) + pos;
         w_addr[ks] = lds0 + (uint32_t)((BM + wn * TN) * 128) + pos;
     }
-    auto fetch = [&](auto pc, const uint32_t (&aa)[2], const uint32_t (&wa)[2]) {
+    auto fetch = [&](auto pc, const uint32_t (&aa)[2], const uint32_t (&wa)[2]) __attribute__((always_inline)) {
         constexpr int p = decltype(pc)::value, ks = p / NI, i = p % NI;
         if constexpr (i == 0)
-            static_for<0, MI>([&](auto jc) {
+            static_for<0, MI>([&](auto jc) __attribute__((always_inline)) {
                 constexpr int j = decltype(jc)::value;
                 lds_read16<j * 2048>(fa[ks & 1][j], aa[ks]);
             });
@@ -165,7 +167,7 @@ __global__ void __launch_bounds__(WM * WN * 64) linear_tile_kernel(const LinArgs
     if (NS > 2 && bound >= NS - 1) wait_vmcnt<LPT * (NS - 2)>(); else wait_vmcnt<0>();
     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
     cut(0, 0);
-    static_for<0, NI * MI>([&](auto pc) { constexpr int p = decltype(pc)::value; hold_acc<false>(acc[p / MI][p % MI]); });
+    static_for<0, NI * MI>([&](auto pc) __attribute__((always_inline)) { constexpr int p = decltype(pc)::value; hold_acc<false>(acc[p / MI][p % MI]); });
     settle_mfma();
     if (NS - 1 < bound) issue(NS - 1, NS - 1);
     static_for<0, D>([&](auto pc) { fetch(pc, a_addr, w_addr); });
@@ -176,7 +178,7 @@ __global__ void __launch_bounds__(WM * WN * 64) linear_tile_kernel(const LinArgs
         uint32_t ca[2], cw[2], na[2], nw[2];
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks) { ca[ks] = a_addr[ks] + co; cw[ks] = w_addr[ks] + co; na[ks] = a_addr[ks] + no; nw[ks] = w_addr[ks] + no; }
-        static_for<0, G>([&](auto gc) {
+        static_for<0, G>([&](auto gc) __attribute__((always_inline)) {
             constexpr int g = decltype(gc)::value;
             if constexpr (g + D == G) {
                 // step kt + 1 has landed and this wave's reads of step kt are complete, for every wave after the barrier: kt's stage may be filled again
@@ -201,7 +203,7 @@ __global__ void __launch_bounds__(WM * WN * 64) linear_tile_kernel(const LinArgs
             constexpr int later = D + (((g + D) / NI) != (g / NI) ? MI : 0);     // reads issued behind this group's
             if constexpr (g % NI == 0) wait_frags<later, MI>(fw[g % R], fa[(g / NI) & 1]);
             else wait_frag<later>(fw[g % R]);
-            static_for<0, MI>([&](auto jc) {
+            static_for<0, MI>([&](auto jc) __attribute__((always_inline)) {
                 constexpr int j = (g & 1) ? MI - 1 - decltype(jc)::value : decltype(jc)::value;
                 mfma<false>(acc[g % NI][j], fw[g % R], fa[(g / NI) & 1][j]);
             });
@@ -212,13 +214,13 @@ __global__ void __launch_bounds__(WM * WN * 64) linear_tile_kernel(const LinArgs
     // the last look-ahead reads are on their way into the fragment registers: they pass through the wait
     wait_frag<0>(fw[0]);
     settle_mfma();
-    static_for<0, NI * MI>([&](auto pc) { constexpr int p = decltype(pc)::value; hold_acc<false>(acc[p / MI][p % MI]); });
+    static_for<0, NI * MI>([&](auto pc) __attribute__((always_inline)) { constexpr int p = decltype(pc)::value; hold_acc<false>(acc[p / MI][p % MI]); });
 #pragma unroll
     for (int r = 1; r < R; ++r) hold_frag(fw[r]);
 #pragma unroll
     for (int j = 0; j < MI; ++j) { hold_frag(fa[0][j]); hold_frag(fa[1][j]); }
 
-    if constexpr (KIND == LIN_ADAPT && BM < 256) {
+    if constexpr (KIND == LIN_ADAPT && BM * BN < 256 * 256) {
         if (!a.in_loop) add_adapters(acc, a, group, row0 + wm * TM, n0 + wn * TN);
     }
 
@@ -290,7 +292,11 @@ template <int KIND> drf_status launch_linear_tile(int tile, const LinArgs& a, hi
 {
     switch (tile) {
     case 0: return launch_tile_shape<256, 256, 2, 4, 2, KIND>(a, st);
-    case 1: return launch_tile_shape<128, 128, 4, 4, 2, KIND>(a, st);
+    case 1: return launch_tile_shape<256, 128, 3, 4, 2, KIND>(a, st);
+    case 2: return launch_tile_shape<128, 128, 4, 4, 2, KIND>(a, st);
+    case 3: return launch_tile_shape<128, 128, 2, 4, 2, KIND>(a, st);
+    case 4: return launch_tile_shape<128, 64, 3, 2, 2, KIND>(a, st);
+    case 5: return launch_tile_shape<64, 128, 3, 2, 2, KIND>(a, st);
     default: return launch_tile_shape<64, 64, 4, 2, 2, KIND>(a, st);
     }
 }
