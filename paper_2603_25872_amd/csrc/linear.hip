@@ -273,7 +273,8 @@ constexpr int kMaxTokenStride = 1 << 22;           // 256 rows within 2^31 bytes
 // Tiles and a time model of a launch of each: rounds of 256 (x per_cu) workgroups of `round` + steps * lat us.
 struct Tile { int bm, bn, per_cu; double base, round, lat; };
 const Tile kLinTiles[] = { { 256, 256, 1, 0.0, 8.0, 1.31 }, { 256, 128, 1, 0.24, 4.29, 0.85 }, { 128, 128, 1, 1.3, 2.95, 0.48 }, { 128, 128, 2, 1.0, 2.65, 0.51 },
-                           { 128, 64, 2, 1.5, 2.1, 0.32 }, { 64, 128, 2, 1.5, 2.1, 0.32 }, { 64, 64, 2, 1.9, 1.4, 0.24 } };
+                           { 128, 64, 2, 1.5, 2.1, 0.32 }, { 64, 128, 2, 1.5, 2.1, 0.32 }, { 64, 64, 2, 1.9, 1.4, 0.24 }, { 64, 64, 1, 1.9, 1.4, 0.2 },
+                           { 256, 256, 1, 0.0, 7.66, 1.31 }, { 256, 288, 1, 0.0, 8.99, 1.59 } };
 constexpr int kTiles = sizeof(kLinTiles) / sizeof(kLinTiles[0]);
 thread_local int g_forced_tile = -1;                    // see drf_probe_linear_tile
 
@@ -303,9 +304,11 @@ template <int KIND> drf_status launch_bf16(LinArgs a, hipStream_t st)
     for (int t = 0; t < kTiles; ++t) {
         const Tile& m = kLinTiles[t];
         const long long tn = (weight_rows + m.bn - 1) / m.bn, by_slot = (long long)a.slots * ((a.tokens + m.bm - 1) / m.bm);
-        // (the largest tile has adapters as steps of its loop only, which keeps to a slot)
-        const bool keep = !cross || (KIND == LIN_ADAPT && t == 0 && a.adapters);
-        if (KIND == LIN_ADAPT && t == 0 && a.adapters && !a.b_vec) continue;
+        if (KIND == LIN_GLU && t == 9) continue;                    // (pairs of pieces in a wave)
+        const bool large = m.bm * m.bn >= 256 * 256;
+        // (the largest tiles have adapters as steps of its loop only, which keeps to a slot)
+        const bool keep = !cross || (KIND == LIN_ADAPT && large && a.adapters);
+        if (KIND == LIN_ADAPT && large && a.adapters && !a.b_vec) continue;
         const long long tm = keep ? by_slot : std::min(by_slot, ((long long)a.slots * a.tokens + m.bm - 1) / m.bm);
         const double us = m.base + std::ceil((double)(tm * tn) / (256 * m.per_cu)) * (m.round + steps * m.lat * m.per_cu);
         if (t == g_forced_tile) { best = t; break; }
@@ -313,7 +316,7 @@ template <int KIND> drf_status launch_bf16(LinArgs a, hipStream_t st)
     }
     const Tile& m = kLinTiles[best];
     const int by_slot = a.slots * ((a.tokens + m.bm - 1) / m.bm), crossing = (a.slots * a.tokens + m.bm - 1) / m.bm;
-    const bool crosses = cross && crossing < by_slot && !(KIND == LIN_ADAPT && best == 0 && a.adapters);
+    const bool crosses = cross && crossing < by_slot && !(KIND == LIN_ADAPT && m.bm * m.bn >= 256 * 256 && a.adapters);
     a.in_loop = KIND == LIN_ADAPT && !crosses && a.b_vec;
     a.slot_rows = crosses ? a.slots * a.tokens : a.tokens;
     a.slot_tiles = (a.slot_rows + m.bm - 1) / m.bm;

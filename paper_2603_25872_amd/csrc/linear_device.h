@@ -171,6 +171,55 @@ __device__ __forceinline__ void add_adapters(f32x4 (&acc)[NI][MI], const LinArgs
     }
 }
 
+// A wave's finished sums with bias and activation, in whole rows through LDS of its own (wbuf): acc[i][j][r] is (row 16 j + l16, weight row 16 i + 4 quarter + r).
+// bias: of its weight rows; out_at: where its rows go (bytes from out0), all ones: nowhere; nc: the first column that it stores.
+template <int MI, int NI, int KIND, int PASS, int PITCH, int CH>
+__device__ __forceinline__ void store_wave_tile(const f32x4 (&acc)[NI][MI], const LinArgs& a, const float* bias, const uint32_t* out_at, char* out0, int nc, unsigned char* wbuf)
+{
+    const int lane = threadIdx.x & 63, l16 = lane & 15, quarter = lane >> 4;
+#pragma unroll
+    for (int p = 0; p < MI * 16 / PASS; ++p) {
+#pragma unroll
+        for (int i = 0; i < NI; i += KIND == LIN_GLU ? 2 : 1) {
+            const f32x4 b0 = *reinterpret_cast<const f32x4*>(bias + i * 16 + 4 * quarter);
+            f32x4 b1 = b0;
+            if constexpr (KIND == LIN_GLU) b1 = *reinterpret_cast<const f32x4*>(bias + (i + 1) * 16 + 4 * quarter);
+#pragma unroll
+            for (int jj = 0; jj < PASS / 16; ++jj) {
+                const int j = p * (PASS / 16) + jj;
+                __builtin_amdgcn_sched_barrier(0);  // (pieces computed far ahead of their stores would spill)
+                f32x4 v = acc[i][j] + b0;
+                if constexpr (KIND == LIN_GLU) {
+                    const f32x4 u = acc[i + 1][j] + b1;
+                    if (a.act == DRF_GLU_GELU)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) v[r] = glu(v[r], u[r], DRF_GLU_GELU);
+                    else
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) v[r] = glu(v[r], u[r], DRF_GLU_SILU);
+                }
+                const bf16x4 o = { (bf16_t)v[0], (bf16_t)v[1], (bf16_t)v[2], (bf16_t)v[3] };
+                *reinterpret_cast<bf16x4*>(wbuf + (jj * 16 + l16) * PITCH + (KIND == LIN_GLU ? i / 2 : i) * 32 + quarter * 8) = o;
+            }
+        }
+#pragma unroll 4
+        for (int id = lane; id < PASS * CH; id += 64) {
+            const int r = id / CH, c = id - r * CH, n = nc + c * 8;
+            const uint32_t at = out_at[p * PASS + r];
+            const u32x4 v = *reinterpret_cast<const u32x4*>(wbuf + r * PITCH + c * 16);
+            if (at == 0xffffffffu || n >= a.N) continue;
+            bf16_t* o = reinterpret_cast<bf16_t*>(out0 + at) + n;
+            if (a.out_vec && n + 8 <= a.N) *reinterpret_cast<u32x4*>(o) = v;
+            else {
+                const bf16x8 e = __builtin_bit_cast(bf16x8, v);
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    if (n + k < a.N) o[k] = e[k];
+            }
+        }
+    }
+}
+
 }  // namespace
 
 // The tiles of linear_tile.h, by KIND (one file each); `first` counts tiles.

@@ -11,7 +11,7 @@
 //    the lower halves of its x A^T, those of a weight row twice the same of B.  Elsewhere the adapters are added to the finished sums (add_adapters);
 //  - the result goes out in whole rows through the idle stages, rows that are not there left out.
 #pragma once
-#include "linear_device.h"
+#include "linear_wide.h"
 
 namespace drf {
 
@@ -80,31 +80,33 @@ __global__ void __launch_bounds__(WM * WN * 64) linear_tile_kernel(const LinArgs
     const ptrdiff_t to_x = (ptrdiff_t)((uintptr_t)x0 - (uintptr_t)w0), to_value = (ptrdiff_t)a.N * a.K * 2;
     const char* low0 = (const char*)a.low + ((size_t)slot0 * a.tokens + row0) * a.low_cols * 4;
     const char* b0 = (const char*)a.b + ((size_t)(ad < 0 ? 0 : ad) * a.N + n0) * a.rank * 2;
+    const ptrdiff_t to_low = (ptrdiff_t)((uintptr_t)low0 - (uintptr_t)b0);
     const uint32_t lds0 = (uint32_t)(uintptr_t)(DRF_LDS_AS unsigned char*)smem;
-    auto issue_one = [&](auto ic, int kt, int stage) __attribute__((always_inline)) {
+    // PLAIN: a step of the product whose rows do not end in it
+    auto issue_one = [&](auto ic, auto plain_c, int kt, int stage) __attribute__((always_inline)) {
         constexpr int i = decltype(ic)::value;
+        constexpr bool PLAIN = decltype(plain_c)::value;
         const int g = wave * LPT + i;
-        if (KIND == LIN_ADAPT && kt >= nk) {
-            const int r = g * 8 + prow, chunk = ppos ^ ((r / 2) & 7), e = kt - nk, left = (a.rank - 32 * e) / 8;
-            const char* src;
-            if (g * 8 < BM) {
-                const int row = row0 + r < a.tokens ? r : 0;
-                src = low0 + (size_t)row * a.low_cols * 4 + (chunk & 3) * 16 + (chunk & 4 ? a.low_cols * 2 : 0) + e * 64;
-            } else {
-                const int n = n0 + r - BM < a.N ? r - BM : a.N - 1 - n0, c = (chunk & 3) < left ? chunk & 3 : left - 1;
-                src = b0 + (size_t)n * a.rank * 2 + c * 16 + e * 64;
-            }
-            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" :: "s"(lds0 + (uint32_t)(stage * STAGE + g * 1024)), "v"(src) : "memory");
-            return;
-        }
         // (sums: a choice between the three addresses would keep them, and everything beside them, in memory)
         const bool of_x = g * 8 < BM, second = KIND == LIN_GLU && !of_x && ((g - BM / 8) & 2);
         const char* base = w0 + (of_x ? to_x : 0) + (second ? to_value : 0) + (size_t)kt * 128;
+        uint32_t vo = voff[i];
+        if constexpr (!PLAIN) {
+            if (KIND == LIN_ADAPT && kt >= nk) {
+                const int r = g * 8 + prow, chunk = ppos ^ ((r / 2) & 7), e = kt - nk, left = (a.rank - 32 * e) / 8;
+                base = b0 + (of_x ? to_low : 0) + e * 64;
+                if (of_x) vo = (uint32_t)((row0 + r < a.tokens ? r : 0) * a.low_cols * 4 + (chunk & 3) * 16 + (chunk & 4 ? a.low_cols * 2 : 0));
+                else vo = (uint32_t)((n0 + r - BM < a.N ? r - BM : a.N - 1 - n0) * a.rank * 2 + ((chunk & 3) < left ? chunk & 3 : left - 1) * 16);
+            } else if (chunks && kt == nk - 1) vo -= over[i & 1];
+        }
         const uint32_t dst = lds0 + (uint32_t)(stage * STAGE + g * 1024);
-        const uint32_t vo = voff[i] - (kt == nk - 1 ? over[i & 1] : 0u);
         asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" :: "s"(dst), "v"(vo), "s"(base) : "memory");
     };
-    auto issue = [&](int kt, int stage) __attribute__((always_inline)) { static_for<0, LPT>([&](auto ic) __attribute__((always_inline)) { issue_one(ic, kt, stage); }); };
+    auto issue = [&](auto plain_c, int kt, int stage) __attribute__((always_inline)) {
+        static_for<0, LPT>([&](auto ic) __attribute__((always_inline)) { issue_one(ic, plain_c, kt, stage); });
+    };
+    constexpr std::true_type YES{};
+    constexpr std::false_type NO{};
     // step kt has landed for every wave: zeros behind the end of its rows, if they end in it
     auto cut = [&](int kt, int stage) __attribute__((always_inline)) {
         const bool low = KIND == LIN_ADAPT && kt >= nk;
@@ -150,7 +152,7 @@ __global__ void __launch_bounds__(WM * WN * 64) linear_tile_kernel(const LinArgs
 
 #pragma unroll
     for (int t = 0; t < NS - 1; ++t)
-        if (t < bound) issue(t, t);
+        if (t < bound) issue(NO, t, t);
     if (tid < BN) {
         int n = tid;
         if constexpr (KIND == LIN_GLU) n = n / 32 * 16 + n % 16;
@@ -169,10 +171,13 @@ __global__ void __launch_bounds__(WM * WN * 64) linear_tile_kernel(const LinArgs
     cut(0, 0);
     static_for<0, NI * MI>([&](auto pc) __attribute__((always_inline)) { constexpr int p = decltype(pc)::value; hold_acc<false>(acc[p / MI][p % MI]); });
     settle_mfma();
-    if (NS - 1 < bound) issue(NS - 1, NS - 1);
+    if (NS - 1 < bound) issue(NO, NS - 1, NS - 1);
     static_for<0, D>([&](auto pc) { fetch(pc, a_addr, w_addr); });
     int cs = 0;                                     // stage of step kt
-    for (int kt = 0; kt < bound; ++kt) {
+    // One step.  PLAIN: the copies that it starts are of plain steps, and there are some.  (Where a lane's offset is made anew for a copy, the copy has to have read it before
+    // the register can take a fragment: 0.2 us a step, so the other steps are a loop of their own.)
+    auto step = [&](auto plain_c, int kt) __attribute__((always_inline)) {
+        constexpr bool PLAIN = decltype(plain_c)::value;
         const int ns = cs + 1 == NS ? 0 : cs + 1;
         const uint32_t co = (uint32_t)cs * (uint32_t)STAGE, no = (uint32_t)ns * (uint32_t)STAGE;
         uint32_t ca[2], cw[2], na[2], nw[2];
@@ -182,18 +187,20 @@ __global__ void __launch_bounds__(WM * WN * 64) linear_tile_kernel(const LinArgs
             constexpr int g = decltype(gc)::value;
             if constexpr (g + D == G) {
                 // step kt + 1 has landed and this wave's reads of step kt are complete, for every wave after the barrier: kt's stage may be filled again
-                if (NS > 2 && kt + NS - 1 < bound) wait_vmcnt<LPT * (NS - 2)>(); else wait_vmcnt<0>();
+                if (NS > 2 && (PLAIN || kt + NS - 1 < bound)) wait_vmcnt<LPT * (NS - 2)>(); else wait_vmcnt<0>();
                 asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-                if (kt + 1 < bound) cut(kt + 1, ns);
+                if constexpr (!PLAIN) {
+                    if (kt + 1 < bound) cut(kt + 1, ns);
+                }
                 if constexpr (!kSpread) {
-                    if (kt + NS < bound) issue(kt + NS, cs);
+                    if (PLAIN || kt + NS < bound) issue(plain_c, kt + NS, cs);
                 }
             }
             if constexpr (kSpread) {
                 if constexpr (g >= G - D && g - (G - D) < HEAD) {
-                    if (kt + NS < bound) issue_one(std::integral_constant<int, g - (G - D)>{}, kt + NS, cs);
+                    if (PLAIN || kt + NS < bound) issue_one(std::integral_constant<int, g - (G - D)>{}, plain_c, kt + NS, cs);
                 } else if constexpr (g < G - D && g < TAIL) {
-                    if (kt >= 1 && kt + 1 < bound) issue_one(std::integral_constant<int, HEAD + g>{}, kt + 1, ns);
+                    if (kt >= 1 && (PLAIN || kt + 1 < bound)) issue_one(std::integral_constant<int, HEAD + g>{}, plain_c, kt + 1, ns);
                 }
             }
             // (in the last step the positions beyond it read the idle stage: LDS that is there, values unused)
@@ -210,7 +217,10 @@ __global__ void __launch_bounds__(WM * WN * 64) linear_tile_kernel(const LinArgs
             __builtin_amdgcn_sched_barrier(0);
         });
         cs = ns;
-    }
+    };
+    int kt = 0;
+    for (const int plain = nk - (chunks ? 1 : 0) - NS; kt < plain; ++kt) step(YES, kt);
+    for (; kt < bound; ++kt) step(NO, kt);
     // the last look-ahead reads are on their way into the fragment registers: they pass through the wait
     wait_frag<0>(fw[0]);
     settle_mfma();
@@ -224,51 +234,8 @@ __global__ void __launch_bounds__(WM * WN * 64) linear_tile_kernel(const LinArgs
         if (!a.in_loop) add_adapters(acc, a, group, row0 + wm * TM, n0 + wn * TN);
     }
 
-    // ---- bias and activation, then in whole rows through LDS of the wave's own: acc[i][j][r] is (row 16 j + l16, weight row 16 i + 4 quarter + r)
     asm volatile("s_barrier" ::: "memory");         // every wave has read its last fragments
-    unsigned char* wbuf = smem + wave * (PASS * PITCH);
-    const int nc = n0 + wn * ON;
-#pragma unroll
-    for (int p = 0; p < TM / PASS; ++p) {
-#pragma unroll
-        for (int i = 0; i < NI; i += KIND == LIN_GLU ? 2 : 1) {
-            const f32x4 b0 = *reinterpret_cast<const f32x4*>(bias + wn * TN + i * 16 + 4 * quarter);
-            f32x4 b1 = b0;
-            if constexpr (KIND == LIN_GLU) b1 = *reinterpret_cast<const f32x4*>(bias + wn * TN + (i + 1) * 16 + 4 * quarter);
-#pragma unroll
-            for (int jj = 0; jj < PASS / 16; ++jj) {
-                const int j = p * (PASS / 16) + jj;
-                __builtin_amdgcn_sched_barrier(0);  // (pieces computed far ahead of their stores would spill)
-                f32x4 v = acc[i][j] + b0;
-                if constexpr (KIND == LIN_GLU) {
-                    const f32x4 u = acc[i + 1][j] + b1;
-                    if (a.act == DRF_GLU_GELU)
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) v[r] = glu(v[r], u[r], DRF_GLU_GELU);
-                    else
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) v[r] = glu(v[r], u[r], DRF_GLU_SILU);
-                }
-                const bf16x4 o = { (bf16_t)v[0], (bf16_t)v[1], (bf16_t)v[2], (bf16_t)v[3] };
-                *reinterpret_cast<bf16x4*>(wbuf + (jj * 16 + l16) * PITCH + (KIND == LIN_GLU ? i / 2 : i) * 32 + quarter * 8) = o;
-            }
-        }
-#pragma unroll 4
-        for (int id = lane; id < PASS * CH; id += 64) {
-            const int r = id / CH, c = id - r * CH, n = nc + c * 8;
-            const uint32_t at = out_at[wm * TM + p * PASS + r];
-            const u32x4 v = *reinterpret_cast<const u32x4*>(wbuf + r * PITCH + c * 16);
-            if (at == 0xffffffffu || n >= a.N) continue;
-            bf16_t* o = reinterpret_cast<bf16_t*>(out0 + at) + n;
-            if (a.out_vec && n + 8 <= a.N) *reinterpret_cast<u32x4*>(o) = v;
-            else {
-                const bf16x8 e = __builtin_bit_cast(bf16x8, v);
-#pragma unroll
-                for (int k = 0; k < 8; ++k)
-                    if (n + k < a.N) o[k] = e[k];
-            }
-        }
-    }
+    store_wave_tile<MI, NI, KIND, PASS, PITCH, CH>(acc, a, bias + wn * TN, out_at + wm * TM, out0, n0 + wn * ON, smem + wave * (PASS * PITCH));
 }
 
 template <int BM, int BN, int NS, int WM, int WN, int KIND> drf_status launch_tile_shape(LinArgs a, hipStream_t st)
@@ -297,7 +264,12 @@ template <int KIND> drf_status launch_linear_tile(int tile, const LinArgs& a, hi
     case 3: return launch_tile_shape<128, 128, 2, 4, 2, KIND>(a, st);
     case 4: return launch_tile_shape<128, 64, 3, 2, 2, KIND>(a, st);
     case 5: return launch_tile_shape<64, 128, 3, 2, 2, KIND>(a, st);
-    default: return launch_tile_shape<64, 64, 4, 2, 2, KIND>(a, st);
+    case 6: return launch_tile_shape<64, 64, 4, 2, 2, KIND>(a, st);
+    case 7: return launch_tile_shape<64, 64, 8, 2, 2, KIND>(a, st);
+    case 8: return launch_wide_shape<256, KIND>(a, st);
+    default:
+        if constexpr (KIND == LIN_GLU) DRF_FAIL(DRF_EINVAL, "no such tile");
+        else return launch_wide_shape<288, KIND>(a, st);
     }
 }
 
