@@ -261,12 +261,10 @@ template <int KIND> drf_status launch_linear_tile(int tile, const LinArgs& a, hi
     case 0: return launch_tile_shape<256, 256, 2, 4, 2, KIND>(a, st);
     case 1: return launch_tile_shape<256, 128, 3, 4, 2, KIND>(a, st);
     case 2: return launch_tile_shape<128, 128, 4, 4, 2, KIND>(a, st);
-    case 3: return launch_tile_shape<128, 128, 2, 4, 2, KIND>(a, st);
-    case 4: return launch_tile_shape<128, 64, 3, 2, 2, KIND>(a, st);
-    case 5: return launch_tile_shape<64, 128, 3, 2, 2, KIND>(a, st);
-    case 6: return launch_tile_shape<64, 64, 4, 2, 2, KIND>(a, st);
-    case 7: return launch_tile_shape<64, 64, 8, 2, 2, KIND>(a, st);
-    case 8: return launch_wide_shape<256, KIND>(a, st);
+    case 3: return launch_tile_shape<128, 64, 3, 2, 2, KIND>(a, st);
+    case 4: return launch_tile_shape<64, 128, 3, 2, 2, KIND>(a, st);
+    case 5: return launch_tile_shape<64, 64, 4, 2, 2, KIND>(a, st);
+    case 6: return launch_wide_shape<256, KIND>(a, st);
     default:
         if constexpr (KIND == LIN_GLU) DRF_FAIL(DRF_EINVAL, "no such tile");
         else return launch_wide_shape<288, KIND>(a, st);
