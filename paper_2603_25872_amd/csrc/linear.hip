@@ -7,62 +7,112 @@
 //
 // This file has the entry points, the choice of a tile, x A^T and all of fp32; bf16 products run on the tiles of linear_tile.h.  The weights are the matrix
 // instruction's first operand throughout: a lane ends with four consecutive columns of one row.
-#include "linear_device.h"
+#include "linear_direct.h"
 #include "../../include/drf_measure.h"
 
 namespace drf {
 
 namespace {
 
+constexpr int kMaxTokenStride = 1 << 22;           // 256 rows within 2^31 bytes
+
+// Tiles and a time model of a launch of each: base + (per round of workgroups) round + steps * max(lat, c * thr) us, where a round is per_cu workgroups on each of 256
+// CUs and c those that share a CU in it.  Least-squares fits to 220 products (16 to 65536 rows, 64 to 9600 columns, an inner axis of 72 to 4800, weights cold);
+// the choice by it is within 1 % of the best tile on average, 35 % behind at worst.
+struct Tile { int bm, bn, per_cu; double base, round, lat, thr; };
+const Tile kLinTiles[] = { { 256, 256, 1, 0.00, 8.15, 1.317, 0 }, { 256, 128, 1, 0.00, 6.01, 0.847, 0 }, { 128, 128, 1, 0.40, 4.08, 0.549, 0 }, { 128, 64, 2, 1.55, 3.36, 0.386, 0.376 },
+                           { 64, 128, 2, 1.45, 3.54, 0.385, 0.347 }, { 64, 64, 2, 1.30, 2.97, 0.274, 0.213 }, { 256, 256, 1, 0.00, 11.7, 1.099, 0 }, { 256, 288, 1, 0.00, 13.6, 1.188, 0 } };
+constexpr int kTiles = sizeof(kLinTiles) / sizeof(kLinTiles[0]);
+// The forms for few rows of linear_direct.h, rows and weight rows a workgroup in sixteens and its waves: fixed + turns * turn + max(0, workgroups / 256 - hidden) * (group + 128-byte
+// pieces of the inner axis * piece) us, fitted likewise (250 and 200 products of 1 to 4096 rows; the choice is within 4 % of the best on average in bf16, 1 % in fp32).
+struct Form { int mi, ni, nw; double fixed, turn, hidden, group, piece; };
+constexpr int kForms = 4;
+const Form kFormsBf16[kForms] = { { 1, 1, 16, 1.79, 1.14, 0.27, 1.22, 0.089 }, { 1, 4, 8, 1.80, 1.48, 0.0, 0.88, 0.236 }, { 2, 2, 8, 2.11, 0.97, 0.0, 0.89, 0.191 }, { 4, 2, 8, 2.60, 1.41, 0.19, 1.76, 0.309 } };
+const Form kFormsF32[kForms] = { { 1, 1, 16, 1.87, 1.36, 0.27, 1.41, 0.103 }, { 1, 4, 8, 2.06, 2.24, 0.20, 1.43, 0.321 }, { 2, 2, 8, 2.32, 1.82, 0.35, 1.53, 0.261 }, { 4, 2, 8, 2.27, 3.25, 0.42, 2.83, 0.466 } };
+const Tile kTileF32 = { 64, 64, 4, 0.0, 3.60, 0.700, 0.634 };      // steps of 32
+
+double tile_us(const Tile& m, long long tiles, int steps)
+{
+    const long long full = tiles / (256 * m.per_cu), share = (tiles - full * 256 * m.per_cu + 255) / 256;
+    return m.base + full * (m.round + steps * std::max(m.lat, m.per_cu * m.thr)) + (share ? m.round + steps * std::max(m.lat, share * m.thr) : 0.0);
+}
+
+// The form with the least modelled time, and that time.
+template <typename T, int KIND> int pick_form(const LinArgs& a, double* us)
+{
+    const Form* forms = sizeof(T) == 2 ? kFormsBf16 : kFormsF32;
+    const long long rows = (long long)a.slots * a.tokens, weight_rows = KIND == LIN_GLU ? 2LL * a.N : a.N;
+    const int pieces = (a.K * (int)sizeof(T) + 127) / 128;
+    int best = 0;
+    *us = 1e300;
+    for (int f = 0; f < kForms; ++f) {
+        const Form& m = forms[f];
+        const double groups = (double)((rows + 16 * m.mi - 1) / (16 * m.mi)) * ((weight_rows + 16 * m.ni - 1) / (16 * m.ni));
+        double t = m.fixed + (pieces + m.nw - 1) / m.nw * m.turn + std::max(0.0, groups / 256 - m.hidden) * (m.group + pieces * m.piece);
+        if (KIND == LIN_ADAPT && a.adapters) t += (0.3 + 0.01 * a.rank) * (1 + groups / 256);
+        if (t < *us) { *us = t; best = f; }
+    }
+    return best;
+}
+thread_local int g_forced_tile = -1;                    // see drf_probe_linear_tile
+
 // ---- x A^T ------------------------------------------------------------------------------------------------
-// bf16: 16 MI rows of one slot by 32 of the rank's columns a workgroup, operands straight to registers, the inner axis dealt over NW waves that add up
-// through LDS.  Reads x once for every 32 columns of the rank; bound by that.  The sums go out as two bf16 operands: the upper 8 bits of the fp32 value and
-// the rest rounded to 8 (2^-16 of the value is lost); one that is no number is itself and zero.
-template <int MI, int NW>
+// 16 MI rows of one slot by 32 of the rank's columns a workgroup, operands straight to registers, the inner axis dealt over NW waves, 128 bytes of it at a
+// time with U turns on the way, that add up through LDS.  Reads x once for every 32 columns of the rank; bound by that.  fp32 sums go out as they are, for bf16
+// as two operands: the upper 8 bits of the fp32 value and the rest rounded to 8 (2^-16 of the value is lost); one that is no number is itself and zero.
+template <typename T, int MI, int NW, int U>
 __global__ void __launch_bounds__(NW * 64) adapters_low_kernel(const LinArgs a)
 {
-    constexpr int U = 4;
+    constexpr int E = 16 / sizeof(T), CHUNK = 8 * E, TURN = NW * CHUNK;
     __shared__ f32x4 part[NW][2 * MI][64];
     const int lane = threadIdx.x & 63, l16 = lane & 15, quarter = lane >> 4, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const long long id = a.first + blockIdx.x;
-    const int parts = a.low_cols / 32, slot = (int)(id / ((long long)a.slot_tiles * parts)), in = (int)(id - (long long)slot * a.slot_tiles * parts);
+    const int parts = (a.rank + 31) / 32, slot = (int)(id / ((long long)a.slot_tiles * parts)), in = (int)(id - (long long)slot * a.slot_tiles * parts);
     const int tile = in / parts, r0 = (in - tile * parts) * 32, row0 = tile * 16 * MI;
     const int ad = adapter_of(a, slot), len = slot_len(a.lens, slot, a.tokens);
     if (ad < 0 || row0 >= len) return;
-    const bf16_t *x[MI], *w[2];
+    const T *x[MI], *w[2];
 #pragma unroll
     for (int j = 0; j < MI; ++j) {
         const int token = row0 + 16 * j + l16;
-        x[j] = (const bf16_t*)a.x.data + slot * a.x.slot_stride + (token < len ? token : row0) * a.x.token_stride + 8 * quarter;
+        x[j] = (const T*)a.x.data + slot * a.x.slot_stride + (token < len ? token : row0) * a.x.token_stride;
     }
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
         const int r = r0 + 16 * i + l16;
-        w[i] = (const bf16_t*)a.a + ((size_t)ad * a.rank + (r < a.rank ? r : a.rank - 1)) * a.K + 8 * quarter;
+        w[i] = (const T*)a.a + ((size_t)ad * a.rank + (r < a.rank ? r : a.rank - 1)) * a.K;
     }
     f32x4 acc[2][MI];
 #pragma unroll
     for (int i = 0; i < 2; ++i)
 #pragma unroll
         for (int j = 0; j < MI; ++j) acc[i][j] = (f32x4){ 0.f, 0.f, 0.f, 0.f };
-    const u32x4 zero = { 0, 0, 0, 0 };
-    for (int k0 = wave * 32; k0 < a.K; k0 += NW * 32 * U) {
-        u32x4 fx[U][MI], fw[U][2];
+    u32x4 fx[U][2][MI], fw[U][2][2];
+    auto load = [&](int t, int k0) __attribute__((always_inline)) {
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int k = k0 + u * NW * 32;
-            const bool in_row = k + 8 * quarter < a.K;
+        for (int h = 0; h < 2; ++h) {
+            const int k = k0 + (4 * h + quarter) * E;
 #pragma unroll
-            for (int j = 0; j < MI; ++j) fx[u][j] = in_row ? *reinterpret_cast<const u32x4*>(x[j] + k) : zero;
+            for (int j = 0; j < MI; ++j) fx[t][h][j] = load_row16(x[j], k, a.K);
 #pragma unroll
-            for (int i = 0; i < 2; ++i) fw[u][i] = in_row ? *reinterpret_cast<const u32x4*>(w[i] + k) : zero;
+            for (int i = 0; i < 2; ++i) fw[t][h][i] = load_row16(w[i], k, a.K);
         }
+    };
 #pragma unroll
-        for (int u = 0; u < U; ++u)
+    for (int t = 0; t < U; ++t)
+        if (wave * CHUNK + t * TURN < a.K) load(t, wave * CHUNK + t * TURN);
+    for (int k = wave * CHUNK; k < a.K; k += U * TURN) {
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
+        for (int t = 0; t < U; ++t) {
+            if (k + t * TURN < a.K)
 #pragma unroll
-                for (int j = 0; j < MI; ++j) acc[i][j] = mma_bf16(fw[u][i], fx[u][j], acc[i][j]);
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i)
+#pragma unroll
+                        for (int j = 0; j < MI; ++j) acc[i][j] = mma(fw[t][h][i], fx[t][h][j], acc[i][j], T{});
+            if (k + (U + t) * TURN < a.K) load(t, k + (U + t) * TURN);
+        }
     }
 #pragma unroll
     for (int i = 0; i < 2; ++i)
@@ -75,189 +125,208 @@ __global__ void __launch_bounds__(NW * 64) adapters_low_kernel(const LinArgs a)
         f32x4 v = part[0][p][lane];
 #pragma unroll
         for (int w2 = 1; w2 < NW; ++w2) v += part[w2][p][lane];
-        bf16x4 hi, lo;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const float t = r + e < a.rank ? v[e] * scale : 0.f;
-            const float top = __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, t) & 0xffff0000u);
-            const bool fine = fabsf(t) < INFINITY;
-            hi[e] = (bf16_t)(fine ? top : t);
-            lo[e] = (bf16_t)(fine ? t - top : 0.f);
-        }
         if (token >= len) continue;
-        bf16_t* o = (bf16_t*)a.low + ((size_t)slot * a.tokens + token) * 2 * a.low_cols + r;
-        *reinterpret_cast<bf16x4*>(o) = hi;
-        *reinterpret_cast<bf16x4*>(o + a.low_cols) = lo;
+        const size_t row = (size_t)slot * a.tokens + token;
+        if constexpr (sizeof(T) == 4) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (r + e < a.rank) ((float*)a.low)[row * a.low_cols + r + e] = v[e] * scale;
+        } else {
+            bf16x4 hi, lo;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float t = r + e < a.rank ? v[e] * scale : 0.f;
+                const float top = __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, t) & 0xffff0000u);
+                const bool fine = fabsf(t) < INFINITY;
+                hi[e] = (bf16_t)(fine ? top : t);
+                lo[e] = (bf16_t)(fine ? t - top : 0.f);
+            }
+            bf16_t* o = (bf16_t*)a.low + row * 2 * a.low_cols + r;
+            *reinterpret_cast<bf16x4*>(o) = hi;
+            *reinterpret_cast<bf16x4*>(o + a.low_cols) = lo;
+        }
     }
 }
 
-template <int MI, int NW> drf_status launch_low(LinArgs a, hipStream_t st)
+template <typename T, int MI, int NW, int U> drf_status launch_low(LinArgs a, hipStream_t st)
 {
     a.slot_tiles = (a.tokens + 16 * MI - 1) / (16 * MI);
-    a.tiles = (long long)a.slots * a.slot_tiles * (a.low_cols / 32);
+    a.tiles = (long long)a.slots * a.slot_tiles * ((a.rank + 31) / 32);
     const long long most = 1 << 22;                                 // (a launch holds fewer than 2^32 threads)
     for (a.first = 0; a.first < a.tiles; a.first += most) {
-        hipLaunchKernelGGL((adapters_low_kernel<MI, NW>), dim3((unsigned)std::min(most, a.tiles - a.first)), dim3(NW * 64), 0, st, a);
+        hipLaunchKernelGGL((adapters_low_kernel<T, MI, NW, U>), dim3((unsigned)std::min(most, a.tiles - a.first)), dim3(NW * 64), 0, st, a);
         DRF_HIP(hipGetLastError());
     }
     return DRF_OK;
 }
 
-// ---- fp32 -------------------------------------------------------------------------------------------------
-// Tiles of 64 rows by 64 rows of the weights on four waves, a wave 32 x 32; 16 elements of the inner axis a step, staged in LDS through registers a step
-// ahead.  LIN_LOW: x A^T of one slot.
-constexpr int LIN_LOW = 3;
-
-// c += w . x over 16 elements of the inner axis, a lane's four each
-__device__ inline void multiply(f32x4& c, const u32x4& w, const u32x4& x)
+template <typename T> drf_status run_low(const LinArgs& a, hipStream_t st)
 {
-    const f32x4 a = __builtin_bit_cast(f32x4, w), b = __builtin_bit_cast(f32x4, x);
-#pragma unroll
-    for (int k = 0; k < 4; ++k) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[k], b[k], c, 0, 0, 0);
+    return a.tokens <= 16 ? launch_low<T, 1, 8, 3>(a, st) : (long long)a.slots * ((a.tokens + 63) / 64) < 512 ? launch_low<T, 2, 8, 3>(a, st) : launch_low<T, 4, 4, 3>(a, st);
 }
 
+// ---- fp32 -------------------------------------------------------------------------------------------------
+// Tiles of 64 rows by 64 rows of the weights on four waves, a wave 32 x 32; 32 elements of the inner axis a step, staged in LDS through registers DEPTH steps ahead, 16
+// bytes at a time at any address.  Bound by the matrix unit where it has enough tiles: 2241 x 3502 x 2153 319 us (106 of 157 TFLOP/s; 128 x 128 tiles 297, but slower below).
 template <int KIND>
 __global__ void __launch_bounds__(256) linear_f32_kernel(const LinArgs a)
 {
-    constexpr int E = 4, BK = 16, PITCH = 80;                       // bytes of a row of 64 in LDS: 16 rows on distinct banks
-    __shared__ __attribute__((aligned(16))) unsigned char stage[2][128 * PITCH];
+    constexpr int W = 2, DEPTH = 2, BM = 32 * W, PITCH = 144, Q = BM / 32;       // pieces of a wave's side; bytes of a row of 128 in LDS; pieces of a thread
+    __shared__ __attribute__((aligned(16))) unsigned char stage[2 * 2 * BM * PITCH];
     const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, quarter = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave & 1, wn = wave >> 1;
     const long long id = a.first + blockIdx.x;
     const int tm = (int)(id / a.tiles_n), tn = (int)(id - (long long)tm * a.tiles_n);
-    const int group = tm / a.slot_tiles, row0 = (tm - group * a.slot_tiles) * 64, n0 = tn * (KIND == LIN_GLU ? 32 : 64);
-    // rows that are not there are read as the tile's first and not stored
-    int adapter = -1;
-    if constexpr (KIND == LIN_LOW) {
-        adapter = adapter_of(a, group);
-        if (adapter < 0) return;
-    }
-    if (a.slot_rows == a.tokens && row0 >= slot_len(a.lens, group, a.tokens)) return;
+    const int row0 = tm * BM, n0 = tn * (KIND == LIN_GLU ? BM / 2 : BM);
+    if (a.slots == 1 && row0 >= slot_len(a.lens, 0, a.tokens)) return;
 
-    // staging: thread t copies the 16-byte pieces t % 4 of rows t / 4 of the activations and of the weights
-    const int sr = tid >> 2, sc = (tid & 3) * E;
-    int s_slot, s_token;
-    if (!locate_row(a, group, row0 + sr, s_slot, s_token)) locate_row(a, group, row0, s_slot, s_token);
-    const float* xr = (const float*)a.x.data + s_slot * a.x.slot_stride + s_token * a.x.token_stride;
-    const float* wr = (const float*)a.w;
-    if constexpr (KIND == LIN_GLU) {
-        int n = n0 + sr / 32 * 16 + sr % 16;
+    // staging: thread t copies piece t % 8 of rows t / 8 + 32 i of the activations and of the weights; rows that are not there are read as slot 0's first and not stored
+    const float *xr[Q], *wr[Q];
+    const int sc = (tid & 7) * 4;
+#pragma unroll
+    for (int i = 0; i < Q; ++i) {
+        const int r = tid / 8 + 32 * i;
+        int slot, token;
+        locate_row(a, 0, row0 + r, slot, token);
+        if (row0 + r >= a.slot_rows) slot = token = 0;
+        xr[i] = (const float*)a.x.data + slot * a.x.slot_stride + token * a.x.token_stride + sc;
+        int n = n0 + (KIND == LIN_GLU ? r / 32 * 16 + r % 16 : r);
         n = n < a.N ? n : a.N - 1;
-        wr += ((size_t)n + (sr / 16 % 2 ? a.N : 0)) * a.K;
-    } else {
-        int n = n0 + sr;
-        n = n < a.N ? n : a.N - 1;
-        wr += (KIND == LIN_LOW ? (size_t)adapter * a.N * a.K : 0) + (size_t)n * a.K;
+        wr[i] = (const float*)a.w + ((size_t)n + (KIND == LIN_GLU && r / 16 % 2 ? a.N : 0)) * a.K + sc;
     }
-    u32x4 px, pw;
-    auto fetch = [&](int k) { px = load16(xr, k + sc, a.K, a.in_vec); pw = load16(wr, k + sc, a.K, a.in_vec); };
-    auto put = [&](int s) {
-        *reinterpret_cast<u32x4*>(&stage[s][sr * PITCH + (tid & 3) * 16]) = px;
-        *reinterpret_cast<u32x4*>(&stage[s][(64 + sr) * PITCH + (tid & 3) * 16]) = pw;
+    typedef float piece __attribute__((ext_vector_type(4), aligned(4)));
+    u32x4 px[DEPTH][Q], pw[DEPTH][Q];
+    auto fetch = [&](int d, int s) __attribute__((always_inline)) {
+        if (s * 32 + 32 <= a.K) {
+#pragma unroll
+            for (int i = 0; i < Q; ++i) {
+                px[d][i] = __builtin_bit_cast(u32x4, *reinterpret_cast<const piece*>(xr[i] + s * 32));
+                pw[d][i] = __builtin_bit_cast(u32x4, *reinterpret_cast<const piece*>(wr[i] + s * 32));
+            }
+        } else
+#pragma unroll
+            for (int i = 0; i < Q; ++i) {
+                px[d][i] = load_row16(xr[i] - sc, s * 32 + sc, a.K);
+                pw[d][i] = load_row16(wr[i] - sc, s * 32 + sc, a.K);
+            }
     };
-    f32x4 acc[2][2];                                                // [weight piece][activation piece]
+    auto put = [&](int d, int s) __attribute__((always_inline)) {
+        unsigned char* st = stage + (s & 1) * 2 * BM * PITCH + (tid & 7) * 16;
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int j = 0; j < 2; ++j) acc[i][j] = (f32x4){ 0.f, 0.f, 0.f, 0.f };
-    const int steps = (a.K + BK - 1) / BK;
-    fetch(0);
-    put(0);
-    __syncthreads();
-    for (int s = 0; s < steps; ++s) {
-        if (s + 1 < steps) fetch((s + 1) * BK);
-        const unsigned char* st = stage[s & 1];
-        u32x4 fx[2], fw[2];
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            fx[i] = *reinterpret_cast<const u32x4*>(st + (wm * 32 + i * 16 + l16) * PITCH + quarter * 16);
-            fw[i] = *reinterpret_cast<const u32x4*>(st + (64 + wn * 32 + i * 16 + l16) * PITCH + quarter * 16);
+        for (int i = 0; i < Q; ++i) {
+            *reinterpret_cast<u32x4*>(st + (tid / 8 + 32 * i) * PITCH) = px[d][i];
+            *reinterpret_cast<u32x4*>(st + (BM + tid / 8 + 32 * i) * PITCH) = pw[d][i];
         }
+    };
+    f32x4 acc[W][W];                                                // [weight piece][activation piece]
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+    for (int i = 0; i < W; ++i)
 #pragma unroll
-            for (int j = 0; j < 2; ++j) multiply(acc[i][j], fw[i], fx[j]);
-        if (s + 1 < steps) put((s + 1) & 1);
-        __syncthreads();
-    }
-
-    int slot[2], token[2];
-    bool live[2];
+        for (int j = 0; j < W; ++j) acc[i][j] = (f32x4){ 0.f, 0.f, 0.f, 0.f };
+    const int steps = (a.K + 31) / 32;
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-        live[j] = locate_row(a, group, row0 + wm * 32 + j * 16 + l16, slot[j], token[j]);
-        if (!live[j]) slot[j] = token[j] = 0;
-    }
-    if constexpr (KIND == LIN_ADAPT) {
-        int first, last, t;
-        locate_row(a, group, row0, first, t);
-        locate_row(a, group, std::min(row0 + 64, a.slot_rows) - 1, last, t);
-        for (int s = first; s <= last; ++s) {                       // (the same for the whole workgroup)
-            const int i = adapter_of(a, s);
-            if (i < 0) continue;
-            const float* b = (const float*)a.b + (size_t)i * a.N * a.rank;
-            // into sums of its own, of which the slot's rows take theirs: an infinite weight of one adapter is nothing to the rows of another
-            f32x4 sum[2][2];
+    for (int d = 0; d < DEPTH; ++d)
+        if (d < steps) fetch(d, d);
+    for (int s0 = 0; s0 < steps; s0 += DEPTH) {
 #pragma unroll
-            for (int p = 0; p < 2; ++p)
+        for (int d = 0; d < DEPTH; ++d) {
+            const int s = s0 + d;
+            if (s >= steps) break;
+            put(d, s);
+            __syncthreads();                                        // (the other stage is written again only behind the next one)
+            if (s + DEPTH < steps) fetch(d, s + DEPTH);
+            const unsigned char* st = stage + (s & 1) * 2 * BM * PITCH;
 #pragma unroll
-                for (int j = 0; j < 2; ++j) sum[p][j] = (f32x4){ 0.f, 0.f, 0.f, 0.f };
-            for (int k = 0; k < a.rank; k += BK) {
-                u32x4 fw[2], fx[2];
+            for (int h = 0; h < 2; ++h) {
+                u32x4 fx[W], fw[W];
 #pragma unroll
-                for (int p = 0; p < 2; ++p) {
-                    int n = n0 + wn * 32 + p * 16 + l16;
-                    n = n < a.N ? n : a.N - 1;
-                    fw[p] = load16(b + (size_t)n * a.rank, k + quarter * E, a.rank, a.b_vec);
-                    fx[p] = (u32x4){ 0, 0, 0, 0 };
-                    if (live[p] && slot[p] == s) fx[p] = load16((const float*)a.low + ((size_t)slot[p] * a.tokens + token[p]) * a.low_cols, k + quarter * E, a.rank, a.b_vec);
+                for (int i = 0; i < W; ++i) {
+                    fx[i] = *reinterpret_cast<const u32x4*>(st + (wm * 16 * W + i * 16 + l16) * PITCH + (4 * h + quarter) * 16);
+                    fw[i] = *reinterpret_cast<const u32x4*>(st + (BM + wn * 16 * W + i * 16 + l16) * PITCH + (4 * h + quarter) * 16);
                 }
 #pragma unroll
-                for (int p = 0; p < 2; ++p)
+                for (int k = 0; k < 4; ++k)
 #pragma unroll
-                    for (int j = 0; j < 2; ++j) multiply(sum[p][j], fw[p], fx[j]);
+                    for (int i = 0; i < W; ++i)
+#pragma unroll
+                        for (int j = 0; j < W; ++j)
+                            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(__builtin_bit_cast(f32x4, fw[i])[k], __builtin_bit_cast(f32x4, fx[j])[k], acc[i][j], 0, 0, 0);
             }
-#pragma unroll
-            for (int p = 0; p < 2; ++p)
-#pragma unroll
-                for (int j = 0; j < 2; ++j)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) acc[p][j][r] += slot[j] == s ? sum[p][j][r] : 0.f;
         }
     }
 
-    // acc[i][j][r] is (row 16 j + l16, column 16 i + 4 quarter + r) of the wave's tile
+    int slot[W], token[W];
+    bool live[W];
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
+    for (int j = 0; j < W; ++j) {
+        live[j] = locate_row(a, 0, row0 + (wm * W + j) * 16 + l16, slot[j], token[j]);
+        if (!live[j]) slot[j] = token[j] = 0;
+    }
+    if (KIND == LIN_ADAPT && a.adapters) {
+        int first, last, t;
+        locate_row(a, 0, row0 + wm * 16 * W, first, t);
+        locate_row(a, 0, std::min(row0 + (wm + 1) * 16 * W, a.slot_rows) - 1, last, t);
+        for (int s = first; s <= last; ++s) {                       // (the same for the whole wave)
+            const int ad = adapter_of(a, s);
+            if (ad < 0) continue;
+            const float* b = (const float*)a.b + (size_t)ad * a.N * a.rank;
+            // into sums of its own, of which the slot's rows take theirs: an infinite weight of one adapter is nothing to the rows of another
+#pragma unroll
+            for (int j = 0; j < W; ++j) {
+                f32x4 sum[W];
+#pragma unroll
+                for (int i = 0; i < W; ++i) sum[i] = (f32x4){ 0.f, 0.f, 0.f, 0.f };
+                for (int k = 0; k < a.rank; k += 16) {
+                    u32x4 fx = { 0, 0, 0, 0 };
+                    if (live[j] && slot[j] == s) fx = load_row16((const float*)a.low + ((size_t)slot[j] * a.tokens + token[j]) * a.low_cols, k + quarter * 4, a.rank);
+#pragma unroll
+                    for (int i = 0; i < W; ++i) {
+                        int n = n0 + (wn * W + i) * 16 + l16;
+                        n = n < a.N ? n : a.N - 1;
+                        sum[i] = mma(load_row16(b + (size_t)n * a.rank, k + quarter * 4, a.rank), fx, sum[i], 0.f);
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < W; ++i)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) acc[i][j][r] += slot[j] == s ? sum[i][r] : 0.f;
+            }
+        }
+    }
+
+    // acc[i][j][r] is (row 16 j + l16, weight row 16 i + 4 quarter + r) of the wave's tile
+#pragma unroll
+    for (int j = 0; j < W; ++j) {
         if (!live[j]) continue;
         float* o = (float*)a.out.data + slot[j] * a.out.slot_stride + token[j] * a.out.token_stride;
 #pragma unroll
-        for (int i = 0; i < (KIND == LIN_GLU ? 1 : 2); ++i) {
-            const int n = n0 + (KIND == LIN_GLU ? wn * 16 : wn * 32 + i * 16) + 4 * quarter;
+        for (int i = 0; i < W; i += KIND == LIN_GLU ? 2 : 1) {
+            const int n = n0 + (KIND == LIN_GLU ? (wn * W + i) * 8 : (wn * W + i) * 16) + 4 * quarter;
+            f32x4 v = acc[i][j];
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                if (n + r >= a.N) continue;
-                float v = acc[i][j][r];
+                const int c = n + r < a.N ? n + r : a.N - 1;
                 if constexpr (KIND == LIN_GLU) {
-                    float u = acc[1][j][r];
-                    if (a.bias) { v += a.bias[n + r]; u += a.bias[a.N + n + r]; }
-                    v = glu(v, u, a.act);
-                } else if constexpr (KIND == LIN_LOW) {
-                    if (a.scales) v *= a.scales[adapter];
-                } else if (a.bias) v += a.bias[n + r];
-                o[n + r] = v;
+                    float u = acc[i + 1][j][r];
+                    if (a.bias) { v[r] += a.bias[c]; u += a.bias[a.N + c]; }
+                    v[r] = glu(v[r], u, a.act);
+                } else if (a.bias) v[r] += a.bias[c];
             }
+            if (n + 4 <= a.N) *reinterpret_cast<piece*>(o + n) = v;
+            else
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    if (n + r < a.N) o[n + r] = v[r];
         }
     }
 }
 
-template <int KIND> drf_status launch_f32(LinArgs a, bool by_slot, hipStream_t st)
+template <int KIND> drf_status launch_f32_tiles(LinArgs a, hipStream_t st)
 {
-    const int columns = KIND == LIN_GLU ? 32 : 64;
-    a.slot_rows = by_slot ? a.tokens : a.slots * a.tokens;
-    a.slot_tiles = (a.slot_rows + 63) / 64;                         // (at most 2^30 rows)
+    constexpr int BM = 64, columns = KIND == LIN_GLU ? BM / 2 : BM;
+    a.slot_rows = a.slots * a.tokens;
     a.tiles_n = (a.N + columns - 1) / columns;
-    a.tiles = (long long)a.slot_tiles * a.tiles_n * (by_slot ? a.slots : 1);
+    a.tiles = (long long)((a.slot_rows + BM - 1) / BM) * a.tiles_n;     // (at most 2^30 rows)
     const long long most = 1 << 23;                                 // (a launch holds fewer than 2^32 threads)
     for (a.first = 0; a.first < a.tiles; a.first += most) {
         hipLaunchKernelGGL((linear_f32_kernel<KIND>), dim3((unsigned)std::min(most, a.tiles - a.first)), dim3(256), 0, st, a);
@@ -266,18 +335,17 @@ template <int KIND> drf_status launch_f32(LinArgs a, bool by_slot, hipStream_t s
     return DRF_OK;
 }
 
+template <int KIND> drf_status launch_f32(const LinArgs& a, hipStream_t st)
+{
+    double us;
+    const int form = pick_form<float, KIND>(a, &us), forced = g_forced_tile - kTiles;
+    if (forced >= 0 && forced < kForms) return launch_linear_direct<float, KIND>(forced, a, st);
+    const long long tiles = ((long long)a.slots * a.tokens + 63) / 64 * (((KIND == LIN_GLU ? 2LL * a.N : a.N) + 63) / 64);
+    if (forced != kForms && us < tile_us(kTileF32, tiles, (a.K + 31) / 32)) return launch_linear_direct<float, KIND>(form, a, st);
+    return launch_f32_tiles<KIND>(a, st);
+}
+
 // ---- bf16 -------------------------------------------------------------------------------------------------
-
-constexpr int kMaxTokenStride = 1 << 22;           // 256 rows within 2^31 bytes
-
-// Tiles and a time model of a launch of each: base + (per round of workgroups) round + steps * max(lat, c * thr) us, where a round is per_cu workgroups on each of 256
-// CUs and c those that share a CU in it.  Least-squares fits to 220 products (16 to 65536 rows, 64 to 9600 columns, an inner axis of 72 to 4800, weights cold);
-// the choice by it is within 1 % of the best tile on average, 35 % behind at worst.
-struct Tile { int bm, bn, per_cu; double base, round, lat, thr; };
-const Tile kLinTiles[] = { { 256, 256, 1, 0.00, 8.15, 1.317, 0 }, { 256, 128, 1, 0.00, 6.01, 0.847, 0 }, { 128, 128, 1, 0.40, 4.08, 0.549, 0 }, { 128, 64, 2, 1.55, 3.36, 0.386, 0.376 },
-                           { 64, 128, 2, 1.45, 3.54, 0.385, 0.347 }, { 64, 64, 2, 1.30, 2.97, 0.274, 0.213 }, { 256, 256, 1, 0.00, 11.7, 1.099, 0 }, { 256, 288, 1, 0.00, 13.6, 1.188, 0 } };
-constexpr int kTiles = sizeof(kLinTiles) / sizeof(kLinTiles[0]);
-thread_local int g_forced_tile = -1;                    // see drf_probe_linear_tile
 
 // Whether tiles of up to 256 rows may cross slots: offsets within one from its first slot on stay below 2^31 bytes.
 bool may_cross(const drf_rows& t, int tokens)
@@ -311,12 +379,16 @@ template <int KIND> drf_status launch_bf16(LinArgs a, hipStream_t st)
         const bool keep = !cross || (KIND == LIN_ADAPT && large && a.adapters);
         if (KIND == LIN_ADAPT && large && a.adapters && !a.b_vec) continue;
         const long long tm = keep ? by_slot : std::min(by_slot, ((long long)a.slots * a.tokens + m.bm - 1) / m.bm);
-        const long long tiles = tm * tn, full = tiles / (256 * m.per_cu), share = (tiles - full * 256 * m.per_cu + 255) / 256;
-        double us = m.base + full * (m.round + steps * std::max(m.lat, m.per_cu * m.thr));
-        if (share) us += m.round + steps * std::max(m.lat, share * m.thr);
+        const bool crosses = !keep && tm < by_slot;
+        double us = tile_us(m, tm * tn, steps + (KIND == LIN_ADAPT && a.adapters && !crosses && a.b_vec ? a.low_cols / 32 : 0));
+        if (KIND == LIN_ADAPT && a.adapters && (crosses || !a.b_vec)) us += (2.0 + 0.05 * a.rank) * (1 + tm * tn / (256 * m.per_cu));
         if (t == g_forced_tile) { best = t; break; }
         if (us < best_us) { best_us = us; best = t; }
     }
+    double form_us;
+    const int form = pick_form<bf16_t, KIND>(a, &form_us), forced = g_forced_tile - kTiles;
+    if (forced >= 0 && forced < kForms) return launch_linear_direct<bf16_t, KIND>(forced, a, st);
+    if (g_forced_tile < 0 && form_us < best_us) return launch_linear_direct<bf16_t, KIND>(form, a, st);
     const Tile& m = kLinTiles[best];
     const int by_slot = a.slots * ((a.tokens + m.bm - 1) / m.bm), crossing = (a.slots * a.tokens + m.bm - 1) / m.bm;
     const bool crosses = cross && crossing < by_slot && !(KIND == LIN_ADAPT && m.bm * m.bn >= 256 * 256 && a.adapters);
@@ -392,37 +464,26 @@ drf_status run_ffn(const drf_gated_ffn_config& c, LinArgs a, void* scratch, hipS
     const bool bf16 = c.dtype == DRF_BF16;
     const drf_rows out = a.out, mid = { scratch, (int64_t)c.tokens * c.hidden, c.hidden };
     a.w = c.w_in; a.bias = c.b_in; a.N = c.hidden; a.K = c.width; a.act = c.act; a.out = mid;
-    a.in_vec = bf16 || (c.width % 4 == 0 && rows_aligned(a.x, 4) && aligned16(c.w_in));
-    const drf_status rc = bf16 ? launch_bf16<LIN_GLU>(a, st) : launch_f32<LIN_GLU>(a, false, st);
+    const drf_status rc = bf16 ? launch_bf16<LIN_GLU>(a, st) : launch_f32<LIN_GLU>(a, st);
     if (rc != DRF_OK) return rc;
     a.x = mid; a.out = out;
     a.w = c.w_out; a.bias = c.b_out; a.N = c.out_width; a.K = c.hidden;
-    a.in_vec = bf16 || (c.hidden % 4 == 0 && aligned16(c.w_out));
-    return bf16 ? launch_bf16<LIN_STORE>(a, st) : launch_f32<LIN_STORE>(a, false, st);
+    return bf16 ? launch_bf16<LIN_STORE>(a, st) : launch_f32<LIN_STORE>(a, st);
 }
 
 drf_status run_adapters(const drf_adapters_config& c, LinArgs a, void* scratch, hipStream_t st)
 {
-    const bool bf16 = c.dtype == DRF_BF16, x_vec = bf16 || (c.width % 4 == 0 && rows_aligned(a.x, 4));
+    const bool bf16 = c.dtype == DRF_BF16;
     a.which = c.which; a.adapters = c.adapters; a.rank = c.rank; a.scales = c.scales; a.a = c.a; a.b = c.b; a.low = scratch;
     a.low_cols = low_columns(c);
-    a.b_vec = aligned16(c.b) && c.rank % (bf16 ? 8 : 4) == 0;
+    a.b_vec = aligned16(c.b) && c.rank % 8 == 0;
     a.K = c.width; a.N = c.out_width;
     if (c.adapters) {
-        drf_status rc;
-        if (bf16) rc = c.tokens <= 16 ? launch_low<1, 8>(a, st) : launch_low<4, 4>(a, st);
-        else {
-            LinArgs l = a;
-            l.out = { scratch, (int64_t)c.tokens * a.low_cols, a.low_cols };
-            l.w = c.a; l.N = c.rank;
-            l.in_vec = x_vec && aligned16(c.a);
-            rc = launch_f32<LIN_LOW>(l, true, st);
-        }
+        const drf_status rc = bf16 ? run_low<bf16_t>(a, st) : run_low<float>(a, st);
         if (rc != DRF_OK) return rc;
     }
     a.w = c.w; a.bias = c.bias;
-    a.in_vec = x_vec && aligned16(c.w);
-    return bf16 ? launch_bf16<LIN_ADAPT>(a, st) : launch_f32<LIN_ADAPT>(a, false, st);
+    return bf16 ? launch_bf16<LIN_ADAPT>(a, st) : launch_f32<LIN_ADAPT>(a, st);
 }
 
 }  // namespace
@@ -480,5 +541,5 @@ extern "C" drf_status drf_linear_adapters(const drf_adapters_config* cfg, const 
 extern "C" int drf_probe_linear_tile(int tile)
 {
     g_forced_tile = tile;
-    return kTiles;
+    return kTiles + kForms + 1;
 }

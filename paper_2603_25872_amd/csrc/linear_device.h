@@ -21,7 +21,7 @@ struct LinArgs {
     int tiles_m, tiles_n;               // tiles of all rows; tiles of columns
     int slot_tiles;                     // tiles of rows that are counted together
     long long first, tiles;             // tile that this launch begins with; all of them
-    int act, out_vec, in_vec;
+    int act, out_vec;
     // adapters
     const int32_t* which;
     const float* scales;
@@ -222,7 +222,8 @@ __device__ __forceinline__ void store_wave_tile(const f32x4 (&acc)[NI][MI], cons
 
 }  // namespace
 
-// The tiles of linear_tile.h, by KIND (one file each); `first` counts tiles.
+// The tiles of linear_tile.h, and the forms for few rows of linear_direct.h (16, 32 and 64 of them a workgroup), by KIND (one file each).
 template <int KIND> drf_status launch_linear_tile(int tile, const LinArgs& a, hipStream_t st);
+template <typename T, int KIND> drf_status launch_linear_direct(int form, const LinArgs& a, hipStream_t st);
 
 }  // namespace drf

@@ -1,0 +1,188 @@
+// Products of few rows, bf16 and fp32: operands straight from memory to registers, the inner axis dealt over the waves of a workgroup, 128 bytes of it at a time, which
+// add up through LDS.  Such a launch is one chain of round trips to memory, and what counts is how many of the weights' bytes are asked for at once: every wave has its
+// operands of U turns on the way.
+#pragma once
+#include "linear_device.h"
+
+namespace drf {
+
+namespace {
+
+// c += w . x over 64 bytes of the inner axis, a lane's 16 each
+__device__ inline f32x4 mma(const u32x4& w, const u32x4& x, f32x4 c, bf16_t) { return mma_bf16(w, x, c); }
+__device__ inline f32x4 mma(const u32x4& w, const u32x4& x, f32x4 c, float)
+{
+    const f32x4 a = __builtin_bit_cast(f32x4, w), b = __builtin_bit_cast(f32x4, x);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[k], b[k], c, 0, 0, 0);
+    return c;
+}
+
+// 16 bytes from element k of a row of n on, at any address of an element; zeros behind the row's end
+template <typename T> __device__ inline u32x4 load_row16(const T* row, int k, int n)
+{
+    constexpr int E = 16 / sizeof(T);
+    typedef T piece __attribute__((ext_vector_type(E), aligned(sizeof(T))));
+    if (k + E <= n) return __builtin_bit_cast(u32x4, *reinterpret_cast<const piece*>(row + k));
+    u32x4 z = { 0, 0, 0, 0 };
+    if (k < n) {
+        T v[E];
+#pragma unroll
+        for (int j = 0; j < E; ++j) v[j] = k + j < n ? row[k + j] : (T)0.f;
+        __builtin_memcpy(&z, v, 16);
+    }
+    return z;
+}
+
+// The adapter's part of four columns from n on of a row: x A^T of it times B's rows.
+template <typename T> __device__ inline void add_low(f32x4& v, const LinArgs& a, int slot, int token, int n)
+{
+    const int ad = adapter_of(a, slot);
+    if (ad < 0) return;
+    const T* b[4];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) b[r] = (const T*)a.b + ((size_t)ad * a.N + (n + r < a.N ? n + r : a.N - 1)) * a.rank;
+    const size_t row = (size_t)slot * a.tokens + token;
+    constexpr int E = 16 / sizeof(T);
+    for (int k = 0; k < a.rank; k += E) {
+        float t[E];
+        if constexpr (sizeof(T) == 2) {
+            const bf16_t* p = (const bf16_t*)a.low + row * 2 * a.low_cols + k;
+            const bf16x8 hi = *reinterpret_cast<const bf16x8*>(p), lo = *reinterpret_cast<const bf16x8*>(p + a.low_cols);
+#pragma unroll
+            for (int e = 0; e < E; ++e) t[e] = (float)hi[e] + (float)lo[e];
+        } else {
+            const f32x4 q = __builtin_bit_cast(f32x4, load_row16((const float*)a.low + row * a.low_cols, k, a.rank));
+#pragma unroll
+            for (int e = 0; e < E; ++e) t[e] = q[e];
+        }
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            T f[E];
+            const u32x4 q = load_row16(b[r], k, a.rank);
+            __builtin_memcpy(f, &q, 16);
+#pragma unroll
+            for (int e = 0; e < E; ++e) v[r] = fmaf(t[e], (float)f[e], v[r]);
+        }
+    }
+}
+
+// 16 MI rows by 16 NI rows of the weights (LIN_GLU: NI / 2 pairs of gates and values).
+template <typename T, int KIND, int MI, int NI, int NW, int U>
+__global__ void __launch_bounds__(NW * 64) linear_direct_kernel(const LinArgs a)
+{
+    constexpr int E = 16 / sizeof(T), CHUNK = 8 * E;                // elements of a turn
+    static_assert(KIND != LIN_GLU || NI % 2 == 0, "gates and values");
+    static_assert(NW * MI * NI <= 64, "partial sums in 64 KB");
+    __shared__ f32x4 part[NW][MI * NI][64];
+    const int lane = threadIdx.x & 63, l16 = lane & 15, quarter = lane >> 4, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const long long id = a.first + blockIdx.x;
+    const int tm = (int)(id / a.tiles_n), tn = (int)(id - (long long)tm * a.tiles_n), row0 = tm * 16 * MI;
+    const int n0 = tn * (KIND == LIN_GLU ? 8 * NI : 16 * NI);
+    const T *x[MI], *w[NI];
+    int slot[MI], token[MI];
+    bool live[MI];
+#pragma unroll
+    for (int j = 0; j < MI; ++j) {
+        live[j] = locate_row(a, 0, row0 + 16 * j + l16, slot[j], token[j]);
+        if (row0 + 16 * j + l16 >= a.slot_rows) slot[j] = token[j] = 0;        // (any row that is there: not stored)
+        x[j] = (const T*)a.x.data + slot[j] * a.x.slot_stride + token[j] * a.x.token_stride;
+    }
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+        int n = KIND == LIN_GLU ? n0 + i / 2 * 16 + l16 : n0 + 16 * i + l16;
+        n = n < a.N ? n : a.N - 1;
+        w[i] = (const T*)a.w + ((size_t)n + (KIND == LIN_GLU && i % 2 ? a.N : 0)) * a.K;
+    }
+    f32x4 acc[NI][MI];
+#pragma unroll
+    for (int i = 0; i < NI; ++i)
+#pragma unroll
+        for (int j = 0; j < MI; ++j) acc[i][j] = (f32x4){ 0.f, 0.f, 0.f, 0.f };
+    u32x4 fx[U][2][MI], fw[U][2][NI];                               // [turn][half]
+    auto load = [&](int t, int k0) __attribute__((always_inline)) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int k = k0 + (4 * h + quarter) * E;
+#pragma unroll
+            for (int i = 0; i < NI; ++i) fw[t][h][i] = load_row16(w[i], k, a.K);
+#pragma unroll
+            for (int j = 0; j < MI; ++j) fx[t][h][j] = load_row16(x[j], k, a.K);
+        }
+    };
+    auto multiply = [&](int t) __attribute__((always_inline)) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int i = 0; i < NI; ++i)
+#pragma unroll
+                for (int j = 0; j < MI; ++j) acc[i][j] = mma(fw[t][h][i], fx[t][h][j], acc[i][j], T{});
+    };
+    constexpr int TURN = NW * CHUNK;
+#pragma unroll
+    for (int t = 0; t < U; ++t)
+        if (wave * CHUNK + t * TURN < a.K) load(t, wave * CHUNK + t * TURN);
+    for (int k = wave * CHUNK; k < a.K; k += U * TURN) {
+#pragma unroll
+        for (int t = 0; t < U; ++t) {
+            if (k + t * TURN < a.K) multiply(t);
+            if (k + (U + t) * TURN < a.K) load(t, k + (U + t) * TURN);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < NI; ++i)
+#pragma unroll
+        for (int j = 0; j < MI; ++j) part[wave][i * MI + j][lane] = acc[i][j];
+    __syncthreads();
+    // results of 16 x 16 dealt over the waves: lane (l16, quarter) has columns 4 quarter .. + 3 of row l16
+    constexpr int OUT = KIND == LIN_GLU ? NI / 2 : NI;
+    for (int p = wave; p < OUT * MI; p += NW) {
+        const int i = p / MI, j = p - i * MI, n = n0 + 16 * i + 4 * quarter, row = row0 + 16 * j + l16;
+        int sl, tk;
+        if (!locate_row(a, 0, row, sl, tk) || n >= a.N) continue;
+        auto total = [&](int piece) {
+            f32x4 v = part[0][piece * MI + j][lane];
+#pragma unroll
+            for (int u = 1; u < NW; ++u) v += part[u][piece * MI + j][lane];
+            return v;
+        };
+        f32x4 v = total(KIND == LIN_GLU ? 2 * i : i), u = v;
+        if constexpr (KIND == LIN_GLU) u = total(2 * i + 1);
+        if constexpr (KIND == LIN_ADAPT) add_low<T>(v, a, sl, tk, n);
+        T* o = (T*)a.out.data + sl * a.out.slot_stride + tk * a.out.token_stride + n;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int c = n + r < a.N ? n + r : a.N - 1;
+            if (a.bias) {
+                v[r] += a.bias[c];
+                if constexpr (KIND == LIN_GLU) u[r] += a.bias[a.N + c];
+            }
+            if constexpr (KIND == LIN_GLU) v[r] = glu(v[r], u[r], a.act);
+        }
+        if (n + 4 <= a.N) {
+            typedef T four __attribute__((ext_vector_type(4), aligned(sizeof(T))));
+            *reinterpret_cast<four*>(o) = (four){ (T)v[0], (T)v[1], (T)v[2], (T)v[3] };
+        } else
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                if (n + r < a.N) o[r] = (T)v[r];
+    }
+}
+
+template <typename T, int KIND, int MI, int NI, int NW, int U> drf_status launch_direct_shape(LinArgs a, hipStream_t st)
+{
+    a.slot_rows = a.slots * a.tokens;
+    const int columns = KIND == LIN_GLU ? 8 * NI : 16 * NI;
+    a.tiles_n = (a.N + columns - 1) / columns;
+    a.tiles = (long long)((a.slot_rows + 16 * MI - 1) / (16 * MI)) * a.tiles_n;
+    const long long most = 1 << 21;                                 // (a launch holds fewer than 2^32 threads)
+    for (a.first = 0; a.first < a.tiles; a.first += most) {
+        hipLaunchKernelGGL((linear_direct_kernel<T, KIND, MI, NI, NW, U>), dim3((unsigned)std::min(most, a.tiles - a.first)), dim3(NW * 64), 0, st, a);
+        DRF_HIP(hipGetLastError());
+    }
+    return DRF_OK;
+}
+
+}  // namespace
+
+}  // namespace drf

@@ -11,6 +11,7 @@
 //    the lower halves of its x A^T, those of a weight row twice the same of B.  Elsewhere the adapters are added to the finished sums (add_adapters);
 //  - the result goes out in whole rows through the idle stages, rows that are not there left out.
 #pragma once
+#include "linear_direct.h"
 #include "linear_wide.h"
 
 namespace drf {
@@ -268,6 +269,16 @@ template <int KIND> drf_status launch_linear_tile(int tile, const LinArgs& a, hi
     default:
         if constexpr (KIND == LIN_GLU) DRF_FAIL(DRF_EINVAL, "no such tile");
         else return launch_wide_shape<288, KIND>(a, st);
+    }
+}
+
+template <typename T, int KIND> drf_status launch_linear_direct(int form, const LinArgs& a, hipStream_t st)
+{
+    switch (form) {
+    case 0: return launch_direct_shape<T, KIND, 1, KIND == LIN_GLU ? 2 : 1, 16, 5>(a, st);
+    case 1: return launch_direct_shape<T, KIND, 1, 4, 8, 3>(a, st);
+    case 2: return launch_direct_shape<T, KIND, 2, 2, 8, 3>(a, st);
+    default: return launch_direct_shape<T, KIND, 4, 2, 8, 2>(a, st);
     }
 }
 

@@ -1,8 +1,10 @@
-// The tiles of linear_tile.h for LIN_STORE (a file of their own: the kinds compile beside one another).
+// The tiles of linear_tile.h and the forms of linear_direct.h for LIN_STORE (a file of their own: the kinds compile beside one another).
 #include "linear_tile.h"
 
 namespace drf {
 
 template drf_status launch_linear_tile<LIN_STORE>(int, const LinArgs&, hipStream_t);
+template drf_status launch_linear_direct<bf16_t, LIN_STORE>(int, const LinArgs&, hipStream_t);
+template drf_status launch_linear_direct<float, LIN_STORE>(int, const LinArgs&, hipStream_t);
 
 }  // namespace drf

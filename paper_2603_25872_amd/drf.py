@@ -647,7 +647,7 @@ def probe_gemm_route(M, N, K, kind=0, rows_per_slot=256):
 
 
 def probe_linear_tile(tile):
-    """bf16 products of gated_ffn() and linear_adapters() on this thread run on tile `tile` where it can take them, -1: by choice; the number of tiles."""
+    """Products of gated_ffn() and linear_adapters() on this thread run on tile or form `tile` where it can take them, -1: by choice; the number of them."""
     return lib().drf_probe_linear_tile(int(tile))
 
 

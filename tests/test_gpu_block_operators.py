@@ -586,7 +586,7 @@ def test_bad_tensors_are_refused(torch, drf):
     assert [tuple(e.shape) for e in empty] == [(2, 0, 64), (0, 4, 128), (0, 4, 64)]
 
 
-# ---- every tile of the bf16 products --------------------------------------------------------------------------
+# ---- every tile and form of the products --------------------------------------------------------------------------
 
 
 @pytest.fixture
@@ -598,17 +598,18 @@ def forced(drf):
 TILED = [(1, 300, 72, 80, 72), (3, 70, 64, 136, 264), (2, 260, 136, 24, 130), (5, 130, 200, 272, 300), (1, 513, 328, 136, 129), (40, 9, 448, 152, 65)]
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("tile", range(16))
 @pytest.mark.parametrize("S,N,D,F,O", TILED)
-def test_gated_ffn_on_every_tile(torch, drf, forced, tile, S, N, D, F, O):
+def test_gated_ffn_on_every_tile(torch, drf, forced, dtype, tile, S, N, D, F, O):
     """Tiles that rows, columns and the inner axis end inside of; slots that end inside of a tile, lengths that leave tiles empty; weights in the last step's idle columns."""
     if tile >= forced(tile):
         pytest.skip("no such tile")
     rng = np.random.default_rng(N + D)
     for layout, act in (("plain", "silu"), ("rows", "gelu"), ("tokens", "silu")):
-        x, w_in, w_out, b_in, b_out = ffn_case(torch, rng, S, N, D, F, O, "bf16", layout)
-        want, slack = ffn(f64(x), f64(w_in), f64(w_out), f64(b_in), f64(b_out), act, "bf16")
-        check(drf.gated_ffn(x, w_in, w_out, b_in, b_out, act), want, "bf16", slack)
+        x, w_in, w_out, b_in, b_out = ffn_case(torch, rng, S, N, D, F, O, dtype, layout)
+        want, slack = ffn(f64(x), f64(w_in), f64(w_out), f64(b_in), f64(b_out), act, dtype)
+        check(drf.gated_ffn(x, w_in, w_out, b_in, b_out, act), want, dtype, slack)
         lens = [(0, N, 1, N // 2, N - 1)[j % 5] for j in range(S)]
         for j, n in enumerate(lens):
             x[j, n:] = float("nan")
@@ -616,23 +617,24 @@ def test_gated_ffn_on_every_tile(torch, drf, forced, tile, S, N, D, F, O):
         drf.gated_ffn(x, w_in, w_out, b_in, b_out, act, lens=torch.tensor(lens, dtype=torch.int32, device="cuda"), out=out)
         for j, n in enumerate(lens):
             assert (out[j, n:] == 7).all()
-            check(out[j, :n], want[j, :n], "bf16", slack[j, :n])
+            check(out[j, :n], want[j, :n], dtype, slack[j, :n])
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("tile", range(16))
 @pytest.mark.parametrize("R", [1, 8, 16, 24, 32, 40, 64, 72, 128, 136])
 @pytest.mark.parametrize("S,N,D,_,O", TILED)
-def test_linear_adapters_on_every_tile(torch, drf, forced, tile, R, S, N, D, _, O):
+def test_linear_adapters_on_every_tile(torch, drf, forced, dtype, tile, R, S, N, D, _, O):
     """The adapter as steps of the product's loop and behind it, ranks that end inside of a step; infinite weights of one slot's adapter reach no other."""
     if tile >= forced(tile):
         pytest.skip("no such tile")
     rng = np.random.default_rng(N + D + R)
     for layout in ("plain", "tokens"):
-        c = list(adapter_case(torch, rng, S, N, D, O, R, 3, "bf16", layout))
+        c = list(adapter_case(torch, rng, S, N, D, O, R, 3, dtype, layout))
         c[4] = [(1, -1, 0, 2, 2)[j % 5] for j in range(S)]
-        want, slack = adapted(*[f64(v) for v in c[:4]], c[4], f64(c[5]), f64(c[6]), "bf16")
+        want, slack = adapted(*[f64(v) for v in c[:4]], c[4], f64(c[5]), f64(c[6]), dtype)
         got = run_adapters(torch, drf, *c)
-        check(got, want, "bf16", slack)
+        check(got, want, dtype, slack)
         lens = [(N, 0, 1, N // 2, N - 1)[j % 5] for j in range(S)]
         out = torch.full_like(got, 7.0)
         y = c[0].clone()
@@ -641,7 +643,7 @@ def test_linear_adapters_on_every_tile(torch, drf, forced, tile, R, S, N, D, _, 
         run_adapters(torch, drf, y, *c[1:], lens=torch.tensor(lens, dtype=torch.int32, device="cuda"), out=out)
         for j, n in enumerate(lens):
             assert (out[j, n:] == 7).all()
-            check(out[j, :n], want[j, :n], "bf16", slack[j, :n])
+            check(out[j, :n], want[j, :n], dtype, slack[j, :n])
         c[2], c[3] = c[2].clone(), c[3].clone()
         c[3][1, :, R - 1] = float("inf")
         others = torch.tensor([i != 1 for i in c[4]], device="cuda")
