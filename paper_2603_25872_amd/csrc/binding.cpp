@@ -402,6 +402,218 @@ PyObject* block_attention(PyObject*, PyObject* const* a, Py_ssize_t n)
     DRF_RUN(g_ops.attend(&s, qb, kb, (float)scale, (const uint32_t*)blocks, &q.h, &k.h, &v.h, &out.h, scratch, bytes, stream));
 }
 
+// ---- operators around the Linears of a block ---------------------------------------------------------
+
+struct BlockOperators {
+    decltype(&drf_residual_norm) residual; decltype(&drf_gated_ffn_scratch_bytes) ffn_bytes; decltype(&drf_gated_ffn) ffn;
+    decltype(&drf_linear_adapters_scratch_bytes) low_bytes; decltype(&drf_linear_adapters) adapters;
+} g_block = {};
+
+// The numbers of a tensor's shape or strides, `dims` of them at most.
+bool numbers(PyObject* v, int dims, long long* out, int* n)
+{
+    if (!v) return false;
+    bool ok = PyTuple_Check(v) && PyTuple_GET_SIZE(v) <= dims;
+    if (!ok) refuse("a tensor of more dimensions than are taken");
+    *n = ok ? (int)PyTuple_GET_SIZE(v) : 0;
+    for (int i = 0; ok && i < *n; ++i) {
+        out[i] = PyLong_AsLongLong(PyTuple_GET_ITEM(v, i));
+        ok = !(out[i] == -1 && PyErr_Occurred());
+    }
+    Py_DECREF(v);
+    return ok;
+}
+
+bool address_of(PyObject* t, void** out)
+{
+    PyObject* p = PyObject_CallMethodNoArgs(t, k_data_ptr);
+    if (!p) return false;
+    *out = PyLong_AsVoidPtr(p);
+    Py_DECREF(p);
+    return !(!*out && PyErr_Occurred());
+}
+
+struct Rows { drf_rows r; long long size[3]; long device; drf_dtype dtype; };
+// A tensor [slots, tokens, columns]; of x's device where there is one.
+bool rows(PyObject* t, const Rows* x, Rows* out)
+{
+    bool is = false;
+    long long stride[3];
+    int n = 0, m = 0;
+    if (!device_of(t, &out->device) || !numbers(PyObject_GetAttr(t, k_shape), 3, out->size, &n) || !numbers(PyObject_CallMethodNoArgs(t, k_stride), 3, stride, &m)) return false;
+    if (n != 3 || m != 3) return refuse("need a device tensor [slots, tokens, columns]");
+    if (stride[2] != 1 && out->size[2] > 1) return refuse("a row's columns must be contiguous");
+    if (!attr_is(t, k_dtype, g_bf16, &is)) return false;
+    out->dtype = DRF_BF16;
+    if (!is) {
+        if (!attr_is(t, k_dtype, g_f32, &is)) return false;
+        if (!is) return refuse("expected bfloat16 or float32");
+        out->dtype = DRF_F32;
+    }
+    if (x && out->device != x->device) return refuse("tensors on two devices");
+    for (int i = 0; i < 3; ++i)
+        if (out->size[i] > 0x7fffffff) return refuse("a size that does not fit 32 bits");
+    out->r = { nullptr, stride[0], stride[1] };
+    return address_of(t, &out->r.data);
+}
+// The same of x's slots and tokens, with so many columns, of a type.
+bool rows_like(PyObject* t, const Rows& x, long long columns, drf_dtype dtype, Rows* out)
+{
+    if (!rows(t, &x, out)) return false;
+    if (out->dtype != dtype) return refuse("tensors of two types");
+    return (out->size[0] == x.size[0] && out->size[1] == x.size[1] && out->size[2] == columns) || refuse("an output or a branch must have the shape of its input");
+}
+
+// fp32 rows [slots, columns] or [slots, tokens, columns] for x; None: no rows.
+bool modulation(PyObject* t, const Rows& x, drf_rows* out)
+{
+    *out = {};
+    if (t == Py_None) return true;
+    bool is = false;
+    long long size[3], stride[3];
+    int n = 0, m = 0;
+    long device = -1;
+    if (!device_of(t, &device) || !attr_is(t, k_dtype, g_f32, &is)) return false;
+    if (!is) return refuse("a modulation must be float32");
+    if (device != x.device) return refuse("tensors on two devices");
+    if (!numbers(PyObject_GetAttr(t, k_shape), 3, size, &n) || !numbers(PyObject_CallMethodNoArgs(t, k_stride), 3, stride, &m)) return false;
+    if (n != m || n < 2 || size[0] != x.size[0] || size[n - 1] != x.size[2] || (n == 3 && size[1] != x.size[1]))
+        return refuse("a modulation must be [slots, columns] or [slots, tokens, columns]");
+    if (stride[n - 1] != 1 && x.size[2] > 1) return refuse("a row's columns must be contiguous");
+    out->slot_stride = stride[0];
+    out->token_stride = n == 3 ? stride[1] : 0;
+    return address_of(t, &out->data);
+}
+
+// Contiguous weights of x's type and device; their sizes.
+bool weights(PyObject* t, const Rows& x, int dims, long long* size, const void** out)
+{
+    void* p = nullptr;
+    int n = 0;
+    long device = -1;
+    if (t == Py_None) return refuse("weights are missing");
+    if (!device_pointer(t, x.dtype == DRF_BF16 ? g_bf16 : g_f32, &p) || !device_of(t, &device) || !numbers(PyObject_GetAttr(t, k_shape), dims, size, &n)) return false;
+    if (device != x.device) return refuse("tensors on two devices");
+    *out = p;
+    for (int i = 0; i < n; ++i)
+        if (size[i] > 0x7fffffff) return refuse("a size that does not fit 32 bits");
+    return n == dims || refuse("weights of another number of dimensions");
+}
+
+bool to_double(PyObject* v, double* out)
+{
+    *out = PyFloat_AsDouble(v);
+    return !(*out == -1.0 && PyErr_Occurred());
+}
+
+bool current_of(const Rows& x, void** stream)
+{
+    Tensor t = {};
+    t.device = x.device;
+    return current(t, stream);
+}
+
+bool block_ready(Py_ssize_t n, Py_ssize_t want)
+{
+    if (n == want && g_block.residual && g_ops.rope) return true;
+    PyErr_Format(PyExc_TypeError, "%zd arguments are taken, after bind_operators() and bind_block_operators()", want);
+    return false;
+}
+
+// residual_norm(x, y, out, h, after, before, eps, x_scale, y_scale, after_gain, after_bias, before_gain, before_bias, gate, shift, scale, lens) -> status
+PyObject* residual_norm(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    Rows x, y, out, h;
+    drf_residual_config c{};
+    int kind[2];
+    double num[3];
+    void *par[4], *lens = nullptr, *stream = nullptr;
+    if (!block_ready(n, 17) || !rows(a[0], nullptr, &x)) return nullptr;
+    const bool has_y = a[1] != Py_None, has_out = a[2] != Py_None, has_h = a[3] != Py_None;
+    if (has_y && (!rows(a[1], &x, &y) || !rows_like(a[1], x, x.size[2], y.dtype, &y))) return nullptr;
+    if (has_out && !rows_like(a[2], x, x.size[2], x.dtype, &out)) return nullptr;
+    if (has_h && (!rows(a[3], &x, &h) || !rows_like(a[3], x, x.size[2], has_y ? y.dtype : h.dtype, &h))) return nullptr;
+    for (int i = 0; i < 2; ++i) if (!to_int(a[4 + i], &kind[i])) return nullptr;
+    for (int i = 0; i < 3; ++i) if (!to_double(a[6 + i], &num[i])) return nullptr;
+    for (int i = 0; i < 4; ++i) if (!vector(a[9 + i], g_f32, x.size[2], x.device, "a norm's parameters", &par[i])) return nullptr;
+    if (!modulation(a[13], x, &c.gate) || !modulation(a[14], x, &c.shift) || !modulation(a[15], x, &c.scale) ||
+        !vector(a[16], g_i32, x.size[0], x.device, "lens", &lens) || !current_of(x, &stream)) return nullptr;
+    c.stream = x.dtype; c.branch = has_y ? y.dtype : has_h ? h.dtype : x.dtype;
+    c.slots = (int)x.size[0]; c.tokens = (int)x.size[1]; c.width = (int)x.size[2];
+    c.lens = (const int32_t*)lens;
+    c.x_scale = (float)num[1]; c.y_scale = (float)num[2];
+    c.after = { (drf_qk_norm)kind[0], num[0], (const float*)par[0], (const float*)par[1] };
+    c.before = { (drf_qk_norm)kind[1], num[0], (const float*)par[2], (const float*)par[3] };
+    DRF_RUN(g_block.residual(&c, &x.r, has_y ? &y.r : nullptr, has_out ? &out.r : nullptr, has_h ? &h.r : nullptr, stream));
+}
+
+// The feed-forward's configuration from (x, w_in, w_out, b_in, b_out, act, lens) at a.
+bool ffn_config(PyObject* const* a, Rows* x, drf_gated_ffn_config* c)
+{
+    long long in[2], out[2];
+    void *bi = nullptr, *bo = nullptr, *lens = nullptr;
+    int act = 0;
+    if (!rows(a[0], nullptr, x) || !weights(a[1], *x, 2, in, &c->w_in) || !weights(a[2], *x, 2, out, &c->w_out)) return false;
+    if (in[0] != 2 * out[1] || in[1] != x->size[2]) return refuse("w_in must have twice the rows that w_out has columns, and x's columns");
+    if (!vector(a[3], g_f32, in[0], x->device, "b_in", &bi) || !vector(a[4], g_f32, out[0], x->device, "b_out", &bo) || !to_int(a[5], &act) ||
+        !vector(a[6], g_i32, x->size[0], x->device, "lens", &lens)) return false;
+    c->dtype = x->dtype; c->act = (drf_glu)act;
+    c->slots = (int)x->size[0]; c->tokens = (int)x->size[1]; c->width = (int)in[1]; c->hidden = (int)out[1]; c->out_width = (int)out[0];
+    c->lens = (const int32_t*)lens; c->b_in = (const float*)bi; c->b_out = (const float*)bo;
+    return true;
+}
+
+// gated_ffn(x, w_in, w_out, b_in, b_out, act, lens, out or None, scratch or None): without an output its scratch bytes, with one the status of drf_gated_ffn
+PyObject* gated_ffn(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    Rows x, out;
+    drf_gated_ffn_config c{};
+    void *scratch = nullptr, *stream = nullptr;
+    if (!block_ready(n, 9) || !ffn_config(a, &x, &c)) return nullptr;
+    if (a[7] == Py_None) return PyLong_FromSize_t(g_block.ffn_bytes(&c));
+    if (!rows_like(a[7], x, c.out_width, x.dtype, &out) || (a[8] != Py_None && !address_of(a[8], &scratch)) || !current_of(x, &stream)) return nullptr;
+    const size_t bytes = g_block.ffn_bytes(&c);
+    DRF_RUN(g_block.ffn(&c, &x.r, &out.r, scratch, bytes, stream));
+}
+
+// linear_adapters(x, w, a, b, which, bias, scales, lens, out or None, scratch or None): as gated_ffn
+PyObject* linear_adapters(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    Rows x, out;
+    drf_adapters_config c{};
+    long long w[2], low[3], b[3];
+    void *which = nullptr, *bias = nullptr, *scales = nullptr, *lens = nullptr, *scratch = nullptr, *stream = nullptr;
+    if (!block_ready(n, 10) || !rows(a[0], nullptr, &x) || !weights(a[1], x, 2, w, &c.w) || !weights(a[2], x, 3, low, &c.a) || !weights(a[3], x, 3, b, &c.b)) return nullptr;
+    if (w[1] != x.size[2] || low[2] != w[1] || b[0] != low[0] || b[1] != w[0] || b[2] != low[1]) {
+        refuse("w must be [out columns, columns], a [adapters, rank, columns] and b [adapters, out columns, rank]");
+        return nullptr;
+    }
+    if (a[4] == Py_None) { refuse("which is missing"); return nullptr; }
+    if (!vector(a[4], g_i32, x.size[0], x.device, "which", &which) || !vector(a[5], g_f32, w[0], x.device, "bias", &bias) ||
+        !vector(a[6], g_f32, low[0], x.device, "scales", &scales) || !vector(a[7], g_i32, x.size[0], x.device, "lens", &lens)) return nullptr;
+    c.dtype = x.dtype;
+    c.slots = (int)x.size[0]; c.tokens = (int)x.size[1]; c.width = (int)w[1]; c.out_width = (int)w[0]; c.rank = (int)low[1]; c.adapters = (int)low[0];
+    c.lens = (const int32_t*)lens; c.which = (const int32_t*)which; c.bias = (const float*)bias; c.scales = (const float*)scales;
+    if (a[8] == Py_None) return PyLong_FromSize_t(g_block.low_bytes(&c));
+    if (!rows_like(a[8], x, c.out_width, x.dtype, &out) || (a[9] != Py_None && !address_of(a[9], &scratch)) || !current_of(x, &stream)) return nullptr;
+    const size_t bytes = g_block.low_bytes(&c);
+    DRF_RUN(g_block.adapters(&c, &x.r, &out.r, scratch, bytes, stream));
+}
+
+// bind_block_operators(five addresses), after bind_operators()
+PyObject* bind_block_operators(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    void* p[5];
+    if (n != 5) { PyErr_SetString(PyExc_TypeError, "bind_block_operators() takes five addresses"); return nullptr; }
+    for (int i = 0; i < 5; ++i)
+        if (!(p[i] = PyLong_AsVoidPtr(a[i]))) {
+            if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "NULL address");
+            return nullptr;
+        }
+    g_block = { (decltype(g_block.residual))p[0], (decltype(g_block.ffn_bytes))p[1], (decltype(g_block.ffn))p[2], (decltype(g_block.low_bytes))p[3], (decltype(g_block.adapters))p[4] };
+    Py_RETURN_NONE;
+}
+
 // bind_operators((addresses), float32, bfloat16, int32, current device, current stream of a device)
 PyObject* bind_operators(PyObject*, PyObject* const* a, Py_ssize_t n)
 {
@@ -425,6 +637,10 @@ PyMethodDef kMethods[] = {
     { "qk_norm_rope", DRF_FAST(qk_norm_rope), "status of drf_qk_norm_rope on these arguments" },
     { "block_select", DRF_FAST(block_select), "status of drf_block_select on these arguments" },
     { "block_attention", DRF_FAST(block_attention), "status of drf_block_attention on these arguments" },
+    { "residual_norm", DRF_FAST(residual_norm), "status of drf_residual_norm on these arguments" },
+    { "gated_ffn", DRF_FAST(gated_ffn), "status of drf_gated_ffn on these arguments, or its scratch bytes" },
+    { "linear_adapters", DRF_FAST(linear_adapters), "status of drf_linear_adapters on these arguments, or its scratch bytes" },
+    { "bind_block_operators", DRF_FAST(bind_block_operators), "addresses of the calls around a block's Linears" },
     { "bind_operators", DRF_FAST(bind_operators), "addresses of the operators' calls, dtypes, and what gives the current device and stream" },
     { "skip", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(skip)), METH_FASTCALL, "status of drf_skip_transition_noise on these arguments" },
     { "bind", bind, METH_O, "address of drf_skip_transition_noise" },

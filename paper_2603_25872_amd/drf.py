@@ -467,6 +467,55 @@ def _dtype_of(t):
     return BF16 if t.dtype == torch.bfloat16 else F32
 
 
+class _BlockCtypes:
+    """The marshalling of the operators around a block's Linears with ctypes."""
+
+    @staticmethod
+    def residual_norm(x, y, out, h, after, before, eps, x_scale, y_scale, after_gain, after_bias, before_gain, before_bias, gate, shift, scale, lens):
+        import torch
+        rx, D = _rows(x), x.shape[2]
+        ry, ro = None if y is None else _rows(y, x, x.shape), None if out is None else _rows(out, x, x.shape, x.dtype)
+        rh = None if h is None else _rows(h, x, x.shape, None if y is None else y.dtype)
+        vec = lambda t: _vector(t, torch.float32, D, x, "a norm's parameters")  # noqa: E731
+        cfg = ResidualConfig(_dtype_of(x), _dtype_of(x if y is None and h is None else h if y is None else y), *x.shape, _vector(lens, torch.int32, x.shape[0], x, "lens"), x_scale, y_scale,
+                             RowNorm(after, eps, vec(after_gain), vec(after_bias)), RowNorm(before, eps, vec(before_gain), vec(before_bias)),
+                             _modulation(gate, x, "gate"), _modulation(shift, x, "shift"), _modulation(scale, x, "scale"))
+        ref = lambda r: None if r is None else C.byref(r)  # noqa: E731
+        return _lib.drf_residual_norm(C.byref(cfg), C.byref(rx), ref(ry), ref(ro), ref(rh), _current(x))
+
+    @staticmethod
+    def gated_ffn(x, w_in, w_out, b_in, b_out, act, lens, out, scratch):
+        import torch
+        rx = _rows(x)
+        S, N, D = x.shape
+        assert w_in.dim() == 2 and w_out.dim() == 2 and w_in.shape[0] == 2 * w_out.shape[1], "w_in must have twice the rows that w_out has columns"
+        O, F = w_out.shape
+        cfg = GatedFfnConfig(_dtype_of(x), act, S, N, D, F, O, _vector(lens, torch.int32, S, x, "lens"), _weights(w_in, x, (2 * F, D), "w_in"),
+                             _weights(w_out, x, (O, F), "w_out"), _vector(b_in, torch.float32, 2 * F, x, "b_in"), _vector(b_out, torch.float32, O, x, "b_out"))
+        n = _lib.drf_gated_ffn_scratch_bytes(C.byref(cfg))
+        if out is None:
+            return n
+        ro = _rows(out, x, (S, N, O), x.dtype)
+        return _lib.drf_gated_ffn(C.byref(cfg), C.byref(rx), C.byref(ro), None if scratch is None else scratch.data_ptr(), n, _current(x))
+
+    @staticmethod
+    def linear_adapters(x, w, a, b, which, bias, scales, lens, out, scratch):
+        import torch
+        rx = _rows(x)
+        S, N, D = x.shape
+        assert w.dim() == 2 and a.dim() == 3, "need w [out columns, columns] and a [adapters, rank, columns]"
+        assert which is not None, "which must have %d elements" % S
+        O, (n_ad, R) = w.shape[0], a.shape[:2]
+        cfg = AdaptersConfig(_dtype_of(x), S, N, D, O, R, n_ad, _vector(lens, torch.int32, S, x, "lens"), _vector(which, torch.int32, S, x, "which"),
+                             _weights(w, x, (O, D), "w"), _weights(a, x, (n_ad, R, D), "a"), _weights(b, x, (n_ad, O, R), "b"),
+                             _vector(bias, torch.float32, O, x, "bias"), _vector(scales, torch.float32, n_ad, x, "scales"))
+        n = _lib.drf_linear_adapters_scratch_bytes(C.byref(cfg))
+        if out is None:
+            return n
+        ro = _rows(out, x, (S, N, O), x.dtype)
+        return _lib.drf_linear_adapters(C.byref(cfg), C.byref(rx), C.byref(ro), None if scratch is None else scratch.data_ptr(), n, _current(x))
+
+
 _ops = None             # _native or _OperatorsCtypes, at the first operator
 
 
@@ -483,6 +532,21 @@ def _operators():
     except ImportError:
         _ops = _OperatorsCtypes
     return _ops
+
+
+_block_ops = None       # _native or _BlockCtypes, at the first of them
+
+
+def _block_operators():
+    global _block_ops
+    L = lib()
+    if _operators() is _OperatorsCtypes:
+        _block_ops = _BlockCtypes
+    else:
+        _ops.bind_block_operators(*(C.cast(f, C.c_void_p).value for f in (L.drf_residual_norm, L.drf_gated_ffn_scratch_bytes, L.drf_gated_ffn,
+                                                                           L.drf_linear_adapters_scratch_bytes, L.drf_linear_adapters)))
+        _block_ops = _ops
+    return _block_ops
 
 
 def rope_config(dims, extents, theta=10000.0, layout="pairs", origin=None, step=None):
@@ -562,24 +626,16 @@ def residual_norm(x, y=None, gate=None, after="none", after_gain=None, after_bia
     before None: no h.  gate, shift, scale: fp32 [slots, columns] or [slots, tokens, columns].  h is of y's type (x's without y).  out may be x, h_out y.
     Rows behind a slot's length are left as they were: those of x in a z made here, zeros in an h.  No gradient is recorded."""
     import torch
-    L = _lib or lib()
-    rx, D = _rows(x), x.shape[2]
-    like = x if y is None else y
+    ops = _block_ops or _block_operators()
     assert y is not None or out is None, "a stream is stored where a branch is added to it"
     assert before is not None or h_out is None, "an output for a norm that is not asked for"
+    assert x.is_cuda, "need a device tensor [slots, tokens, columns]"
     if y is not None and out is None:
         out = torch.empty_like(x) if lens is None else x.detach().clone()
     if before is not None and h_out is None:
-        h_out = (torch.empty if lens is None else torch.zeros)(x.shape, dtype=like.dtype, device=x.device)
-    ry = None if y is None else _rows(y, x, x.shape)
-    ro = None if y is None else _rows(out, x, x.shape, x.dtype)
-    rh = None if before is None else _rows(h_out, x, x.shape, like.dtype if y is not None else None)
-    vec = lambda t: _vector(t, torch.float32, D, x, "a norm's parameters")  # noqa: E731
-    cfg = ResidualConfig(_dtype_of(x), _dtype_of(h_out if y is None else y), *x.shape, _vector(lens, torch.int32, x.shape[0], x, "lens"), float(x_scale), float(y_scale),
-                         RowNorm(_QK[after], float(eps), vec(after_gain), vec(after_bias)), RowNorm(_QK[before or "none"], float(eps), vec(before_gain), vec(before_bias)),
-                         _modulation(gate, x, "gate"), _modulation(shift, x, "shift"), _modulation(scale, x, "scale"))
-    ref = lambda r: None if r is None else C.byref(r)  # noqa: E731
-    _check(L.drf_residual_norm(C.byref(cfg), C.byref(rx), ref(ry), ref(ro), ref(rh), _current(x)))
+        h_out = (torch.empty if lens is None else torch.zeros)(x.shape, dtype=x.dtype if y is None else y.dtype, device=x.device)
+    _check(ops.residual_norm(x, y, out, h_out, _QK[after], _QK[before or "none"], float(eps), float(x_scale), float(y_scale), after_gain, after_bias, before_gain,
+                             before_bias, gate, shift, scale, lens))
     return (x if y is None else out), h_out
 
 
@@ -588,19 +644,12 @@ def gated_ffn(x, w_in, w_out, b_in=None, b_out=None, act="silu", lens=None, out=
     [out columns, hidden], biases fp32; act "silu" or "gelu" (the tanh form).  Rows behind a slot's length are left as they were: zeros in an output made here.  No
     gradient is recorded."""
     import torch
-    L = _lib or lib()
-    rx = _rows(x)
-    S, N, D = x.shape
-    assert w_in.dim() == 2 and w_out.dim() == 2 and w_in.shape[0] == 2 * w_out.shape[1], "w_in must have twice the rows that w_out has columns"
-    O, F = w_out.shape
+    ops, kind = _block_ops or _block_operators(), _GLU[act]
+    n = ops.gated_ffn(x, w_in, w_out, b_in, b_out, kind, lens, None, None)
     if out is None:
-        out = (torch.empty if lens is None else torch.zeros)((S, N, O), dtype=x.dtype, device=x.device)
-    ro = _rows(out, x, (S, N, O), x.dtype)
-    cfg = GatedFfnConfig(_dtype_of(x), _GLU[act], S, N, D, F, O, _vector(lens, torch.int32, S, x, "lens"), _weights(w_in, x, (2 * F, D), "w_in"),
-                         _weights(w_out, x, (O, F), "w_out"), _vector(b_in, torch.float32, 2 * F, x, "b_in"), _vector(b_out, torch.float32, O, x, "b_out"))
-    n = L.drf_gated_ffn_scratch_bytes(C.byref(cfg))
-    scratch = torch.empty(n, dtype=torch.uint8, device=x.device)
-    _check(L.drf_gated_ffn(C.byref(cfg), C.byref(rx), C.byref(ro), scratch.data_ptr(), n, _current(x)))
+        out = (torch.empty if lens is None else torch.zeros)((x.shape[0], x.shape[1], w_out.shape[0]), dtype=x.dtype, device=x.device)
+    scratch = torch.empty(n, dtype=torch.uint8, device=x.device) if n else None
+    _check(ops.gated_ffn(x, w_in, w_out, b_in, b_out, kind, lens, out, scratch))
     return out
 
 
@@ -609,21 +658,12 @@ def linear_adapters(x, w, a, b, which, bias=None, scales=None, lens=None, out=No
     and b [adapters, out columns, rank], which int32 [slots] (an index outside of the adapters: none), bias and scales fp32.  Rows behind a slot's length are left as
     they were: zeros in an output made here.  No gradient is recorded."""
     import torch
-    L = _lib or lib()
-    rx = _rows(x)
-    S, N, D = x.shape
-    assert w.dim() == 2 and a.dim() == 3, "need w [out columns, columns] and a [adapters, rank, columns]"
-    O, (n_ad, R) = w.shape[0], a.shape[:2]
+    ops = _block_ops or _block_operators()
+    n = ops.linear_adapters(x, w, a, b, which, bias, scales, lens, None, None)
     if out is None:
-        out = (torch.empty if lens is None else torch.zeros)((S, N, O), dtype=x.dtype, device=x.device)
-    ro = _rows(out, x, (S, N, O), x.dtype)
-    assert which is not None, "which must have %d elements" % S
-    cfg = AdaptersConfig(_dtype_of(x), S, N, D, O, R, n_ad, _vector(lens, torch.int32, S, x, "lens"), _vector(which, torch.int32, S, x, "which"),
-                         _weights(w, x, (O, D), "w"), _weights(a, x, (n_ad, R, D), "a"), _weights(b, x, (n_ad, O, R), "b"),
-                         _vector(bias, torch.float32, O, x, "bias"), _vector(scales, torch.float32, n_ad, x, "scales"))
-    n = L.drf_linear_adapters_scratch_bytes(C.byref(cfg))
+        out = (torch.empty if lens is None else torch.zeros)((x.shape[0], x.shape[1], w.shape[0]), dtype=x.dtype, device=x.device)
     scratch = torch.empty(n, dtype=torch.uint8, device=x.device) if n else None
-    _check(L.drf_linear_adapters(C.byref(cfg), C.byref(rx), C.byref(ro), None if scratch is None else scratch.data_ptr(), n, _current(x)))
+    _check(ops.linear_adapters(x, w, a, b, which, bias, scales, lens, out, scratch))
     return out
 
 

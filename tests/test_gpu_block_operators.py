@@ -649,3 +649,45 @@ def test_linear_adapters_on_every_tile(torch, drf, forced, dtype, tile, R, S, N,
         others = torch.tensor([i != 1 for i in c[4]], device="cuda")
         again = run_adapters(torch, drf, *c)
         assert torch.equal(again[others], got[others]) and not torch.isfinite(again[0]).any()
+
+
+def test_both_marshallings_agree(torch, drf):
+    """The CPython module and ctypes make the same calls of the same arguments, and refuse the same ones."""
+    x, y, rows = torch.randn(2, 5, 64, device="cuda"), torch.randn(2, 5, 64, device="cuda").bfloat16(), torch.randn(2, 5, 192, device="cuda")
+    w, w_out, v, i = torch.randn(128, 64, device="cuda"), torch.randn(40, 64, device="cuda"), torch.randn(64, device="cuda"), torch.tensor([1, -1], dtype=torch.int32, device="cuda")
+    a, b, lens = torch.randn(3, 6, 64, device="cuda"), torch.randn(3, 128, 6, device="cuda"), torch.tensor([5, 2], dtype=torch.int32, device="cuda")
+    calls = [lambda: drf.residual_norm(x, y, gate=rows[:, 0, :64], after="rms", after_gain=v, x_scale=0.5, y_scale=2, before="layer", before_gain=v, before_bias=v, shift=rows[..., 64:128],
+                                       scale=rows[..., 128:], eps=1e-3, lens=lens),
+             lambda: drf.residual_norm(x), lambda: drf.residual_norm(x, y, before=None), lambda: drf.residual_norm(x, h_out=y.clone()),
+             lambda: drf.gated_ffn(x, w, w_out, b_in=w[:, 0].contiguous(), b_out=v[:40], act="gelu", lens=lens), lambda: drf.gated_ffn(x[:, ::2], w, w_out),
+             lambda: drf.linear_adapters(x, w, a, b, i, bias=w[:, 1].contiguous(), scales=v[:3], lens=lens), lambda: drf.linear_adapters(x, w, a[:0], b[:0], i),
+             lambda: drf.gated_ffn(x[:0], w, w_out), lambda: drf.linear_adapters(x[:, :0], w, a, b, i)]
+    bad = [lambda: drf.residual_norm(x, y[:1]), lambda: drf.residual_norm(x, y, out=y), lambda: drf.residual_norm(x[0]), lambda: drf.residual_norm(x, y, gate=v), lambda: drf.residual_norm(x.cpu()),
+           lambda: drf.residual_norm(x, y, shift=rows[..., :63]), lambda: drf.residual_norm(x.double()), lambda: drf.residual_norm(x, y, lens=i.long()), lambda: drf.residual_norm(y, x),
+           lambda: drf.residual_norm(x, before_gain=v.bfloat16()), lambda: drf.residual_norm(x, x_scale=float("inf")), lambda: drf.residual_norm(x, eps=float("nan")),
+           lambda: drf.gated_ffn(x, w, w_out[:, :32]), lambda: drf.gated_ffn(y, w, w_out), lambda: drf.gated_ffn(x, w[None], w_out), lambda: drf.gated_ffn(x, w, w_out, b_in=v),
+           lambda: drf.gated_ffn(x, w, w_out, out=x), lambda: drf.gated_ffn(x, w, None), lambda: drf.gated_ffn(x[..., :32], w, w_out), lambda: drf.gated_ffn(x, w.t(), w_out),
+           lambda: drf.linear_adapters(x, w, a, b, None), lambda: drf.linear_adapters(x, w, a, b[:2], i), lambda: drf.linear_adapters(x, w, a[0], b, i), lambda: drf.linear_adapters(x, w, a, b, v),
+           lambda: drf.linear_adapters(x, w, a, b, i, scales=v), lambda: drf.linear_adapters(x, w, a, b, i[:1]), lambda: drf.linear_adapters(x.cpu(), w, a, b, i)]
+    native = drf._block_operators()
+    if native is drf._BlockCtypes:
+        pytest.skip("no native module for this interpreter")
+
+    def outcome(f):
+        try:
+            r = f()
+            return [None if t is None else t.clone() for t in (r if isinstance(r, tuple) else (r,))]
+        except Exception as e:
+            return e.status if isinstance(e, drf.DrfError) else AssertionError if isinstance(e, (AssertionError, AttributeError)) else type(e)
+    results = []
+    try:
+        for form in (native, drf._BlockCtypes):
+            drf._block_ops = form
+            results.append([outcome(f) for f in calls + bad])
+    finally:
+        drf._block_ops = native
+    for k, (p, q) in enumerate(zip(*results)):
+        if k < len(calls):
+            assert len(p) == len(q) and all(s is t if s is None or t is None else torch.equal(s, t) for s, t in zip(p, q)), k
+        else:
+            assert p == q and not isinstance(p, list), (k - len(calls), p, q)
