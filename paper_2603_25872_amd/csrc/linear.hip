@@ -17,19 +17,21 @@ namespace {
 constexpr int kMaxTokenStride = 1 << 22;           // 256 rows within 2^31 bytes
 
 // Tiles and a time model of a launch of each: base + (per round of workgroups) round + steps * max(lat, c * thr) us, where a round is per_cu workgroups on each of 256
-// CUs and c those that share a CU in it.  Least-squares fits to 220 products (16 to 65536 rows, 64 to 9600 columns, an inner axis of 72 to 4800, weights cold);
-// the choice by it is within 1 % of the best tile on average, 35 % behind at worst.
+// CUs and c those that share a CU in it.  Least-squares fits to 260 products (16 to 65536 rows, 64 to 9600 columns, an inner axis of 72 to 4800, weights cold);
+// the choice by it is within 1 % of the best tile on average, 11 % behind at worst.
 struct Tile { int bm, bn, per_cu; double base, round, lat, thr; };
-const Tile kLinTiles[] = { { 256, 256, 1, 0.00, 8.15, 1.317, 0 }, { 256, 128, 1, 0.00, 6.01, 0.847, 0 }, { 128, 128, 1, 0.40, 4.08, 0.549, 0 }, { 128, 64, 2, 1.55, 3.36, 0.386, 0.376 },
-                           { 64, 128, 2, 1.45, 3.54, 0.385, 0.347 }, { 64, 64, 2, 1.30, 2.97, 0.274, 0.213 }, { 256, 256, 1, 0.00, 11.7, 1.099, 0 }, { 256, 288, 1, 0.00, 13.6, 1.188, 0 } };
+const Tile kLinTiles[] = { { 256, 256, 1, 0.00, 9.05, 1.075, 0 }, { 256, 128, 1, 0.00, 6.40, 0.723, 0 }, { 128, 128, 1, 0.43, 4.47, 0.451, 0 }, { 128, 64, 2, 1.54, 3.59, 0.324, 0.324 },
+                           { 64, 128, 2, 1.60, 3.50, 0.333, 0.333 }, { 64, 64, 2, 1.75, 2.83, 0.207, 0.207 }, { 256, 256, 1, 0.00, 11.9, 0.965, 0 }, { 256, 288, 1, 0.00, 13.6, 1.067, 0 } };
 constexpr int kTiles = sizeof(kLinTiles) / sizeof(kLinTiles[0]);
 // The forms for few rows of linear_direct.h, rows and weight rows a workgroup in sixteens and its waves: fixed + turns * turn + max(0, workgroups / 256 - hidden) * (group + 128-byte
-// pieces of the inner axis * piece) us, fitted likewise (250 and 200 products of 1 to 4096 rows; the choice is within 4 % of the best on average in bf16, 1 % in fp32).
+// pieces of the inner axis * piece) us, fitted likewise (140 and 100 products of 1 to 4096 rows; the choice is within 5 % of the best on average in bf16, 3 % in fp32).
 struct Form { int mi, ni, nw; double fixed, turn, hidden, group, piece; };
-constexpr int kForms = 4;
-const Form kFormsBf16[kForms] = { { 1, 1, 16, 1.79, 1.14, 0.27, 1.22, 0.089 }, { 1, 4, 8, 1.80, 1.48, 0.0, 0.88, 0.236 }, { 2, 2, 8, 2.11, 0.97, 0.0, 0.89, 0.191 }, { 4, 2, 8, 2.60, 1.41, 0.19, 1.76, 0.309 } };
-const Form kFormsF32[kForms] = { { 1, 1, 16, 1.87, 1.36, 0.27, 1.41, 0.103 }, { 1, 4, 8, 2.06, 2.24, 0.20, 1.43, 0.321 }, { 2, 2, 8, 2.32, 1.82, 0.35, 1.53, 0.261 }, { 4, 2, 8, 2.27, 3.25, 0.42, 2.83, 0.466 } };
-const Tile kTileF32 = { 64, 64, 4, 0.0, 3.60, 0.700, 0.634 };      // steps of 32
+constexpr int kForms = 5;
+const Form kFormsBf16[kForms] = { { 1, 1, 16, 1.83, 1.13, 0.27, 1.18, 0.095 }, { 1, 4, 8, 1.84, 1.75, 0.40, 0.80, 0.282 }, { 2, 2, 8, 2.18, 1.03, 0.06, 0.85, 0.196 }, { 4, 2, 8, 2.47, 1.47, 0.37, 1.71, 0.343 },
+                                  { 1, 2, 8, 2.08, 0.93, 0.25, 0.66, 0.161 } };
+const Form kFormsF32[kForms] = { { 1, 1, 16, 1.80, 1.40, 0.28, 1.40, 0.104 }, { 1, 4, 8, 2.00, 2.23, 0.20, 1.50, 0.304 }, { 2, 2, 8, 2.21, 1.84, 0.34, 1.57, 0.254 }, { 4, 2, 8, 2.31, 3.18, 0.34, 2.68, 0.459 },
+                                 { 1, 2, 8, 2.10, 1.02, 0.0, 0.71, 0.164 } };
+const Tile kTileF32 = { 64, 64, 4, 0.0, 3.67, 0.692, 0.630 };      // steps of 32
 
 double tile_us(const Tile& m, long long tiles, int steps)
 {
@@ -50,6 +52,7 @@ template <typename T, int KIND> int pick_form(const LinArgs& a, double* us)
         const double groups = (double)((rows + 16 * m.mi - 1) / (16 * m.mi)) * ((weight_rows + 16 * m.ni - 1) / (16 * m.ni));
         double t = m.fixed + (pieces + m.nw - 1) / m.nw * m.turn + std::max(0.0, groups / 256 - m.hidden) * (m.group + pieces * m.piece);
         if (KIND == LIN_ADAPT && a.adapters) t += (0.3 + 0.01 * a.rank) * (1 + groups / 256);
+        if (f == kForms - 1) t *= 1.08;                             // (level with the first and third it has lost in pairs and with adapters)
         if (t < *us) { *us = t; best = f; }
     }
     return best;

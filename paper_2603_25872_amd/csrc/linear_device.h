@@ -73,6 +73,27 @@ template <typename T> __device__ inline u32x4 load16(const T* row, int k, int n,
     return r;
 }
 
+// The bias of a tile's BN weight rows into LDS, by copies of 4 bytes a lane where there is one (nothing waits for them before the first step's copies, which are
+// younger) and zeros where there is none.  Whole 64s of them are written.
+template <int BN, int NW, int KIND> __device__ __forceinline__ void stage_bias(const LinArgs& a, float* bias, int n0, int wave)
+{
+    const int lane = threadIdx.x & 63;
+    if (!a.bias) {
+        for (int t = threadIdx.x; t < BN; t += NW * 64) bias[t] = 0.f;
+        return;
+    }
+#pragma unroll
+    for (int c = 0; c < (BN + 64 * NW - 1) / (64 * NW); ++c) {
+        const int piece = c * NW + wave, t = piece * 64 + lane;
+        if (piece * 64 >= BN) continue;
+        int n = KIND == LIN_GLU ? t / 32 * 16 + t % 16 : t;
+        n = n0 + n < a.N ? n0 + n : a.N - 1;
+        if constexpr (KIND == LIN_GLU) n += t / 16 % 2 ? a.N : 0;
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2"
+                     :: "s"((uint32_t)(uintptr_t)(DRF_LDS_AS float*)bias + (uint32_t)piece * 256u), "v"((uint32_t)n * 4u), "s"(a.bias) : "memory");
+    }
+}
+
 // What the adapters add to a wave's tile: acc[i][j][r] is (row mw + 16 j + l16, column nw + 16 i + 4 quarter + r) of the group's rows.
 // A slot's product goes into sums of its own, of which its rows take theirs: an infinite weight of one adapter is nothing to the rows of another.  Where slots
 // are shorter than a tile's sixteen rows a lane adds up its elements one by one, each row from its own adapter, read once.
@@ -89,21 +110,23 @@ __device__ __forceinline__ void add_adapters(f32x4 (&acc)[NI][MI], const LinArgs
             const int ad = adapter_of(a, slot);
             if (ad < 0) continue;
             const bf16_t* t = (const bf16_t*)a.low + ((size_t)slot * a.tokens + token) * 2 * LC;
+            const bf16_t* b0 = (const bf16_t*)a.b + (size_t)ad * a.N * a.rank;
+            for (int k = 0; k < a.rank; k += 8) {                   // (all pieces' loads beside one another)
+                const bf16x8 hi = *reinterpret_cast<const bf16x8*>(t + k), lo = *reinterpret_cast<const bf16x8*>(t + LC + k);
+                u32x4 f[NI][4];
 #pragma unroll
-            for (int i = 0; i < NI; ++i) {
-                const int n = nw + 16 * i + 4 * quarter;
-                const bf16_t* b[4];
-#pragma unroll
-                for (int r = 0; r < 4; ++r) b[r] = (const bf16_t*)a.b + ((size_t)ad * a.N + (n + r < a.N ? n + r : a.N - 1)) * a.rank;
-                for (int k = 0; k < a.rank; k += 8) {
-                    const bf16x8 hi = *reinterpret_cast<const bf16x8*>(t + k), lo = *reinterpret_cast<const bf16x8*>(t + LC + k);
+                for (int i = 0; i < NI; ++i)
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
-                        const bf16x8 f = __builtin_bit_cast(bf16x8, load16(b[r], k, a.rank, a.b_vec));
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) acc[i][j][r] = fmaf((float)hi[e] + (float)lo[e], (float)f[e], acc[i][j][r]);
+                        const int n = nw + 16 * i + 4 * quarter + r;
+                        f[i][r] = load16(b0 + (size_t)(n < a.N ? n : a.N - 1) * a.rank, k, a.rank, a.b_vec);
                     }
-                }
+#pragma unroll
+                for (int i = 0; i < NI; ++i)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) acc[i][j][r] = fmaf((float)hi[e] + (float)lo[e], (float)__builtin_bit_cast(bf16x8, f[i][r])[e], acc[i][j][r]);
             }
         }
         return;

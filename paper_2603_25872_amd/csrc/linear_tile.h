@@ -25,7 +25,7 @@ __global__ void __launch_bounds__(WM * WN * 64) linear_tile_kernel(const LinArgs
     constexpr int STAGE = (BM + BN) * 128, SEG = (BM + BN) / 8, LPT = SEG / NW, GROUP_M = 8;
     constexpr int ON = KIND == LIN_GLU ? TN / 2 : TN, PITCH = ON * 2 + 16, CH = ON / 8;        // columns of a wave's result; its rows in LDS, in 16-byte pieces
     constexpr int PASS = NW * TM * PITCH <= NS * STAGE ? TM : 32;     // rows of it at a time
-    static_assert(SEG % NW == 0 && LPT % 2 == 0 && BM <= NW * 64 && BN <= NW * 64 && NW * PASS * PITCH <= NS * STAGE, "tile shape");
+    static_assert(BN % 64 == 0 && SEG % NW == 0 && LPT % 2 == 0 && BM <= NW * 64 && NW * PASS * PITCH <= NS * STAGE, "tile shape");
     extern __shared__ __attribute__((aligned(128))) unsigned char smem[];   // stages | bias of the tile's weight rows | where its rows go
     float* bias = reinterpret_cast<float*>(smem + NS * STAGE);
     uint32_t* out_at = reinterpret_cast<uint32_t*>(bias + BN);
@@ -151,17 +151,10 @@ __global__ void __launch_bounds__(WM * WN * 64) linear_tile_kernel(const LinArgs
         lds_read16<i * 2048>(fw[p % R], wa[ks]);
     };
 
+    stage_bias<BN, NW, KIND>(a, bias, n0, wave);
 #pragma unroll
     for (int t = 0; t < NS - 1; ++t)
         if (t < bound) issue(NO, t, t);
-    if (tid < BN) {
-        int n = tid;
-        if constexpr (KIND == LIN_GLU) n = n / 32 * 16 + n % 16;
-        n += n0;
-        n = n < a.N ? n : a.N - 1;
-        if constexpr (KIND == LIN_GLU) n += tid / 16 % 2 ? a.N : 0;
-        bias[tid] = a.bias ? a.bias[n] : 0.f;
-    }
     if (tid < BM) {
         int slot, token;
         const bool live = locate_row(a, group, row0 + tid, slot, token);
@@ -278,7 +271,8 @@ template <typename T, int KIND> drf_status launch_linear_direct(int form, const 
     case 0: return launch_direct_shape<T, KIND, 1, KIND == LIN_GLU ? 2 : 1, 16, 5>(a, st);
     case 1: return launch_direct_shape<T, KIND, 1, 4, 8, 3>(a, st);
     case 2: return launch_direct_shape<T, KIND, 2, 2, 8, 3>(a, st);
-    default: return launch_direct_shape<T, KIND, 4, 2, 8, 2>(a, st);
+    case 3: return launch_direct_shape<T, KIND, 4, 2, 8, 2>(a, st);
+    default: return launch_direct_shape<T, KIND, 1, 2, 8, 4>(a, st);
     }
 }
 

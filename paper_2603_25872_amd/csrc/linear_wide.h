@@ -20,7 +20,7 @@ __global__ void __launch_bounds__(256, 1) linear_wide_kernel(const LinArgs a)
     static_assert(KIND != LIN_GLU || BN == 256, "pairs of pieces in a wave");
     extern __shared__ __attribute__((aligned(128))) unsigned char smem[];   // two stages | bias of the tile's weight rows | where its rows go
     float* bias = reinterpret_cast<float*>(smem + 2 * STAGE);
-    uint32_t* out_at = reinterpret_cast<uint32_t*>(bias + BN);
+    uint32_t* out_at = reinterpret_cast<uint32_t*>(bias + (BN + 63) / 64 * 64);
 
     const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, quarter = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave & 1, wn = wave >> 1;
@@ -146,15 +146,8 @@ __global__ void __launch_bounds__(256, 1) linear_wide_kernel(const LinArgs a)
     constexpr std::true_type YES{};
     constexpr std::false_type NO{};
 
+    stage_bias<BN, 4, KIND>(a, bias, n0, wave);
     static_for<0, NL>([&](auto ic) __attribute__((always_inline)) { copy_one(ic, NO, 0, 0); });
-    for (int t = tid; t < BN; t += 256) {
-        int n = t;
-        if constexpr (KIND == LIN_GLU) n = n / 32 * 16 + n % 16;
-        n += n0;
-        n = n < a.N ? n : a.N - 1;
-        if constexpr (KIND == LIN_GLU) n += t / 16 % 2 ? a.N : 0;
-        bias[t] = a.bias ? a.bias[n] : 0.f;
-    }
     {
         int slot, token;
         const bool live = locate_row(a, group, row0 + tid, slot, token);
@@ -227,7 +220,7 @@ __global__ void __launch_bounds__(256, 1) linear_wide_kernel(const LinArgs a)
 
 template <int BN, int KIND> drf_status launch_wide_shape(LinArgs a, hipStream_t st)
 {
-    constexpr size_t smem = (size_t)2 * (256 + BN) * 128 + BN * 4 + 256 * 4;
+    constexpr size_t smem = (size_t)2 * (256 + BN) * 128 + (BN + 63) / 64 * 256 + 256 * 4;
     static_assert(smem <= 160 * 1024, "LDS of a CU");
     static std::atomic<uint64_t> lds_allowed{ 0 };
     auto kern = linear_wide_kernel<BN, KIND>;
