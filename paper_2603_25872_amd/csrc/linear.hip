@@ -52,7 +52,6 @@ template <typename T, int KIND> int pick_form(const LinArgs& a, double* us)
         const double groups = (double)((rows + 16 * m.mi - 1) / (16 * m.mi)) * ((weight_rows + 16 * m.ni - 1) / (16 * m.ni));
         double t = m.fixed + (pieces + m.nw - 1) / m.nw * m.turn + std::max(0.0, groups / 256 - m.hidden) * (m.group + pieces * m.piece);
         if (KIND == LIN_ADAPT && a.adapters) t += (0.3 + 0.01 * a.rank) * (1 + groups / 256);
-        if (f == kForms - 1) t *= 1.08;                             // (level with the first and third it has lost in pairs and with adapters)
         if (t < *us) { *us = t; best = f; }
     }
     return best;
@@ -61,12 +60,12 @@ thread_local int g_forced_tile = -1;                    // see drf_probe_linear_
 
 // ---- x A^T ------------------------------------------------------------------------------------------------
 // 16 MI rows of one slot by 32 of the rank's columns a workgroup, operands straight to registers, the inner axis dealt over NW waves, 128 bytes of it at a
-// time with U turns on the way, that add up through LDS.  Reads x once for every 32 columns of the rank; bound by that.  fp32 sums go out as they are, for bf16
+// time with U turns on the way (U = 0: all at once), that add up through LDS.  Reads x once for every 32 columns of the rank; bound by that.  fp32 sums go out as they are, for bf16
 // as two operands: the upper 8 bits of the fp32 value and the rest rounded to 8 (2^-16 of the value is lost); one that is no number is itself and zero.
 template <typename T, int MI, int NW, int U>
 __global__ void __launch_bounds__(NW * 64) adapters_low_kernel(const LinArgs a)
 {
-    constexpr int E = 16 / sizeof(T), CHUNK = 8 * E, TURN = NW * CHUNK;
+    constexpr int E = 16 / sizeof(T);
     __shared__ f32x4 part[NW][2 * MI][64];
     const int lane = threadIdx.x & 63, l16 = lane & 15, quarter = lane >> 4, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const long long id = a.first + blockIdx.x;
@@ -90,33 +89,12 @@ __global__ void __launch_bounds__(NW * 64) adapters_low_kernel(const LinArgs a)
     for (int i = 0; i < 2; ++i)
 #pragma unroll
         for (int j = 0; j < MI; ++j) acc[i][j] = (f32x4){ 0.f, 0.f, 0.f, 0.f };
-    u32x4 fx[U][2][MI], fw[U][2][2];
-    auto load = [&](int t, int k0) __attribute__((always_inline)) {
+    if constexpr (U > 0) direct_product<T, MI, 2, NW, U>(acc, x, w, a.K, wave, quarter);
+    else if (wave == 0)                             // (rows of less than 16 bytes)
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int k = k0 + (4 * h + quarter) * E;
+        for (int i = 0; i < 2; ++i)
 #pragma unroll
-            for (int j = 0; j < MI; ++j) fx[t][h][j] = load_row16(x[j], k, a.K);
-#pragma unroll
-            for (int i = 0; i < 2; ++i) fw[t][h][i] = load_row16(w[i], k, a.K);
-        }
-    };
-#pragma unroll
-    for (int t = 0; t < U; ++t)
-        if (wave * CHUNK + t * TURN < a.K) load(t, wave * CHUNK + t * TURN);
-    for (int k = wave * CHUNK; k < a.K; k += U * TURN) {
-#pragma unroll
-        for (int t = 0; t < U; ++t) {
-            if (k + t * TURN < a.K)
-#pragma unroll
-                for (int h = 0; h < 2; ++h)
-#pragma unroll
-                    for (int i = 0; i < 2; ++i)
-#pragma unroll
-                        for (int j = 0; j < MI; ++j) acc[i][j] = mma(fw[t][h][i], fx[t][h][j], acc[i][j], T{});
-            if (k + (U + t) * TURN < a.K) load(t, k + (U + t) * TURN);
-        }
-    }
+            for (int j = 0; j < MI; ++j) acc[i][j] = mma(load_row16(w[i], quarter * E, a.K), load_row16(x[j], quarter * E, a.K), acc[i][j], T{});
 #pragma unroll
     for (int i = 0; i < 2; ++i)
 #pragma unroll
@@ -165,6 +143,9 @@ template <typename T, int MI, int NW, int U> drf_status launch_low(LinArgs a, hi
 
 template <typename T> drf_status run_low(const LinArgs& a, hipStream_t st)
 {
+    if constexpr (sizeof(T) == 4) {
+        if (a.K < 4) return launch_low<T, 1, 1, 0>(a, st);
+    }
     return a.tokens <= 16 ? launch_low<T, 1, 8, 3>(a, st) : (long long)a.slots * ((a.tokens + 63) / 64) < 512 ? launch_low<T, 2, 8, 3>(a, st) : launch_low<T, 4, 4, 3>(a, st);
 }
 
@@ -342,9 +323,9 @@ template <int KIND> drf_status launch_f32(const LinArgs& a, hipStream_t st)
 {
     double us;
     const int form = pick_form<float, KIND>(a, &us), forced = g_forced_tile - kTiles;
-    if (forced >= 0 && forced < kForms) return launch_linear_direct<float, KIND>(forced, a, st);
+    if (forced >= 0 && forced < kForms && a.K >= 4) return launch_linear_direct<float, KIND>(forced, a, st);     // (rows of at least 16 bytes)
     const long long tiles = ((long long)a.slots * a.tokens + 63) / 64 * (((KIND == LIN_GLU ? 2LL * a.N : a.N) + 63) / 64);
-    if (forced != kForms && us < tile_us(kTileF32, tiles, (a.K + 31) / 32)) return launch_linear_direct<float, KIND>(form, a, st);
+    if (forced != kForms && a.K >= 4 && us < tile_us(kTileF32, tiles, (a.K + 31) / 32)) return launch_linear_direct<float, KIND>(form, a, st);
     return launch_f32_tiles<KIND>(a, st);
 }
 
@@ -377,8 +358,8 @@ template <int KIND> drf_status launch_bf16(LinArgs a, hipStream_t st)
         const Tile& m = kLinTiles[t];
         const long long tn = (weight_rows + m.bn - 1) / m.bn, by_slot = (long long)a.slots * ((a.tokens + m.bm - 1) / m.bm);
         if (KIND == LIN_GLU && m.bn % 64) continue;                    // (pairs of pieces in a wave)
-        const bool large = m.bm * m.bn >= 256 * 256;
-        // (the largest tiles have adapters as steps of its loop only, which keeps to a slot)
+        const bool large = m.bm * m.bn >= 256 * 128;
+        // (the largest tiles have adapters as steps of their loop only, and then keep to a slot)
         const bool keep = !cross || (KIND == LIN_ADAPT && large && a.adapters);
         if (KIND == LIN_ADAPT && large && a.adapters && !a.b_vec) continue;
         const long long tm = keep ? by_slot : std::min(by_slot, ((long long)a.slots * a.tokens + m.bm - 1) / m.bm);
@@ -394,7 +375,7 @@ template <int KIND> drf_status launch_bf16(LinArgs a, hipStream_t st)
     if (g_forced_tile < 0 && form_us < best_us) return launch_linear_direct<bf16_t, KIND>(form, a, st);
     const Tile& m = kLinTiles[best];
     const int by_slot = a.slots * ((a.tokens + m.bm - 1) / m.bm), crossing = (a.slots * a.tokens + m.bm - 1) / m.bm;
-    const bool crosses = cross && crossing < by_slot && !(KIND == LIN_ADAPT && m.bm * m.bn >= 256 * 256 && a.adapters);
+    const bool crosses = cross && crossing < by_slot && !(KIND == LIN_ADAPT && m.bm * m.bn >= 256 * 128 && a.adapters);
     a.in_loop = KIND == LIN_ADAPT && !crosses && a.b_vec;
     a.slot_rows = crosses ? a.slots * a.tokens : a.tokens;
     a.slot_tiles = (a.slot_rows + m.bm - 1) / m.bm;

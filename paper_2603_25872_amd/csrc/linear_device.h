@@ -103,32 +103,54 @@ __device__ __forceinline__ void add_adapters(f32x4 (&acc)[NI][MI], const LinArgs
     const int lane = threadIdx.x & 63, l16 = lane & 15, quarter = lane >> 4, LC = a.low_cols;
     if (!a.adapters) return;
     if (a.tokens < 16) {
+        bool some[MI];
+        const bf16_t *t[MI], *b0[MI];
 #pragma unroll
-        for (int j = 0; j < MI; ++j) {
+        for (int j = 0; j < MI; ++j) {                              // (all rows' adapters, then all their loads beside one another; those of a row without one are some row's)
             int slot, token;
-            if (!locate_row(a, group, mw + 16 * j + l16, slot, token)) continue;
+            some[j] = locate_row(a, group, mw + 16 * j + l16, slot, token);
+            if (!some[j]) slot = token = 0;
             const int ad = adapter_of(a, slot);
-            if (ad < 0) continue;
-            const bf16_t* t = (const bf16_t*)a.low + ((size_t)slot * a.tokens + token) * 2 * LC;
-            const bf16_t* b0 = (const bf16_t*)a.b + (size_t)ad * a.N * a.rank;
-            for (int k = 0; k < a.rank; k += 8) {                   // (all pieces' loads beside one another)
-                const bf16x8 hi = *reinterpret_cast<const bf16x8*>(t + k), lo = *reinterpret_cast<const bf16x8*>(t + LC + k);
-                u32x4 f[NI][4];
-#pragma unroll
-                for (int i = 0; i < NI; ++i)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        const int n = nw + 16 * i + 4 * quarter + r;
-                        f[i][r] = load16(b0 + (size_t)(n < a.N ? n : a.N - 1) * a.rank, k, a.rank, a.b_vec);
-                    }
-#pragma unroll
-                for (int i = 0; i < NI; ++i)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r)
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) acc[i][j][r] = fmaf((float)hi[e] + (float)lo[e], (float)__builtin_bit_cast(bf16x8, f[i][r])[e], acc[i][j][r]);
-            }
+            some[j] = some[j] && ad >= 0;
+            t[j] = (const bf16_t*)a.low + ((size_t)slot * a.tokens + token) * 2 * LC;
+            b0[j] = (const bf16_t*)a.b + (size_t)(ad < 0 ? 0 : ad) * a.N * a.rank;
         }
+        constexpr int JG = NI <= 2 ? 2 : 1;                         // rows' pieces at a time
+#pragma unroll
+        for (int j0 = 0; j0 < MI; j0 += JG)
+            for (int k = 0; k < a.rank; k += 8) {
+                bf16x8 hi[JG], lo[JG];
+                u32x4 f[JG][NI][4];
+#pragma unroll
+                for (int j = 0; j < JG; ++j) {
+                    hi[j] = *reinterpret_cast<const bf16x8*>(t[j0 + j] + k);
+                    lo[j] = *reinterpret_cast<const bf16x8*>(t[j0 + j] + LC + k);
+#pragma unroll
+                    for (int i = 0; i < NI; ++i)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) {
+                            const int n = nw + 16 * i + 4 * quarter + r;
+                            f[j][i][r] = load16(b0[j0 + j] + (size_t)(n < a.N ? n : a.N - 1) * a.rank, k, a.rank, a.b_vec);
+                        }
+                }
+#pragma unroll
+                for (int j = 0; j < JG; ++j) {
+                    float low[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) low[e] = (float)hi[j][e] + (float)lo[j][e];
+#pragma unroll
+                    for (int i = 0; i < NI; ++i) {
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) {
+                            float v = 0.f;
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) v = fmaf(low[e], (float)__builtin_bit_cast(bf16x8, f[j][i][r])[e], v);
+                            acc[i][j0 + j][r] += some[j0 + j] ? v : 0.f;
+                        }
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+                }
+            }
         return;
     }
     auto slot_of = [&](int m) { return a.slot_rows == a.tokens ? group : fast_div(m < a.slot_rows ? m : a.slot_rows - 1, a.tok_magic, a.tok_shift); };
@@ -164,32 +186,43 @@ __device__ __forceinline__ void add_adapters(f32x4 (&acc)[NI][MI], const LinArgs
         }
         return;
     }
+    // several slots, one after the other: each on the rows' pieces that it reaches into
+    const bf16_t* t[MI];
+    int mine[MI];
 #pragma unroll
     for (int j = 0; j < MI; ++j) {
-        const int m = mw + 16 * j, last = slot_of(m + 15), mine = slot_of(m + l16);
-        for (int s = slot_of(m); s <= last; ++s) {
-            const int ad = adapter_of(a, s);
-            if (ad < 0) continue;
-            const bf16_t* t = low_row(m + l16) + 8 * quarter;
-            constexpr int NG = NI < 4 ? NI : 4;                     // pieces at a time
+        t[j] = low_row(mw + 16 * j + l16) + 8 * quarter;
+        mine[j] = slot_of(mw + 16 * j + l16);
+    }
+    const int last = slot_of(mw + 16 * MI - 1);
+    for (int s = slot_of(mw); s <= last; ++s) {
+        const int ad = adapter_of(a, s);
+        if (ad < 0) continue;
+        constexpr int NG = MI >= 4 || NI < 4 ? 2 : 4;               // pieces at a time
 #pragma unroll
-            for (int i0 = 0; i0 < NI; i0 += NG) {
-                f32x4 sum[NG];
+        for (int i0 = 0; i0 < NI; i0 += NG) {
+            f32x4 sum[MI][NG];
 #pragma unroll
-                for (int i = 0; i < NG; ++i) sum[i] = (f32x4){ 0.f, 0.f, 0.f, 0.f };
-                for (int k = 0; k < LC; k += 32) {
-                    const u32x4 hi = *reinterpret_cast<const u32x4*>(t + k), lo = *reinterpret_cast<const u32x4*>(t + LC + k);
+            for (int j = 0; j < MI; ++j)
 #pragma unroll
-                    for (int i = 0; i < NG; ++i) {
-                        const u32x4 f = b_frag(ad, i0 + i, k);
-                        sum[i] = mma_bf16(f, lo, mma_bf16(f, hi, sum[i]));
-                    }
+                for (int i = 0; i < NG; ++i) sum[j][i] = (f32x4){ 0.f, 0.f, 0.f, 0.f };
+            for (int k = 0; k < LC; k += 32) {
+                u32x4 f[NG];
+#pragma unroll
+                for (int i = 0; i < NG; ++i) f[i] = b_frag(ad, i0 + i, k);
+#pragma unroll
+                for (int j = 0; j < MI; ++j) {
+                    const u32x4 hi = *reinterpret_cast<const u32x4*>(t[j] + k), lo = *reinterpret_cast<const u32x4*>(t[j] + LC + k);
+#pragma unroll
+                    for (int i = 0; i < NG; ++i) sum[j][i] = mma_bf16(f[i], lo, mma_bf16(f[i], hi, sum[j][i]));
                 }
+            }
+#pragma unroll
+            for (int j = 0; j < MI; ++j)
 #pragma unroll
                 for (int i = 0; i < NG; ++i)
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) acc[i0 + i][j][r] += mine == s ? sum[i][r] : 0.f;
-            }
+                    for (int r = 0; r < 4; ++r) acc[i0 + i][j][r] += mine[j] == s ? sum[j][i][r] : 0.f;
         }
     }
 }

@@ -34,6 +34,76 @@ template <typename T> __device__ inline u32x4 load_row16(const T* row, int k, in
     return z;
 }
 
+// The same in two parts, for rows of at least 16 bytes: a load that asks nothing (16 bytes that lie in the row, the last ones where k is near its end), so that many go out
+// one behind the other, and what they are once they are there.
+template <typename T> __device__ inline u32x4 load_near(const T* row, int k, int n)
+{
+    constexpr int E = 16 / sizeof(T);
+    typedef T piece __attribute__((ext_vector_type(E), aligned(sizeof(T))));
+    return __builtin_bit_cast(u32x4, *reinterpret_cast<const piece*>(row + (k + E <= n ? k : n - E)));
+}
+__device__ inline u32x4 row_piece(u32x4 v, int k, int n, bf16_t) { return k < n ? v : (u32x4){ 0, 0, 0, 0 }; }     // (n is a multiple of 8)
+__device__ inline u32x4 row_piece(u32x4 v, int k, int n, float)
+{
+    const int c = n - k;
+    u32x4 r;
+    r[0] = c >= 4 ? v[0] : c == 3 ? v[1] : c == 2 ? v[2] : c == 1 ? v[3] : 0u;
+    r[1] = c >= 4 ? v[1] : c == 3 ? v[2] : c == 2 ? v[3] : 0u;
+    r[2] = c >= 4 ? v[2] : c == 3 ? v[3] : 0u;
+    r[3] = c >= 4 ? v[3] : 0u;
+    return r;
+}
+
+// acc += w x^T over a wave's share of the inner axis: turns of 128 bytes, wave, wave + NW, .., U of them on the way.
+template <typename T, int MI, int NI, int NW, int U>
+__device__ __forceinline__ void direct_product(f32x4 (&acc)[NI][MI], const T* const (&x)[MI], const T* const (&w)[NI], int K, int wave, int quarter)
+{
+    constexpr int E = 16 / sizeof(T), CHUNK = 8 * E, TURN = NW * CHUNK;
+    const int first = wave * CHUNK, turns = first < K ? (K - first + TURN - 1) / TURN : 0;
+    u32x4 fx[U][2][MI], fw[U][2][NI];
+    auto load = [&](int t, int turn) __attribute__((always_inline)) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int k = first + turn * TURN + (4 * h + quarter) * E;
+#pragma unroll
+            for (int i = 0; i < NI; ++i) fw[t][h][i] = load_near(w[i], k, K);
+#pragma unroll
+            for (int j = 0; j < MI; ++j) fx[t][h][j] = load_near(x[j], k, K);
+        }
+    };
+    auto multiply = [&](int t, int turn) __attribute__((always_inline)) {
+        if (first + turn * TURN + CHUNK > K) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int k = first + turn * TURN + (4 * h + quarter) * E;
+#pragma unroll
+                for (int i = 0; i < NI; ++i) fw[t][h][i] = row_piece(fw[t][h][i], k, K, T{});
+#pragma unroll
+                for (int j = 0; j < MI; ++j) fx[t][h][j] = row_piece(fx[t][h][j], k, K, T{});
+            }
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int i = 0; i < NI; ++i)
+#pragma unroll
+                for (int j = 0; j < MI; ++j) acc[i][j] = mma(fw[t][h][i], fx[t][h][j], acc[i][j], T{});
+    };
+#pragma unroll
+    for (int t = 0; t < U; ++t)
+        if (t < turns) load(t, t);
+    int it = 0;
+    for (; it + 2 * U <= turns; it += U)            // (no questions between the loads: they are counted, and none waits for all)
+#pragma unroll
+        for (int t = 0; t < U; ++t) { multiply(t, it + t); load(t, it + t + U); }
+    for (; it < turns; it += U)
+#pragma unroll
+        for (int t = 0; t < U; ++t) {
+            if (it + t < turns) multiply(t, it + t);
+            if (it + t + U < turns) load(t, it + t + U);
+        }
+}
+
 // The adapter's part of four columns from n on of a row: x A^T of it times B's rows.
 template <typename T> __device__ inline void add_low(f32x4& v, const LinArgs& a, int slot, int token, int n)
 {
@@ -71,7 +141,6 @@ template <typename T> __device__ inline void add_low(f32x4& v, const LinArgs& a,
 template <typename T, int KIND, int MI, int NI, int NW, int U>
 __global__ void __launch_bounds__(NW * 64) linear_direct_kernel(const LinArgs a)
 {
-    constexpr int E = 16 / sizeof(T), CHUNK = 8 * E;                // elements of a turn
     static_assert(KIND != LIN_GLU || NI % 2 == 0, "gates and values");
     static_assert(NW * MI * NI <= 64, "partial sums in 64 KB");
     __shared__ f32x4 part[NW][MI * NI][64];
@@ -99,36 +168,7 @@ __global__ void __launch_bounds__(NW * 64) linear_direct_kernel(const LinArgs a)
     for (int i = 0; i < NI; ++i)
 #pragma unroll
         for (int j = 0; j < MI; ++j) acc[i][j] = (f32x4){ 0.f, 0.f, 0.f, 0.f };
-    u32x4 fx[U][2][MI], fw[U][2][NI];                               // [turn][half]
-    auto load = [&](int t, int k0) __attribute__((always_inline)) {
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int k = k0 + (4 * h + quarter) * E;
-#pragma unroll
-            for (int i = 0; i < NI; ++i) fw[t][h][i] = load_row16(w[i], k, a.K);
-#pragma unroll
-            for (int j = 0; j < MI; ++j) fx[t][h][j] = load_row16(x[j], k, a.K);
-        }
-    };
-    auto multiply = [&](int t) __attribute__((always_inline)) {
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int i = 0; i < NI; ++i)
-#pragma unroll
-                for (int j = 0; j < MI; ++j) acc[i][j] = mma(fw[t][h][i], fx[t][h][j], acc[i][j], T{});
-    };
-    constexpr int TURN = NW * CHUNK;
-#pragma unroll
-    for (int t = 0; t < U; ++t)
-        if (wave * CHUNK + t * TURN < a.K) load(t, wave * CHUNK + t * TURN);
-    for (int k = wave * CHUNK; k < a.K; k += U * TURN) {
-#pragma unroll
-        for (int t = 0; t < U; ++t) {
-            if (k + t * TURN < a.K) multiply(t);
-            if (k + (U + t) * TURN < a.K) load(t, k + (U + t) * TURN);
-        }
-    }
+    direct_product<T, MI, NI, NW, U>(acc, x, w, a.K, wave, quarter);
 #pragma unroll
     for (int i = 0; i < NI; ++i)
 #pragma unroll

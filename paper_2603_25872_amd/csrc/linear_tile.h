@@ -224,7 +224,7 @@ __global__ void __launch_bounds__(WM * WN * 64) linear_tile_kernel(const LinArgs
 #pragma unroll
     for (int j = 0; j < MI; ++j) { hold_frag(fa[0][j]); hold_frag(fa[1][j]); }
 
-    if constexpr (KIND == LIN_ADAPT && BM * BN < 256 * 256) {
+    if constexpr (KIND == LIN_ADAPT && BM * BN < 256 * 128) {
         if (!a.in_loop) add_adapters(acc, a, group, row0 + wm * TM, n0 + wn * TN);
     }
 
@@ -268,7 +268,7 @@ template <int KIND> drf_status launch_linear_tile(int tile, const LinArgs& a, hi
 template <typename T, int KIND> drf_status launch_linear_direct(int form, const LinArgs& a, hipStream_t st)
 {
     switch (form) {
-    case 0: return launch_direct_shape<T, KIND, 1, KIND == LIN_GLU ? 2 : 1, 16, 5>(a, st);
+    case 0: return launch_direct_shape<T, KIND, 1, KIND == LIN_GLU ? 2 : 1, 16, KIND == LIN_GLU ? 2 : 5>(a, st);     // (16 waves: 128 registers a lane)
     case 1: return launch_direct_shape<T, KIND, 1, 4, 8, 3>(a, st);
     case 2: return launch_direct_shape<T, KIND, 2, 2, 8, 3>(a, st);
     case 3: return launch_direct_shape<T, KIND, 4, 2, 8, 2>(a, st);
