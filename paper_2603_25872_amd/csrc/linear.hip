@@ -39,6 +39,23 @@ double tile_us(const Tile& m, long long tiles, int steps)
     return m.base + full * (m.round + steps * std::max(m.lat, m.per_cu * m.thr)) + (share ? m.round + steps * std::max(m.lat, share * m.thr) : 0.0);
 }
 
+// What adapters add, x A^T's launch included: first + pieces of 8 of the rank * rank + workgroups / 256 * (group + pieces * group_rank) us for a form (fitted to products of
+// 1 to 800 rows of 1 to 40 slots, ranks of 8 to 128, 4 % off on average; unaligned rows of B count 1.7 times).  With it the choice is within 2 % of the best on average, 24 %
+// at worst; it matters most where every row has an adapter of its own (200 x 384 x 1152, rank 128, fp32: 31 us, the tile 220).
+struct FormAdapters { double first, rank, group, group_rank; };
+const FormAdapters kAdaptBf16[kForms] = { { 1.96, 0.232, 0, 0.246 }, { 2.36, 0.422, 0.476, 0.07 }, { 2.32, 0.401, 0.492, 0.075 }, { 2.39, 0.80, 0.69, 0.1 }, { 2.13, 0.306, 0.165, 0.219 } };
+const FormAdapters kAdaptF32[kForms] = { { 2.65, 0.307, 0.066, 0.35 }, { 3.08, 0.55, 0.632, 0.058 }, { 2.81, 0.491, 0.563, 0.072 }, { 2.78, 0.848, 0.3, 0.05 }, { 2.59, 0.359, 0.153, 0.25 } };
+
+// The same for the bf16 tiles: steps of the loop, or behind it a lane's elements one by one (slots shorter than 16 rows), or slot after slot.
+double tile_adapters_us(const Tile& m, const LinArgs& a, long long tiles, bool crosses)
+{
+    const double rounds = (double)((tiles + 256 * m.per_cu - 1) / (256 * m.per_cu));
+    const int pieces = m.bm * m.bn >= 128 * 64 ? 8 : 4, eights = (a.rank + 7) / 8, steps = (a.rank + 31) / 32;     // of 16 x 16 in a wave's tile
+    if (!crosses && a.b_vec) return 2.5 + 0.2 * steps;
+    if (a.tokens < 16) return rounds * (4.5 + 0.4 * pieces * eights * (a.b_vec ? 1.0 : 3.5));
+    return rounds * (4 + 0.25 * pieces + 0.11 * pieces * steps * (crosses ? std::min(a.slots, 31 / a.tokens + 2) : 1) + (a.b_vec ? 0 : 3));
+}
+
 // The form with the least modelled time, and that time.
 template <typename T, int KIND> int pick_form(const LinArgs& a, double* us)
 {
@@ -51,7 +68,11 @@ template <typename T, int KIND> int pick_form(const LinArgs& a, double* us)
         const Form& m = forms[f];
         const double groups = (double)((rows + 16 * m.mi - 1) / (16 * m.mi)) * ((weight_rows + 16 * m.ni - 1) / (16 * m.ni));
         double t = m.fixed + (pieces + m.nw - 1) / m.nw * m.turn + std::max(0.0, groups / 256 - m.hidden) * (m.group + pieces * m.piece);
-        if (KIND == LIN_ADAPT && a.adapters) t += (0.3 + 0.01 * a.rank) * (1 + groups / 256);
+        if (KIND == LIN_ADAPT && a.adapters) {
+            const FormAdapters& p = (sizeof(T) == 2 ? kAdaptBf16 : kAdaptF32)[f];
+            const double eights = (a.rank + 7) / 8 * (sizeof(T) == 2 && !a.b_vec ? 1.7 : 1.0);
+            t += p.first + eights * p.rank + groups / 256 * (p.group + eights * p.group_rank);
+        }
         if (t < *us) { *us = t; best = f; }
     }
     return best;
@@ -325,7 +346,12 @@ template <int KIND> drf_status launch_f32(const LinArgs& a, hipStream_t st)
     const int form = pick_form<float, KIND>(a, &us), forced = g_forced_tile - kTiles;
     if (forced >= 0 && forced < kForms && a.K >= 4) return launch_linear_direct<float, KIND>(forced, a, st);     // (rows of at least 16 bytes)
     const long long tiles = ((long long)a.slots * a.tokens + 63) / 64 * (((KIND == LIN_GLU ? 2LL * a.N : a.N) + 63) / 64);
-    if (forced != kForms && a.K >= 4 && us < tile_us(kTileF32, tiles, (a.K + 31) / 32)) return launch_linear_direct<float, KIND>(form, a, st);
+    double tile = tile_us(kTileF32, tiles, (a.K + 31) / 32);
+    if (KIND == LIN_ADAPT && a.adapters) {                          // slot after slot of a wave's 32 rows
+        const int reach = std::min(std::min(a.slots, 32), 31 / a.tokens + 1 + (a.tokens > 1));
+        tile += 1.1 + 1.1 * std::max(1.0, tiles / 256.0) + reach * (0.42 + 0.64 * ((a.rank + 15) / 16)) * (double)((tiles + 1023) / 1024);
+    }
+    if (forced != kForms && a.K >= 4 && us < tile) return launch_linear_direct<float, KIND>(form, a, st);
     return launch_f32_tiles<KIND>(a, st);
 }
 
@@ -365,7 +391,7 @@ template <int KIND> drf_status launch_bf16(LinArgs a, hipStream_t st)
         const long long tm = keep ? by_slot : std::min(by_slot, ((long long)a.slots * a.tokens + m.bm - 1) / m.bm);
         const bool crosses = !keep && tm < by_slot;
         double us = tile_us(m, tm * tn, steps + (KIND == LIN_ADAPT && a.adapters && !crosses && a.b_vec ? a.low_cols / 32 : 0));
-        if (KIND == LIN_ADAPT && a.adapters && (crosses || !a.b_vec)) us += (2.0 + 0.05 * a.rank) * (1 + tm * tn / (256 * m.per_cu));
+        if (KIND == LIN_ADAPT && a.adapters) us += tile_adapters_us(m, a, tm * tn, crosses);
         if (t == g_forced_tile) { best = t; break; }
         if (us < best_us) { best_us = us; best = t; }
     }

@@ -54,9 +54,11 @@ __device__ inline u32x4 row_piece(u32x4 v, int k, int n, float)
     return r;
 }
 
-// acc += w x^T over a wave's share of the inner axis: turns of 128 bytes, wave, wave + NW, .., U of them on the way.
-template <typename T, int MI, int NI, int NW, int U>
-__device__ __forceinline__ void direct_product(f32x4 (&acc)[NI][MI], const T* const (&x)[MI], const T* const (&w)[NI], int K, int wave, int quarter)
+struct Nothing { __device__ void operator()() const {} };
+
+// acc += w x^T over a wave's share of the inner axis: turns of 128 bytes, wave, wave + NW, .., U of them on the way.  beside(): other loads, behind the first of these.
+template <typename T, int MI, int NI, int NW, int U, typename F = Nothing>
+__device__ __forceinline__ void direct_product(f32x4 (&acc)[NI][MI], const T* const (&x)[MI], const T* const (&w)[NI], int K, int wave, int quarter, F beside = F{})
 {
     constexpr int E = 16 / sizeof(T), CHUNK = 8 * E, TURN = NW * CHUNK;
     const int first = wave * CHUNK, turns = first < K ? (K - first + TURN - 1) / TURN : 0;
@@ -92,6 +94,7 @@ __device__ __forceinline__ void direct_product(f32x4 (&acc)[NI][MI], const T* co
 #pragma unroll
     for (int t = 0; t < U; ++t)
         if (t < turns) load(t, t);
+    beside();
     int it = 0;
     for (; it + 2 * U <= turns; it += U)            // (no questions between the loads: they are counted, and none waits for all)
 #pragma unroll
@@ -168,18 +171,28 @@ __global__ void __launch_bounds__(NW * 64) linear_direct_kernel(const LinArgs a)
     for (int i = 0; i < NI; ++i)
 #pragma unroll
         for (int j = 0; j < MI; ++j) acc[i][j] = (f32x4){ 0.f, 0.f, 0.f, 0.f };
-    direct_product<T, MI, NI, NW, U>(acc, x, w, a.K, wave, quarter);
+    // results of 16 x 16, one for each of the first waves: lane (l16, quarter) has columns 4 quarter .. + 3 of row l16.  Its bias is asked for beside the product's operands
+    // (feed-forward of 1 x 1152 x 4608: 17.2 -> 16.3 us; an adapter's operands asked for there as well took 64 x 1152 x 6912 of rank 16 from 16.4 to 17.0 us).
+    constexpr int OUT = KIND == LIN_GLU ? NI / 2 : NI;
+    static_assert(OUT * MI <= NW, "a result a wave");
+    const int i = wave / MI, j = wave - i * MI, n = n0 + 16 * i + 4 * quarter, row = row0 + 16 * j + l16;
+    float bias[KIND == LIN_GLU ? 2 : 1][4] = {};
+    direct_product<T, MI, NI, NW, U>(acc, x, w, a.K, wave, quarter, [&]() __attribute__((always_inline)) {
+        if (!a.bias || wave >= OUT * MI) return;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int c = n + r < a.N ? n + r : a.N - 1;
+            bias[0][r] = a.bias[c];
+            if constexpr (KIND == LIN_GLU) bias[1][r] = a.bias[a.N + c];
+        }
+    });
 #pragma unroll
     for (int i = 0; i < NI; ++i)
 #pragma unroll
         for (int j = 0; j < MI; ++j) part[wave][i * MI + j][lane] = acc[i][j];
     __syncthreads();
-    // results of 16 x 16 dealt over the waves: lane (l16, quarter) has columns 4 quarter .. + 3 of row l16
-    constexpr int OUT = KIND == LIN_GLU ? NI / 2 : NI;
-    for (int p = wave; p < OUT * MI; p += NW) {
-        const int i = p / MI, j = p - i * MI, n = n0 + 16 * i + 4 * quarter, row = row0 + 16 * j + l16;
-        int sl, tk;
-        if (!locate_row(a, 0, row, sl, tk) || n >= a.N) continue;
+    int sl, tk;
+    if (wave < OUT * MI && locate_row(a, 0, row, sl, tk) && n < a.N) {
         auto total = [&](int piece) {
             f32x4 v = part[0][piece * MI + j][lane];
 #pragma unroll
@@ -192,12 +205,8 @@ __global__ void __launch_bounds__(NW * 64) linear_direct_kernel(const LinArgs a)
         T* o = (T*)a.out.data + sl * a.out.slot_stride + tk * a.out.token_stride + n;
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-            const int c = n + r < a.N ? n + r : a.N - 1;
-            if (a.bias) {
-                v[r] += a.bias[c];
-                if constexpr (KIND == LIN_GLU) u[r] += a.bias[a.N + c];
-            }
-            if constexpr (KIND == LIN_GLU) v[r] = glu(v[r], u[r], a.act);
+            v[r] += bias[0][r];
+            if constexpr (KIND == LIN_GLU) v[r] = glu(v[r], u[r] + bias[1][r], a.act);
         }
         if (n + 4 <= a.N) {
             typedef T four __attribute__((ext_vector_type(4), aligned(sizeof(T))));
