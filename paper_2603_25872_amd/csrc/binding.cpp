@@ -1,10 +1,10 @@
-// The argument marshalling of the skip calls and of the attention operators as CPython functions.
+// The argument marshalling of the skip calls and of the operators as CPython functions.
 //
 // One anchor's skip transitions are a 3.4 us kernel behind a call that took 8.1 us: a launch of ~3 us and 5 us of ctypes structures, array
 // types and argument conversion.  Here the same conversions and checks are done on the objects themselves: 8.1 -> 6.3 us a call
 // (1 x 4096 elements, four targets).  The library's function comes as an address (bind), so this module links to nothing but the interpreter.
 // The operators take two to five strided tensors each; a call that rotates one token: 11.2 -> 8.5 us with the allocation of its output, one that norms and
-// rotates q and k of 12 x 256 tokens: 17.5 -> 11.9 (6.0 of it on the GPU).
+// rotates q and k of 12 x 256 tokens: 17.5 -> 11.9 (6.0 of it on the GPU), one that updates a row of the residual stream: 18.8 -> 10.4.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
@@ -646,7 +646,7 @@ PyMethodDef kMethods[] = {
     { "bind", bind, METH_O, "address of drf_skip_transition_noise" },
     { nullptr, nullptr, 0, nullptr },
 };
-PyModuleDef kModule = { PyModuleDef_HEAD_INIT, "_native", "Argument marshalling of the skip calls and the attention operators", -1, kMethods, nullptr, nullptr, nullptr, nullptr };
+PyModuleDef kModule = { PyModuleDef_HEAD_INIT, "_native", "Argument marshalling of the skip calls and the operators", -1, kMethods, nullptr, nullptr, nullptr, nullptr };
 
 }  // namespace
 

@@ -81,7 +81,8 @@ thread_local int g_forced_tile = -1;                    // see drf_probe_linear_
 
 // ---- x A^T ------------------------------------------------------------------------------------------------
 // 16 MI rows of one slot by 32 of the rank's columns a workgroup, operands straight to registers, the inner axis dealt over NW waves, 128 bytes of it at a
-// time with U turns on the way (U = 0: all at once), that add up through LDS.  Reads x once for every 32 columns of the rank; bound by that.  fp32 sums go out as they are, for bf16
+// time with U turns on the way (U = 0: all at once), that add up through LDS.  Reads x once for every 32 columns of the rank; bound by that: 65536 x 1152 47 us, 3.2 TB/s (on two and one
+// pieces of rows a workgroup 51 and 65), 64 rows of as many requests 5.  fp32 sums go out as they are, for bf16
 // as two operands: the upper 8 bits of the fp32 value and the rest rounded to 8 (2^-16 of the value is lost); one that is no number is itself and zero.
 template <typename T, int MI, int NW, int U>
 __global__ void __launch_bounds__(NW * 64) adapters_low_kernel(const LinArgs a)

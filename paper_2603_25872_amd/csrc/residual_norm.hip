@@ -2,7 +2,8 @@
 //   z = x_scale x + y_scale gate * after(y),  h = before(z) (1 + scale) + shift
 //
 // A row's lanes hold it in registers from its load to its stores: mean, then the squares of what is left of it (two sums, so that a large mean costs nothing
-// of the variance), each over the lanes without LDS where one wave has a row.  Everything is read and written once: bound by memory.
+// of the variance), each over the lanes without LDS where one wave has a row.  Everything is read and written once: bound by memory.  6 x 4096 x 1152, stream in fp32, branch in
+// bf16, LayerNorm before (340 MB): 64.7 us, 5.25 TB/s;  4 x 16384 x 1536 in bf16, RMS on both sides (805 MB): 144 us, 5.6;  a large copy: 5.15.  One row: 4.5 us, a launch.
 #include <algorithm>
 #include <type_traits>
 
