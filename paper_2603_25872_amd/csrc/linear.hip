@@ -29,7 +29,7 @@ struct Form { int mi, ni, nw; double fixed, turn, hidden, group, piece; };
 constexpr int kForms = 5;
 const Form kFormsBf16[kForms] = { { 1, 1, 16, 1.83, 1.13, 0.27, 1.18, 0.095 }, { 1, 4, 8, 1.84, 1.75, 0.40, 0.80, 0.282 }, { 2, 2, 8, 2.18, 1.03, 0.06, 0.85, 0.196 }, { 4, 2, 8, 2.47, 1.47, 0.37, 1.71, 0.343 },
                                   { 1, 2, 8, 2.08, 0.93, 0.25, 0.66, 0.161 } };
-const Form kFormsF32[kForms] = { { 1, 1, 16, 1.80, 1.40, 0.28, 1.40, 0.104 }, { 1, 4, 8, 2.00, 2.23, 0.20, 1.50, 0.304 }, { 2, 2, 8, 2.21, 1.84, 0.34, 1.57, 0.254 }, { 4, 2, 8, 2.31, 3.18, 0.34, 2.68, 0.459 },
+const Form kFormsF32[kForms] = { { 1, 1, 16, 1.80, 1.40, 0.28, 1.40, 0.104 }, { 0 } /* (never ahead) */, { 2, 2, 8, 2.21, 1.84, 0.34, 1.57, 0.254 }, { 4, 2, 8, 2.31, 3.18, 0.34, 2.68, 0.459 },
                                  { 1, 2, 8, 2.10, 1.02, 0.0, 0.71, 0.164 } };
 const Tile kTileF32 = { 64, 64, 4, 0.0, 3.67, 0.692, 0.630 };      // steps of 32
 
@@ -44,7 +44,7 @@ double tile_us(const Tile& m, long long tiles, int steps)
 // at worst; it matters most where every row has an adapter of its own (200 x 384 x 1152, rank 128, fp32: 31 us, the tile 220).
 struct FormAdapters { double first, rank, group, group_rank; };
 const FormAdapters kAdaptBf16[kForms] = { { 1.96, 0.232, 0, 0.246 }, { 2.36, 0.422, 0.476, 0.07 }, { 2.32, 0.401, 0.492, 0.075 }, { 2.39, 0.80, 0.69, 0.1 }, { 2.13, 0.306, 0.165, 0.219 } };
-const FormAdapters kAdaptF32[kForms] = { { 2.65, 0.307, 0.066, 0.35 }, { 3.08, 0.55, 0.632, 0.058 }, { 2.81, 0.491, 0.563, 0.072 }, { 2.78, 0.848, 0.3, 0.05 }, { 2.59, 0.359, 0.153, 0.25 } };
+const FormAdapters kAdaptF32[kForms] = { { 2.65, 0.307, 0.066, 0.35 }, { 0 }, { 2.81, 0.491, 0.563, 0.072 }, { 2.78, 0.848, 0.3, 0.05 }, { 2.59, 0.359, 0.153, 0.25 } };
 
 // The same for the bf16 tiles: steps of the loop, or behind it a lane's elements one by one (slots shorter than 16 rows), or slot after slot.
 double tile_adapters_us(const Tile& m, const LinArgs& a, long long tiles, bool crosses)
@@ -66,6 +66,7 @@ template <typename T, int KIND> int pick_form(const LinArgs& a, double* us)
     *us = 1e300;
     for (int f = 0; f < kForms; ++f) {
         const Form& m = forms[f];
+        if (!m.mi) continue;
         const double groups = (double)((rows + 16 * m.mi - 1) / (16 * m.mi)) * ((weight_rows + 16 * m.ni - 1) / (16 * m.ni));
         double t = m.fixed + (pieces + m.nw - 1) / m.nw * m.turn + std::max(0.0, groups / 256 - m.hidden) * (m.group + pieces * m.piece);
         if (KIND == LIN_ADAPT && a.adapters) {
@@ -345,7 +346,7 @@ template <int KIND> drf_status launch_f32(const LinArgs& a, hipStream_t st)
 {
     double us;
     const int form = pick_form<float, KIND>(a, &us), forced = g_forced_tile - kTiles;
-    if (forced >= 0 && forced < kForms && a.K >= 4) return launch_linear_direct<float, KIND>(forced, a, st);     // (rows of at least 16 bytes)
+    if (forced >= 0 && forced < kForms && kFormsF32[forced].mi && a.K >= 4) return launch_linear_direct<float, KIND>(forced, a, st);     // (rows of at least 16 bytes)
     const long long tiles = ((long long)a.slots * a.tokens + 63) / 64 * (((KIND == LIN_GLU ? 2LL * a.N : a.N) + 63) / 64);
     double tile = tile_us(kTileF32, tiles, (a.K + 31) / 32);
     if (KIND == LIN_ADAPT && a.adapters) {                          // slot after slot of a wave's 32 rows

@@ -272,7 +272,9 @@ template <typename T, int KIND> drf_status launch_linear_direct(int form, const 
 {
     switch (form) {
     case 0: return launch_direct_shape<T, KIND, 1, KIND == LIN_GLU ? 2 : 1, 16, KIND == LIN_GLU ? 2 : 5>(a, st);     // (16 waves: 128 registers a lane)
-    case 1: return launch_direct_shape<T, KIND, 1, 4, 8, 3>(a, st);
+    case 1:
+        if constexpr (sizeof(T) == 2) return launch_direct_shape<T, KIND, 1, 4, 8, 3>(a, st);
+        DRF_FAIL(DRF_EINVAL, "no such form");
     case 2: return launch_direct_shape<T, KIND, 2, 2, 8, 3>(a, st);
     case 3: return launch_direct_shape<T, KIND, 4, 2, 8, 2>(a, st);
     default: return launch_direct_shape<T, KIND, 1, 2, 8, 4>(a, st);
