@@ -101,8 +101,8 @@ int drf_probe_block_route(int slots, int tokens, int hidden, int heads, int mlp_
 drf_status drf_graph_stats(drf_denoiser* den, int* captured, int* failed, long long* replays);
 
 /*
- * The products of drf_gated_ffn and drf_linear_adapters called on this thread from now on run on tile `tile` where it can take them: 0 .. 7 the tiles of bf16, 8 .. 12
- * the forms for few rows, 13 the tile of fp32; -1: by choice.  Returns the number of them.  Host only.
+ * The products of drf_gated_ffn and drf_linear_adapters called on this thread from now on run on tile `tile` where it can take them: 0 .. 7 the tiles of bf16, 8 .. 13
+ * the forms for few rows, 14 the tile of fp32; -1: by choice.  Returns the number of them.  Host only.
  */
 int drf_probe_linear_tile(int tile);
 

@@ -26,11 +26,11 @@ constexpr int kTiles = sizeof(kLinTiles) / sizeof(kLinTiles[0]);
 // The forms for few rows of linear_direct.h, rows and weight rows a workgroup in sixteens and its waves: fixed + turns * turn + max(0, workgroups / 256 - hidden) * (group + 128-byte
 // pieces of the inner axis * piece) us, fitted likewise (140 and 100 products of 1 to 4096 rows; the choice is within 5 % of the best on average in bf16, 3 % in fp32).
 struct Form { int mi, ni, nw; double fixed, turn, hidden, group, piece; };
-constexpr int kForms = 5;
+constexpr int kForms = 6;
 const Form kFormsBf16[kForms] = { { 1, 1, 16, 1.83, 1.13, 0.27, 1.18, 0.095 }, { 1, 4, 8, 1.84, 1.75, 0.40, 0.80, 0.282 }, { 2, 2, 8, 2.18, 1.03, 0.06, 0.85, 0.196 }, { 4, 2, 8, 2.47, 1.47, 0.37, 1.71, 0.343 },
-                                  { 1, 2, 8, 2.08, 0.93, 0.25, 0.66, 0.161 } };
+                                  { 1, 2, 8, 2.08, 0.93, 0.25, 0.66, 0.161 }, { 1, 1, 16, 2.0, 1.3, 0, 0, 0 } /* 8 rows by 8, see below */ };
 const Form kFormsF32[kForms] = { { 1, 1, 16, 1.80, 1.40, 0.28, 1.40, 0.104 }, { 0 } /* (never ahead) */, { 2, 2, 8, 2.21, 1.84, 0.34, 1.57, 0.254 }, { 4, 2, 8, 2.31, 3.18, 0.34, 2.68, 0.459 },
-                                 { 1, 2, 8, 2.10, 1.02, 0.0, 0.71, 0.164 } };
+                                 { 1, 2, 8, 2.10, 1.02, 0.0, 0.71, 0.164 }, { 0 } };
 const Tile kTileF32 = { 64, 64, 4, 0.0, 3.67, 0.692, 0.630 };      // steps of 32
 
 double tile_us(const Tile& m, long long tiles, int steps)
@@ -43,8 +43,8 @@ double tile_us(const Tile& m, long long tiles, int steps)
 // 1 to 800 rows of 1 to 40 slots, ranks of 8 to 128, 4 % off on average; unaligned rows of B count 1.7 times).  With it the choice is within 2 % of the best on average, 24 %
 // at worst; it matters most where every row has an adapter of its own (200 x 384 x 1152, rank 128, fp32: 31 us, the tile 220).
 struct FormAdapters { double first, rank, group, group_rank; };
-const FormAdapters kAdaptBf16[kForms] = { { 1.96, 0.232, 0, 0.246 }, { 2.36, 0.422, 0.476, 0.07 }, { 2.32, 0.401, 0.492, 0.075 }, { 2.39, 0.80, 0.69, 0.1 }, { 2.13, 0.306, 0.165, 0.219 } };
-const FormAdapters kAdaptF32[kForms] = { { 2.65, 0.307, 0.066, 0.35 }, { 0 }, { 2.81, 0.491, 0.563, 0.072 }, { 2.78, 0.848, 0.3, 0.05 }, { 2.59, 0.359, 0.153, 0.25 } };
+const FormAdapters kAdaptBf16[kForms] = { { 1.96, 0.232, 0, 0.246 }, { 2.36, 0.422, 0.476, 0.07 }, { 2.32, 0.401, 0.492, 0.075 }, { 2.39, 0.80, 0.69, 0.1 }, { 2.13, 0.306, 0.165, 0.219 }, { 1.96, 0.232, 0, 0.246 } };
+const FormAdapters kAdaptF32[kForms] = { { 2.65, 0.307, 0.066, 0.35 }, { 0 }, { 2.81, 0.491, 0.563, 0.072 }, { 2.78, 0.848, 0.3, 0.05 }, { 2.59, 0.359, 0.153, 0.25 }, { 0 } };
 
 // The same for the bf16 tiles: steps of the loop, or behind it a lane's elements one by one (slots shorter than 16 rows), or slot after slot.
 double tile_adapters_us(const Tile& m, const LinArgs& a, long long tiles, bool crosses)
@@ -67,8 +67,12 @@ template <typename T, int KIND> int pick_form(const LinArgs& a, double* us)
     for (int f = 0; f < kForms; ++f) {
         const Form& m = forms[f];
         if (!m.mi) continue;
-        const double groups = (double)((rows + 16 * m.mi - 1) / (16 * m.mi)) * ((weight_rows + 16 * m.ni - 1) / (16 * m.ni));
-        double t = m.fixed + (pieces + m.nw - 1) / m.nw * m.turn + std::max(0.0, groups / 256 - m.hidden) * (m.group + pieces * m.piece);
+        // the last form takes 8 rows by 8 and twice the pieces a turn.  Up to one workgroup a CU it is what few columns of a long inner axis want (1 x 4608 x 1152 7.5 -> 5.8 us,
+        // 1 x 9216 x 1152 12.7 -> 8.6, 8 x 4608 x 1152 9.0 -> 7.3), behind it every other is ahead (1 x 4608 x 2304 7.7, this one 10.8)
+        const int split = f == kForms - 1 ? 2 : 1, mr = 16 / split * m.mi, nr = 16 / split * m.ni, at_once = m.nw * split;
+        const double groups = (double)((rows + mr - 1) / mr) * ((weight_rows + nr - 1) / nr);
+        if (split > 1 && (KIND == LIN_GLU || groups > 256)) continue;
+        double t = m.fixed + (pieces + at_once - 1) / at_once * m.turn + std::max(0.0, groups / 256 - m.hidden) * (m.group + pieces * m.piece);
         if (KIND == LIN_ADAPT && a.adapters) {
             const FormAdapters& p = (sizeof(T) == 2 ? kAdaptBf16 : kAdaptF32)[f];
             const double eights = (a.rank + 7) / 8 * (sizeof(T) == 2 && !a.b_vec ? 1.7 : 1.0);
@@ -399,7 +403,7 @@ template <int KIND> drf_status launch_bf16(LinArgs a, hipStream_t st)
     }
     double form_us;
     const int form = pick_form<bf16_t, KIND>(a, &form_us), forced = g_forced_tile - kTiles;
-    if (forced >= 0 && forced < kForms) return launch_linear_direct<bf16_t, KIND>(forced, a, st);
+    if (forced >= 0 && forced < (KIND == LIN_GLU ? kForms - 1 : kForms)) return launch_linear_direct<bf16_t, KIND>(forced, a, st);
     if (g_forced_tile < 0 && form_us < best_us) return launch_linear_direct<bf16_t, KIND>(form, a, st);
     const Tile& m = kLinTiles[best];
     const int by_slot = a.slots * ((a.tokens + m.bm - 1) / m.bm), crossing = (a.slots * a.tokens + m.bm - 1) / m.bm;

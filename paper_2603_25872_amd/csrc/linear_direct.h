@@ -57,17 +57,18 @@ __device__ inline u32x4 row_piece(u32x4 v, int k, int n, float)
 
 struct Nothing { __device__ void operator()() const {} };
 
-// acc += w x^T over a wave's share of the inner axis: turns of 128 bytes, wave, wave + NW, .., U of them on the way.  beside(): other loads, behind the first of these.
-template <typename T, int MI, int NI, int NW, int U, typename F = Nothing>
-__device__ __forceinline__ void direct_product(f32x4 (&acc)[NI][MI], const T* const (&x)[MI], const T* const (&w)[NI], int K, int wave, int quarter, F beside = F{})
+// acc += w x^T over a wave's share of the inner axis: turns of SP times 128 bytes, wave, wave + NW, .., U of them on the way; a lane's is `part` of its turn's.
+// beside(): other loads, behind the first of these.
+template <typename T, int MI, int NI, int NW, int U, int SP = 1, typename F = Nothing>
+__device__ __forceinline__ void direct_product(f32x4 (&acc)[NI][MI], const T* const (&x)[MI], const T* const (&w)[NI], int K, int wave, int quarter, int part = 0, F beside = F{})
 {
-    constexpr int E = 16 / sizeof(T), CHUNK = 8 * E, TURN = NW * CHUNK;
+    constexpr int E = 16 / sizeof(T), CHUNK = 8 * E * SP, TURN = NW * CHUNK;
     const int first = wave * CHUNK, turns = first < K ? (K - first + TURN - 1) / TURN : 0;
     u32x4 fx[U][2][MI], fw[U][2][NI];
     auto load = [&](int t, int turn) __attribute__((always_inline)) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            const int k = first + turn * TURN + (4 * h + quarter) * E;
+            const int k = first + turn * TURN + (8 * part + 4 * h + quarter) * E;
 #pragma unroll
             for (int i = 0; i < NI; ++i) fw[t][h][i] = load_near(w[i], k, K);
 #pragma unroll
@@ -78,7 +79,7 @@ __device__ __forceinline__ void direct_product(f32x4 (&acc)[NI][MI], const T* co
         if (first + turn * TURN + CHUNK > K) {
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const int k = first + turn * TURN + (4 * h + quarter) * E;
+                const int k = first + turn * TURN + (8 * part + 4 * h + quarter) * E;
 #pragma unroll
                 for (int i = 0; i < NI; ++i) fw[t][h][i] = row_piece(fw[t][h][i], k, K, T{});
 #pragma unroll
@@ -141,8 +142,10 @@ template <typename T> __device__ inline void add_low(f32x4& v, const LinArgs& a,
     }
 }
 
-// 16 MI rows by 16 NI rows of the weights (LIN_GLU: NI / 2 pairs of gates and values).
-template <typename T, int KIND, int MI, int NI, int NW, int U>
+// LANES MI rows by LANES NI rows of the weights (LIN_GLU: NI / 2 pairs of gates and values), LANES = 16 / SP.  SP > 1: a matrix instruction's sixteen rows are SP parts of the
+// inner axis of LANES rows, of both operands; what counts of its result are the SP blocks on the diagonal, and a result's blocks are added up with the waves'.  So more
+// workgroups share few weight rows.
+template <typename T, int KIND, int MI, int NI, int NW, int U, int SP>
 __global__ void __launch_bounds__(NW * 64) linear_direct_kernel(const LinArgs a)
 {
     static_assert(KIND != LIN_GLU || NI % 2 == 0, "gates and values");
@@ -150,20 +153,22 @@ __global__ void __launch_bounds__(NW * 64) linear_direct_kernel(const LinArgs a)
     __shared__ f32x4 part[NW][MI * NI][64];
     const int lane = threadIdx.x & 63, l16 = lane & 15, quarter = lane >> 4, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const long long id = a.first + blockIdx.x;
-    const int tm = (int)(id / a.tiles_n), tn = (int)(id - (long long)tm * a.tiles_n), row0 = tm * 16 * MI;
-    const int n0 = tn * (KIND == LIN_GLU ? 8 * NI : 16 * NI);
+    constexpr int LANES = 16 / SP;
+    const int lrow = l16 % LANES, half = l16 / LANES;
+    const int tm = (int)(id / a.tiles_n), tn = (int)(id - (long long)tm * a.tiles_n), row0 = tm * LANES * MI;
+    const int n0 = tn * (KIND == LIN_GLU ? LANES / 2 * NI : LANES * NI);
     const T *x[MI], *w[NI];
     int slot[MI], token[MI];
     bool live[MI];
 #pragma unroll
     for (int j = 0; j < MI; ++j) {
-        live[j] = locate_row(a, 0, row0 + 16 * j + l16, slot[j], token[j]);
-        if (row0 + 16 * j + l16 >= a.slot_rows) slot[j] = token[j] = 0;        // (any row that is there: not stored)
+        live[j] = locate_row(a, 0, row0 + LANES * j + lrow, slot[j], token[j]);
+        if (row0 + LANES * j + lrow >= a.slot_rows) slot[j] = token[j] = 0;        // (any row that is there: not stored)
         x[j] = (const T*)a.x.data + slot[j] * a.x.slot_stride + token[j] * a.x.token_stride;
     }
 #pragma unroll
     for (int i = 0; i < NI; ++i) {
-        int n = KIND == LIN_GLU ? n0 + i / 2 * 16 + l16 : n0 + 16 * i + l16;
+        int n = KIND == LIN_GLU ? n0 + i / 2 * LANES + lrow : n0 + LANES * i + lrow;
         n = n < a.N ? n : a.N - 1;
         w[i] = (const T*)a.w + ((size_t)n + (KIND == LIN_GLU && i % 2 ? a.N : 0)) * a.K;
     }
@@ -176,9 +181,9 @@ __global__ void __launch_bounds__(NW * 64) linear_direct_kernel(const LinArgs a)
     // (feed-forward of 1 x 1152 x 4608: 17.2 -> 16.3 us; an adapter's operands asked for there as well took 64 x 1152 x 6912 of rank 16 from 16.4 to 17.0 us).
     constexpr int OUT = KIND == LIN_GLU ? NI / 2 : NI;
     static_assert(OUT * MI <= NW, "a result a wave");
-    const int i = wave / MI, j = wave - i * MI, n = n0 + 16 * i + 4 * quarter, row = row0 + 16 * j + l16;
+    const int i = wave / MI, j = wave - i * MI, n = n0 + LANES * i + 4 * quarter, row = row0 + LANES * j + l16;
     float bias[KIND == LIN_GLU ? 2 : 1][4] = {};
-    direct_product<T, MI, NI, NW, U>(acc, x, w, a.K, wave, quarter, [&]() __attribute__((always_inline)) {
+    direct_product<T, MI, NI, NW, U, SP>(acc, x, w, a.K, wave, quarter, half, [&]() __attribute__((always_inline)) {
         if (!a.bias || wave >= OUT * MI) return;
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
@@ -193,11 +198,11 @@ __global__ void __launch_bounds__(NW * 64) linear_direct_kernel(const LinArgs a)
         for (int j = 0; j < MI; ++j) part[wave][i * MI + j][lane] = acc[i][j];
     __syncthreads();
     int sl, tk;
-    if (wave < OUT * MI && locate_row(a, 0, row, sl, tk) && n < a.N) {
+    if (wave < OUT * MI && (SP == 1 || (l16 < LANES && 4 * quarter < LANES)) && locate_row(a, 0, row, sl, tk) && n < a.N) {
         auto total = [&](int piece) {
             f32x4 v = part[0][piece * MI + j][lane];
 #pragma unroll
-            for (int u = 1; u < NW; ++u) v += part[u][piece * MI + j][lane];
+            for (int u = 1; u < NW * SP; ++u) v += part[u / SP][piece * MI + j][lane + u % SP * (LANES / 4 * 16 + LANES)];
             return v;
         };
         f32x4 v = total(KIND == LIN_GLU ? 2 * i : i), u = v;
@@ -219,15 +224,15 @@ __global__ void __launch_bounds__(NW * 64) linear_direct_kernel(const LinArgs a)
     }
 }
 
-template <typename T, int KIND, int MI, int NI, int NW, int U> drf_status launch_direct_shape(LinArgs a, hipStream_t st)
+template <typename T, int KIND, int MI, int NI, int NW, int U, int SP = 1> drf_status launch_direct_shape(LinArgs a, hipStream_t st)
 {
     a.slot_rows = a.slots * a.tokens;
-    const int columns = KIND == LIN_GLU ? 8 * NI : 16 * NI;
+    constexpr int rows = 16 / SP * MI, columns = 16 / SP * NI / (KIND == LIN_GLU ? 2 : 1);
     a.tiles_n = (a.N + columns - 1) / columns;
-    a.tiles = (long long)((a.slot_rows + 16 * MI - 1) / (16 * MI)) * a.tiles_n;
+    a.tiles = (long long)((a.slot_rows + rows - 1) / rows) * a.tiles_n;
     const long long most = 1 << 21;                                 // (a launch holds fewer than 2^32 threads)
     for (a.first = 0; a.first < a.tiles; a.first += most) {
-        hipLaunchKernelGGL((linear_direct_kernel<T, KIND, MI, NI, NW, U>), dim3((unsigned)std::min(most, a.tiles - a.first)), dim3(NW * 64), 0, st, a);
+        hipLaunchKernelGGL((linear_direct_kernel<T, KIND, MI, NI, NW, U, SP>), dim3((unsigned)std::min(most, a.tiles - a.first)), dim3(NW * 64), 0, st, a);
         DRF_HIP(hipGetLastError());
     }
     return DRF_OK;

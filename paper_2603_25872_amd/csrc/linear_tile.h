@@ -277,7 +277,10 @@ template <typename T, int KIND> drf_status launch_linear_direct(int form, const 
         DRF_FAIL(DRF_EINVAL, "no such form");
     case 2: return launch_direct_shape<T, KIND, 2, 2, 8, 3>(a, st);
     case 3: return launch_direct_shape<T, KIND, 4, 2, 8, 2>(a, st);
-    default: return launch_direct_shape<T, KIND, 1, 2, 8, 4>(a, st);
+    case 4: return launch_direct_shape<T, KIND, 1, 2, 8, 4>(a, st);
+    default:
+        if constexpr (sizeof(T) == 2 && KIND != LIN_GLU) return launch_direct_shape<T, KIND, 1, 1, 16, 2, 2>(a, st);
+        DRF_FAIL(DRF_EINVAL, "no such form");
     }
 }
 

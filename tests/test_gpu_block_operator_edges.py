@@ -39,7 +39,7 @@ def test_offsets_past_32_bits(torch, drf, forced, dtype, S, N, ss, ts):  # noqa:
     _, w, a, b, which, bias, scales = adapter_case(torch, rng, S, N, 136, 136, 40, 3, dtype)
     block, low = ffn(f64(x), f64(w_in), f64(w_out), f64(b_in), f64(b_out), "silu", dtype), adapted(f64(x), f64(w), f64(a), f64(b), which, f64(bias), f64(scales), dtype)
     wide, out = far(torch, x.shape, (ss, ts), x.dtype).copy_(x), far(torch, x.shape, (ss, ts), x.dtype)
-    for tile in (-1, 0, 1, 2, 3, 5, 6, 7, 9, 10, 13):
+    for tile in (-1, 0, 1, 2, 3, 5, 6, 7, 9, 10, 13, 14):
         forced(tile)
         out.fill_(7.0)
         check(drf.gated_ffn(wide, w_in, w_out, b_in, b_out, out=out), block[0], dtype, block[1])
@@ -53,7 +53,7 @@ def test_offsets_past_32_bits(torch, drf, forced, dtype, S, N, ss, ts):  # noqa:
     check(got[1], h, dtype, eh)
 
 
-@pytest.mark.parametrize("dtype,tiles,S,D,F", [("bf16", (4, 5, 8, 10, 12), 65540, 8, 8), ("f32", (9, 13), 131080, 4, 1)])
+@pytest.mark.parametrize("dtype,tiles,S,D,F", [("bf16", (4, 5, 8, 10, 12, 13), 65540, 8, 8), ("f32", (8, 14), 131080, 4, 1)])
 def test_more_tiles_than_one_launch_takes(torch, drf, forced, dtype, tiles, S, D, F):  # noqa: F811
     """One slot's rows for all slots: all results are the first slot's."""
     rng = np.random.default_rng(S)

@@ -599,7 +599,7 @@ TILED = [(1, 300, 72, 80, 72), (3, 70, 64, 136, 264), (2, 260, 136, 24, 130), (5
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("tile", range(14))
+@pytest.mark.parametrize("tile", range(15))
 @pytest.mark.parametrize("S,N,D,F,O", TILED)
 def test_gated_ffn_on_every_tile(torch, drf, forced, dtype, tile, S, N, D, F, O):
     """Tiles that rows, columns and the inner axis end inside of; slots that end inside of a tile, lengths that leave tiles empty; weights in the last step's idle columns."""
@@ -621,7 +621,7 @@ def test_gated_ffn_on_every_tile(torch, drf, forced, dtype, tile, S, N, D, F, O)
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("tile", range(14))
+@pytest.mark.parametrize("tile", range(15))
 @pytest.mark.parametrize("R", [1, 8, 16, 24, 32, 40, 64, 72, 128, 136])
 @pytest.mark.parametrize("S,N,D,_,O", TILED)
 def test_linear_adapters_on_every_tile(torch, drf, forced, dtype, tile, R, S, N, D, _, O):
