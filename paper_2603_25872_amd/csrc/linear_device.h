@@ -278,7 +278,7 @@ __device__ __forceinline__ void store_wave_tile(const f32x4 (&acc)[NI][MI], cons
 
 }  // namespace
 
-// The tiles of linear_tile.h, and the forms for few rows of linear_direct.h (16, 32 and 64 of them a workgroup), by KIND (one file each).
+// The tiles of linear_tile.h, and the forms for few rows of linear_direct.h (8 to 64 of them a workgroup), by KIND (one file each).
 template <int KIND> drf_status launch_linear_tile(int tile, const LinArgs& a, hipStream_t st);
 template <typename T, int KIND> drf_status launch_linear_direct(int form, const LinArgs& a, hipStream_t st);
 
