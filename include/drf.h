@@ -467,7 +467,8 @@ typedef struct { void* data; int64_t slot_stride, token_stride; } drf_rows;
  *   gate, shift, scale   fp32, rows of a slot (token_stride 0) or of every token; data NULL: 1, 0 and 0
  *   x, out          of type stream; y, h of type branch (DRF_BF16 with a DRF_BF16 stream)
  *   out NULL: z is not stored.  h NULL: no h.  y NULL: z = x_scale x, and out has to be NULL; after, gate and y_scale are not looked at.
- * h is formed from z as it is before its rounding to the stream's type.  Norms add their squares in fp32: values up to 1e18.  Rows behind a slot's
+ * h is formed from z as it is before its rounding to the stream's type.  Norms take rows of any finite values, also where their squares or the sum of them are beyond
+ * fp32, as far as fp32 holds the sum of a row's values (DRF_QK_LAYER); eps 0: a row of zeros, or for DRF_QK_LAYER of one value, has none.  Rows behind a slot's
  * length (lens, DEVICE int32 [slots] or NULL) are neither read nor written.  out may be x itself and h y itself (address and strides), otherwise
  * no output overlaps another tensor.  1 <= width <= 16384.
  */

@@ -15,7 +15,10 @@ namespace {
 
 constexpr int kMaxWidth = 16384;
 
-struct RowNormArgs { int norm; float eps; const float *gain, *bias; };
+// A row's squares and their sum are taken in fp32 as they are where that holds them: the sum is finite, and either above kFewSquares (what its smallest terms lose to
+// underflow, 16384 of 2^-126 at most, is 2^-29 of it) or of no account beside an eps of kMuchEps or more.  Other rows have a power of two taken out of them first.
+constexpr float kFewSquares = 1e-25f, kMuchEps = 1e-30f;
+struct RowNormArgs { int norm; float eps; double eps_given; const float *gain, *bias; };
 struct ResidualArgs {
     drf_rows x, y, out, h, gate, shift, scale;
     int rows, tokens, width;
@@ -44,6 +47,13 @@ __device__ inline float wave_total(float v)
     return __builtin_bit_cast(float, (int)s[0]) + __builtin_bit_cast(float, (int)s[1]);
 }
 
+__device__ inline float wave_most(float v)
+{
+#pragma unroll
+    for (int o = 32; o; o >>= 1) v = fmaxf(v, __shfl_xor(v, o));
+    return v;
+}
+
 // E columns of a row at any address that is a multiple of an element: the memory system takes 16 bytes at once from there too.
 template <typename T, int E> struct Piece { typedef T type __attribute__((ext_vector_type(E), aligned(sizeof(T)))); };
 template <typename T> struct Piece<T, 1> { typedef T type __attribute__((ext_vector_type(1))); };
@@ -68,7 +78,7 @@ __global__ void __launch_bounds__(512) residual_norm_kernel(const ResidualArgs a
 {
     constexpr bool GROUP = FORM == ROW_GROUP, STAGED = FORM == ROW_STAGED;
     constexpr int KINDS = BIAS ? 4 : 3, ROW = NV * 64 * E;
-    __shared__ float part[GROUP ? 4 : 1][8];
+    __shared__ float part[GROUP ? 8 : 1][8];
     __shared__ __attribute__((aligned(32))) float table[STAGED ? KINDS * ROW : 1];
     const int waves = blockDim.x >> 6, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int li = GROUP ? threadIdx.x : threadIdx.x & 63, lanes = GROUP ? blockDim.x : 64;
@@ -102,21 +112,8 @@ __global__ void __launch_bounds__(512) residual_norm_kernel(const ResidualArgs a
         skip[v] = left >= E ? 0 : left > 0 ? E - left : E;
         col[v] = left >= E ? c : a.width - E;
     }
-    auto norm = [&](float (&r)[NV][E], int kind, float eps, int first) {
-        if (kind == DRF_QK_NONE) return;
+    auto squares = [&](const float (&r)[NV][E]) {
         float s = 0.f;
-        if (kind == DRF_QK_LAYER) {
-#pragma unroll
-            for (int v = 0; v < NV; ++v)
-#pragma unroll
-                for (int j = 0; j < E; ++j) s += j >= skip[v] ? r[v][j] : 0.f;
-            const float mean = total(s, first) * a.inv_width;
-            s = 0.f;
-#pragma unroll
-            for (int v = 0; v < NV; ++v)
-#pragma unroll
-                for (int j = 0; j < E; ++j) r[v][j] -= mean;
-        }
 #pragma unroll
         for (int v = 0; v < NV; ++v)
 #pragma unroll
@@ -124,7 +121,48 @@ __global__ void __launch_bounds__(512) residual_norm_kernel(const ResidualArgs a
                 const float t = j >= skip[v] ? r[v][j] : 0.f;
                 s = fmaf(t, t, s);
             }
-        const float inv = 1.f / sqrtf(fmaf(total(s, first + 1), a.inv_width, eps));
+        return s;
+    };
+    auto norm = [&](float (&r)[NV][E], const RowNormArgs& n, int first) {
+        if (n.norm == DRF_QK_NONE) return;
+        if (n.norm == DRF_QK_LAYER) {
+            float s = 0.f;
+#pragma unroll
+            for (int v = 0; v < NV; ++v)
+#pragma unroll
+                for (int j = 0; j < E; ++j) s += j >= skip[v] ? r[v][j] : 0.f;
+            const float mean = total(s, first) * a.inv_width;
+#pragma unroll
+            for (int v = 0; v < NV; ++v)
+#pragma unroll
+                for (int j = 0; j < E; ++j) r[v][j] -= mean;
+        }
+        float s = total(squares(r), first + 1), eps = n.eps;
+        if (__builtin_expect(!(s < INFINITY) || (s < kFewSquares && eps < kMuchEps), 0)) {     // (the same for all lanes of the row)
+            float most = 0.f;
+#pragma unroll
+            for (int v = 0; v < NV; ++v)
+#pragma unroll
+                for (int j = 0; j < E; ++j) most = fmaxf(most, j >= skip[v] ? fabsf(r[v][j]) : 0.f);
+            most = wave_most(most);
+            if constexpr (GROUP) {
+                if ((threadIdx.x & 63) == 0) part[first + 2][wave] = most;
+                __syncthreads();
+                for (int w = 0; w < waves; ++w) most = fmaxf(most, part[first + 2][w]);
+            }
+            if (most < INFINITY) {                  // (a row with an infinity: no number there, zeros beside it)
+                // x / sqrt(mean x^2 + eps) with x = 2^e t, |t| < 4: t / sqrt(mean t^2 + eps 2^-2e).  The lowest e that any fp32 row needs keeps an eps below kMuchEps finite
+                const int e = most > 0.f ? max(-110, min(126, ilogbf(most))) : -110;
+                const float f = ldexpf(1.f, -e);
+#pragma unroll
+                for (int v = 0; v < NV; ++v)
+#pragma unroll
+                    for (int j = 0; j < E; ++j) r[v][j] *= f;
+                s = total(squares(r), first + 3);
+                eps = n.eps_given > 0.0 ? fmaxf((float)ldexp(n.eps_given, -2 * e), 1.17549435e-38f) : 0.f;
+            }
+        }
+        const float inv = 1.f / sqrtf(fmaf(s, a.inv_width, eps));
 #pragma unroll
         for (int v = 0; v < NV; ++v)
 #pragma unroll
@@ -214,7 +252,7 @@ __global__ void __launch_bounds__(512) residual_norm_kernel(const ResidualArgs a
         }
     if constexpr (GROUP) __syncthreads();           // (a row in its own place: all of it is read before any of it is written)
     if (has_y) {
-        norm(y, a.after.norm, a.after.eps, 0);
+        norm(y, a.after, 0);
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
             float g[E], gb[E];
@@ -236,7 +274,7 @@ __global__ void __launch_bounds__(512) residual_norm_kernel(const ResidualArgs a
         }
     }
     if (!has_h) return;
-    norm(z, a.before.norm, a.before.eps, 2);
+    norm(z, a.before, 4);
     TB* o = (TB*)a.h.data + slot * a.h.slot_stride + token * a.h.token_stride;
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
@@ -294,7 +332,7 @@ drf_status fill_norm(const char* what, const drf_row_norm& n, RowNormArgs* out)
     if (n.norm == DRF_QK_NONE && n.gain) DRF_FAIL(DRF_EINVAL, "%s: a gain without a norm", what);
     if (n.norm != DRF_QK_LAYER && n.bias) DRF_FAIL(DRF_EINVAL, "%s: a bias belongs to DRF_QK_LAYER", what);
     // (an eps that fp32 does not hold is still no zero: a row of zeros stays one)
-    *out = { (int)n.norm, n.eps > 0.0 ? std::max((float)n.eps, 1.17549435e-38f) : 0.f, n.gain, n.bias };
+    *out = { (int)n.norm, n.eps > 0.0 ? std::max((float)n.eps, 1.17549435e-38f) : 0.f, n.eps, n.gain, n.bias };
     return DRF_OK;
 }
 

@@ -1,0 +1,23 @@
+"""What the tests of the operators around a block's Linears compare with, by itself: a wrong result is refused whatever it is."""
+import numpy as np
+import pytest
+
+from test_gpu_block_operator_values import close
+
+
+def test_results_that_are_no_numbers_are_refused():
+    want = np.array([[1.0, -2.0], [np.inf, np.nan]])
+    close(want.copy(), want, "f32", 0.0)
+    for bad in (np.nan, np.inf, -np.inf, 1.0 + 2.0 ** -20, -1.0):
+        got = want.copy()
+        got[0, 0] = bad
+        for slack in (0.0, np.zeros((2, 2)), 2.0 ** -21):
+            with pytest.raises(AssertionError):
+                close(got, want, "f32", slack)
+    for at, bad in (((1, 0), 3.0), ((1, 0), -np.inf), ((1, 0), np.nan), ((1, 1), 0.0), ((1, 1), np.inf)):
+        got = want.copy()
+        got[at] = bad
+        with pytest.raises(AssertionError):
+            close(got, want, "f32", 1.0)
+    with pytest.raises(AssertionError):
+        close(want[:1], want, "f32", 0.0)
