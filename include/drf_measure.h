@@ -105,6 +105,12 @@ drf_status drf_graph_stats(drf_denoiser* den, int* captured, int* failed, long l
  * the forms for few rows, 14 the tile of fp32; -1: by choice.  Returns the number of them.  Host only.
  */
 int drf_probe_linear_tile(int tile);
+/*
+ * The tile or form that this thread's last product of a kind went to: 0 the second of drf_gated_ffn, 1 its first (gate and value), 2 drf_linear_adapters'; -1: there was none.
+ * Another than the one asked for: the product cannot run there (1: not on 7 and 13; 2 with rows of B that are no 16-byte pieces: not on 0, 1, 6 and 7; DRF_F32: 8, 10, 11,
+ * 12 and 14 only).  Host only.
+ */
+int drf_probe_linear_route(int product);
 
 /*
  * Measurement hook: ONE launch of the fused update kernel in the shape drf_sample gives it after a

@@ -83,6 +83,7 @@ template <typename T, int KIND> int pick_form(const LinArgs& a, double* us)
     return best;
 }
 thread_local int g_forced_tile = -1;                    // see drf_probe_linear_tile
+thread_local int g_route[3] = { -1, -1, -1 };           // see drf_probe_linear_route
 
 // ---- x A^T ------------------------------------------------------------------------------------------------
 // 16 MI rows of one slot by 32 of the rank's columns a workgroup, operands straight to registers, the inner axis dealt over NW waves, 128 bytes of it at a
@@ -350,14 +351,16 @@ template <int KIND> drf_status launch_f32(const LinArgs& a, hipStream_t st)
 {
     double us;
     const int form = pick_form<float, KIND>(a, &us), forced = g_forced_tile - kTiles;
-    if (forced >= 0 && forced < kForms && kFormsF32[forced].mi && a.K >= 4) return launch_linear_direct<float, KIND>(forced, a, st);     // (rows of at least 16 bytes)
+    auto direct = [&](int f) { g_route[KIND] = kTiles + f; return launch_linear_direct<float, KIND>(f, a, st); };
+    if (forced >= 0 && forced < kForms && kFormsF32[forced].mi && a.K >= 4) return direct(forced);     // (rows of at least 16 bytes)
     const long long tiles = ((long long)a.slots * a.tokens + 63) / 64 * (((KIND == LIN_GLU ? 2LL * a.N : a.N) + 63) / 64);
     double tile = tile_us(kTileF32, tiles, (a.K + 31) / 32);
     if (KIND == LIN_ADAPT && a.adapters) {                          // slot after slot of a wave's 32 rows
         const int reach = std::min(std::min(a.slots, 32), 31 / a.tokens + 1 + (a.tokens > 1));
         tile += 1.1 + 1.1 * std::max(1.0, tiles / 256.0) + reach * (0.42 + 0.64 * ((a.rank + 15) / 16)) * (double)((tiles + 1023) / 1024);
     }
-    if (forced != kForms && a.K >= 4 && us < tile) return launch_linear_direct<float, KIND>(form, a, st);
+    if (forced != kForms && a.K >= 4 && us < tile) return direct(form);
+    g_route[KIND] = kTiles + kForms;
     return launch_f32_tiles<KIND>(a, st);
 }
 
@@ -403,8 +406,10 @@ template <int KIND> drf_status launch_bf16(LinArgs a, hipStream_t st)
     }
     double form_us;
     const int form = pick_form<bf16_t, KIND>(a, &form_us), forced = g_forced_tile - kTiles;
-    if (forced >= 0 && forced < (KIND == LIN_GLU ? kForms - 1 : kForms)) return launch_linear_direct<bf16_t, KIND>(forced, a, st);
-    if (g_forced_tile < 0 && form_us < best_us) return launch_linear_direct<bf16_t, KIND>(form, a, st);
+    auto direct = [&](int f) { g_route[KIND] = kTiles + f; return launch_linear_direct<bf16_t, KIND>(f, a, st); };
+    if (forced >= 0 && forced < (KIND == LIN_GLU ? kForms - 1 : kForms)) return direct(forced);
+    if (g_forced_tile < 0 && form_us < best_us) return direct(form);
+    g_route[KIND] = best;
     const Tile& m = kLinTiles[best];
     const int by_slot = a.slots * ((a.tokens + m.bm - 1) / m.bm), crossing = (a.slots * a.tokens + m.bm - 1) / m.bm;
     const bool crosses = cross && crossing < by_slot && !(KIND == LIN_ADAPT && m.bm * m.bn >= 256 * 128 && a.adapters);
@@ -559,3 +564,5 @@ extern "C" int drf_probe_linear_tile(int tile)
     g_forced_tile = tile;
     return kTiles + kForms + 1;
 }
+
+extern "C" int drf_probe_linear_route(int product) { return product >= 0 && product < 3 ? g_route[product] : -1; }

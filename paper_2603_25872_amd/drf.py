@@ -36,7 +36,7 @@ SYMBOLS = ["drf_denoiser_weight_count", "drf_denoiser_create", "drf_denoiser_des
            "drf_residual_norm", "drf_gated_ffn_scratch_bytes", "drf_gated_ffn", "drf_linear_adapters_scratch_bytes", "drf_linear_adapters"]
 # include/drf_measure.h: test and measurement hooks
 MEASURE_SYMBOLS = ["drf_eps_trace", "drf_profile_enable", "drf_profile_read", "drf_probe_gemm_bf16",
-                   "drf_probe_attn_bf16", "drf_probe_cross_attn_bf16", "drf_probe_attn_route", "drf_probe_gemm_route", "drf_probe_block_route", "drf_probe_linear_tile", "drf_probe_update_fused", "drf_graph_stats", "drf_calibrate_mfma_bf16", "drf_calibrate_copy"]
+                   "drf_probe_attn_bf16", "drf_probe_cross_attn_bf16", "drf_probe_attn_route", "drf_probe_gemm_route", "drf_probe_block_route", "drf_probe_linear_tile", "drf_probe_linear_route", "drf_probe_update_fused", "drf_graph_stats", "drf_calibrate_mfma_bf16", "drf_calibrate_copy"]
 STATIC_SCRATCH_BYTES = 48 << 20
 
 
@@ -154,7 +154,7 @@ def lib():
         L.drf_probe_cross_attn_bf16.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p] + [C.c_int] * 7 + [C.c_void_p]
         L.drf_probe_attn_route.argtypes = [C.c_int] * 6
         L.drf_probe_block_route.argtypes = [C.c_int] * 5
-        L.drf_probe_linear_tile.argtypes = [C.c_int]
+        L.drf_probe_linear_tile.argtypes = L.drf_probe_linear_route.argtypes = [C.c_int]
         L.drf_probe_gemm_route.argtypes = [C.c_int] * 5 + [C.c_void_p]
         L.drf_last_error.restype = C.c_char_p
         L.drf_denoiser_weight_count_attn.restype = C.c_size_t
@@ -689,6 +689,11 @@ def probe_gemm_route(M, N, K, kind=0, rows_per_slot=256):
 def probe_linear_tile(tile):
     """Products of gated_ffn() and linear_adapters() on this thread run on tile or form `tile` where it can take them, -1: by choice; the number of them."""
     return lib().drf_probe_linear_tile(int(tile))
+
+
+def probe_linear_route(product):
+    """The tile or form that this thread's last product went to: 0 the second of gated_ffn(), 1 its first, 2 linear_adapters(); -1: there was none."""
+    return lib().drf_probe_linear_route(int(product))
 
 
 def probe_attn_bf16(qkv, slots, tokens, heads, head_dim, out=None):

@@ -1,10 +1,12 @@
-"""The operators around a block's Linears at the ends of their values: rows of any magnitude through the norms.  References are those of test_gpu_block_operators.py, and so
-are the tolerances; a result that is no number is refused wherever the reference has one."""
+"""The operators around a block's Linears at the ends of their values and on every kernel by name: rows of any magnitude through the norms, and each
+tile and form of the products, which the probe names, beside rows and scratch that are no numbers.  References are those of test_gpu_block_operators.py, and so are the
+tolerances; a result that is no number is refused wherever the reference has one."""
 import numpy as np
 import pytest
 
-from test_gpu_block_operators import HALF, f64, normed, rand
-from test_gpu_block_operators import drf, torch  # noqa: F401
+from test_gpu_block_operator_edges import FAR, far
+from test_gpu_block_operators import HALF, adapted, adapter_case, f64, ffn, ffn_case, normed, rand, run_adapters
+from test_gpu_block_operators import drf, forced, torch  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -60,3 +62,115 @@ def test_rows_without_a_norm_of_their_own(torch, drf):  # noqa: F811
             keep = torch.tensor([i not in (1, 4, 9) for i in range(13)], device="cuda")
             assert torch.equal(got[0, keep], want[0, keep])
             assert (got[0, 1] == 0).all() and torch.isnan(got[0, 9]).all() and torch.isnan(got[0, 4, 3]) and (got[0, 4, :3] == 0).all() and (got[0, 4, 4:] == 0).all()
+
+
+# ---- every tile and form, by name -------------------------------------------------------------------------------
+
+# tiles of bf16, forms for few rows (8 to 13), the tile of fp32 (14): those that a product can take.  Gate and value need pairs of pieces in a wave (not 7, 13); ranks of B whose
+# rows are no 16-byte pieces leave the largest tiles out; fp32 has four forms
+STORE = {"bf16": list(range(14)), "f32": [8, 10, 11, 12, 14]}
+GLU = {"bf16": [t for t in range(14) if t not in (7, 13)], "f32": STORE["f32"]}
+ADAPT = {"bf16": STORE["bf16"], "f32": STORE["f32"]}
+ADAPT_ODD = {"bf16": [t for t in range(14) if t not in (0, 1, 6, 7)], "f32": STORE["f32"]}
+each = lambda kinds: [(d, t) for d in ("bf16", "f32") for t in kinds[d]]  # noqa: E731
+
+
+def on(drf, forced, tile, kind, call):  # noqa: F811
+    """The call's result, with its product of that kind held to the tile, on which it ran."""
+    forced(tile)
+    out = call()
+    assert drf.probe_linear_route(kind) == tile
+    return out
+
+
+SHAPES = [(3, 70, 64, 136, 264), (5, 130, 200, 272, 300), (40, 9, 448, 152, 65), (1, 300, 72, 80, 72)]
+LENS = lambda S, N: [(N, 0, 1, N // 2, N - 1)[j % 5] for j in range(S)]  # noqa: E731
+
+
+def native(torch, drf, name, args, out):  # noqa: F811
+    """The call with scratch that holds no number."""
+    ops = drf._block_operators()
+    call = getattr(ops, name)
+    n = call(*args, None, None)
+    scratch = torch.full((n // 2,), float("nan"), dtype=torch.bfloat16, device="cuda")
+    drf._check(call(*args, out, scratch))
+    return out
+
+
+def poisoned(x, lens):
+    y = x.clone()
+    for j, n in enumerate(lens):
+        y[j, n:] = float("nan")
+    return y
+
+
+def inside(got, want, slack, lens, dtype):
+    for j, n in enumerate(lens):
+        assert (got[j, n:] == 7).all()
+        close(f64(got[j, :n]), want[j, :n], dtype, slack[j, :n])
+
+
+@pytest.mark.parametrize("dtype,tile", each(STORE))
+@pytest.mark.parametrize("S,N,D,F,O", SHAPES)
+def test_gated_ffn_by_name(torch, drf, forced, dtype, tile, S, N, D, F, O):  # noqa: F811
+    """Both products on the tile (or the first by choice, where it takes no gate and value), rows behind lengths and scratch are NaN: live rows are what they were."""
+    rng = np.random.default_rng(N + D)
+    x, w_in, w_out, b_in, b_out = ffn_case(torch, rng, S, N, D, F, O, dtype)
+    want, slack = ffn(f64(x), f64(w_in), f64(w_out), f64(b_in), f64(b_out), "silu", dtype)
+    lens = LENS(S, N)
+    for n in (None, lens):
+        t = None if n is None else torch.tensor(n, dtype=torch.int32, device="cuda")
+        out = torch.full((S, N, O), 7.0, dtype=x.dtype, device="cuda")
+        args = (x if n is None else poisoned(x, n), w_in, w_out, b_in, b_out, drf.GLU_SILU, t)
+        got = on(drf, forced, tile, 0, lambda: native(torch, drf, "gated_ffn", args, out))
+        assert tile not in GLU[dtype] or drf.probe_linear_route(1) == tile
+        inside(got, want, slack, [N] * S if n is None else n, dtype)
+
+
+@pytest.mark.parametrize("R,dtype,tile", [(R, *k) for R in (8, 40, 5) for k in each(ADAPT_ODD if R % 8 else ADAPT)])
+@pytest.mark.parametrize("S,N,D,_,O", SHAPES)
+def test_linear_adapters_by_name(torch, drf, forced, dtype, tile, R, S, N, D, _, O):  # noqa: F811
+    rng = np.random.default_rng(N + D + R)
+    x, w, a, b, _, bias, scales = adapter_case(torch, rng, S, N, D, O, R, 3, dtype)
+    which = [(1, -1, 0, 2, 2)[j % 5] for j in range(S)]
+    want, slack = adapted(f64(x), f64(w), f64(a), f64(b), which, f64(bias), f64(scales), dtype)
+    i = torch.tensor(which, dtype=torch.int32, device="cuda")
+    for n in (None, LENS(S, N)):
+        t = None if n is None else torch.tensor(n, dtype=torch.int32, device="cuda")
+        out = torch.full((S, N, O), 7.0, dtype=x.dtype, device="cuda")
+        args = (x if n is None else poisoned(x, n), w, a, b, i, bias, scales, t)
+        got = on(drf, forced, tile, 2, lambda: native(torch, drf, "linear_adapters", args, out))
+        inside(got, want, slack, [N] * S if n is None else n, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("S,N,ss,ts", FAR)
+def test_offsets_past_32_bits_by_name(torch, drf, forced, dtype, S, N, ss, ts):  # noqa: F811
+    rng = np.random.default_rng(N)
+    x, w_in, w_out, b_in, b_out = ffn_case(torch, rng, S, N, 136, 64, 136, dtype)
+    _, w, a, b, which, bias, scales = adapter_case(torch, rng, S, N, 136, 136, 40, 3, dtype)
+    block, low = ffn(f64(x), f64(w_in), f64(w_out), f64(b_in), f64(b_out), "silu", dtype), adapted(f64(x), f64(w), f64(a), f64(b), which, f64(bias), f64(scales), dtype)
+    wide, out = far(torch, x.shape, (ss, ts), x.dtype).copy_(x), far(torch, x.shape, (ss, ts), x.dtype)
+    for tile in STORE[dtype]:
+        out.fill_(7.0)
+        close(f64(on(drf, forced, tile, 0, lambda: drf.gated_ffn(wide, w_in, w_out, b_in, b_out, out=out))), block[0], dtype, block[1])
+        out.fill_(7.0)
+        close(f64(on(drf, forced, tile, 2, lambda: run_adapters(torch, drf, wide, w, a, b, which, bias, scales, out=out))), low[0], dtype, low[1])
+    del wide, out
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()
+
+
+def test_the_probe_names_what_ran(torch, drf, forced):  # noqa: F811
+    """A number that a product cannot take leaves the choice to the model, and the probe says so."""
+    rng = np.random.default_rng(1)
+    c = ffn_case(torch, rng, 1, 300, 72, 80, 72, "f32")
+    forced(-1)
+    drf.gated_ffn(*c)
+    chosen = [drf.probe_linear_route(k) for k in (0, 1)]
+    assert all(k in STORE["f32"] for k in chosen)
+    for tile in (0, 7, 9, 13):
+        forced(tile)
+        drf.gated_ffn(*c)
+        assert [drf.probe_linear_route(k) for k in (0, 1)] == chosen
+    assert drf.probe_linear_route(3) == drf.probe_linear_route(-1) == -1
