@@ -517,7 +517,8 @@ drf_status drf_gated_ffn(const drf_gated_ffn_config* cfg, const drf_rows* x, con
  *   a, b    DEVICE [adapters][rank][width] and [adapters][out_width][rank]; scales fp32 [adapters] or NULL: ones
  *   which   DEVICE int32 [slots]; an index below 0 or from `adapters` on: the slot has none
  *   scratch DEVICE, 16-byte aligned, drf_linear_adapters_scratch_bytes() bytes
- * x A^T is kept in fp32, in DRF_BF16 as the sum of two bf16 operands (16 bits of it; an infinite element of b gives its rows NaN).  Types, alignment, strides, lengths and sizes as in drf_gated_ffn;
+ * x A^T is kept in fp32, in DRF_BF16 as the sum of two bf16 operands (16 bits of it; values below 2^-100 may count as zero beside an infinite element of b).  Types, alignment,
+ * strides, lengths and sizes as in drf_gated_ffn;
  * w and a 16-byte aligned and width % 8 == 0 in DRF_BF16, b, rank and out_width any; 1 <= rank <= 256, adapters >= 0 (0: a and b may be NULL).
  */
 typedef struct {

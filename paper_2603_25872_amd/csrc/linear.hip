@@ -89,7 +89,8 @@ thread_local int g_route[3] = { -1, -1, -1 };           // see drf_probe_linear_
 // 16 MI rows of one slot by 32 of the rank's columns a workgroup, operands straight to registers, the inner axis dealt over NW waves, 128 bytes of it at a
 // time with U turns on the way (U = 0: all at once), that add up through LDS.  Reads x once for every 32 columns of the rank; bound by that: 65536 x 1152 47 us, 3.2 TB/s (on two and one
 // pieces of rows a workgroup 51 and 65), 64 rows of as many requests 5.  fp32 sums go out as they are, for bf16
-// as two operands: the upper 8 bits of the fp32 value and the rest rounded to 8 (2^-16 of the value is lost); one that is no number is itself and zero.
+// as two operands: the upper 8 bits of the next fp32 value towards zero, and the rest rounded to 8 (2^-16 of the value is lost).  So neither is zero and both have the
+// value's sign: times an infinite weight they are that infinity.  A zero, an infinity and what is no number are themselves twice.
 template <typename T, int MI, int NW, int U>
 __global__ void __launch_bounds__(NW * 64) adapters_low_kernel(const LinArgs a)
 {
@@ -145,10 +146,10 @@ __global__ void __launch_bounds__(NW * 64) adapters_low_kernel(const LinArgs a)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const float t = r + e < a.rank ? v[e] * scale : 0.f;
-                const float top = __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, t) & 0xffff0000u);
-                const bool fine = fabsf(t) < INFINITY;
+                const float top = __builtin_bit_cast(float, (__builtin_bit_cast(uint32_t, t) - 1u) & 0xffff0000u);
+                const bool fine = fabsf(t) > 0.f && fabsf(t) < INFINITY;
                 hi[e] = (bf16_t)(fine ? top : t);
-                lo[e] = (bf16_t)(fine ? t - top : 0.f);
+                lo[e] = (bf16_t)(fine ? t - top : t);
             }
             bf16_t* o = (bf16_t*)a.low + row * 2 * a.low_cols + r;
             *reinterpret_cast<bf16x4*>(o) = hi;

@@ -1,5 +1,5 @@
-"""The operators around a block's Linears at the ends of their values and on every kernel by name: rows of any magnitude through the norms, and each
-tile and form of the products, which the probe names, beside rows and scratch that are no numbers.  References are those of test_gpu_block_operators.py, and so are the
+"""The operators around a block's Linears at the ends of their values and on every kernel by name: rows of any magnitude through the norms, infinite weights of an adapter, and
+each tile and form of the products, which the probe names, beside rows and scratch that are no numbers.  References are those of test_gpu_block_operators.py, and so are the
 tolerances; a result that is no number is refused wherever the reference has one."""
 import numpy as np
 import pytest
@@ -64,7 +64,7 @@ def test_rows_without_a_norm_of_their_own(torch, drf):  # noqa: F811
             assert (got[0, 1] == 0).all() and torch.isnan(got[0, 9]).all() and torch.isnan(got[0, 4, 3]) and (got[0, 4, :3] == 0).all() and (got[0, 4, 4:] == 0).all()
 
 
-# ---- every tile and form, by name -------------------------------------------------------------------------------
+# ---- infinite weights of an adapter ---------------------------------------------------------------------------
 
 # tiles of bf16, forms for few rows (8 to 13), the tile of fp32 (14): those that a product can take.  Gate and value need pairs of pieces in a wave (not 7, 13); ranks of B whose
 # rows are no 16-byte pieces leave the largest tiles out; fp32 has four forms
@@ -82,6 +82,46 @@ def on(drf, forced, tile, kind, call):  # noqa: F811
     assert drf.probe_linear_route(kind) == tile
     return out
 
+
+@pytest.mark.parametrize("R", [8, 24, 40, 5])
+@pytest.mark.parametrize("S,N", [(2, 70), (6, 3), (1, 300)])
+def test_infinite_weights_of_an_adapter(torch, drf, forced, R, S, N):  # noqa: F811
+    """x A^T of whole numbers (which eight bits hold) and of zeros times an infinite weight: an infinity of its sign, or no number where it is zero."""
+    rng = np.random.default_rng(R)
+    D, O = 64, 72
+    x = torch.from_numpy(rng.integers(-3, 4, (S, N, D)).astype(np.float32))
+    w, a, b = torch.zeros(O, D), torch.zeros(2, R, D), torch.from_numpy(rng.integers(1, 5, (2, O, R)).astype(np.float32))
+    a[:, torch.arange(R), torch.arange(R)] = 1.0                    # (x A^T: the first columns of x)
+    a[1] *= 0.5
+    b[0, 3, 2], b[0, 5, R - 1], b[1, 4, 0] = float("inf"), float("-inf"), float("inf")
+    w[:, D - 1] = 1.0
+    which = [j % 2 for j in range(S)]
+    with np.errstate(invalid="ignore"):
+        t = [x[j, :, :R].double().numpy() * (1.0, 0.5)[which[j]] for j in range(S)]
+        want = np.stack([x[j, :, D - 1:].double().numpy() + sum(t[j][:, r:r + 1] * b[which[j], :, r].double().numpy()[None] for r in range(R)) for j in range(S)])
+    for dtype in ("bf16", "f32"):
+        args = [v.to(torch.bfloat16 if dtype == "bf16" else torch.float32).cuda() for v in (x, w, a, b)]
+        for tile in (ADAPT_ODD if R % 8 else ADAPT)[dtype]:
+            got = f64(on(drf, forced, tile, 2, lambda: run_adapters(torch, drf, *args, which, None, None)))
+            assert np.array_equal(np.isnan(got), np.isnan(want)) and np.array_equal(got[np.isinf(want)], want[np.isinf(want)]), (dtype, tile)
+            fine = np.isfinite(want)
+            close(got[fine], want[fine], dtype, 0.0)
+
+
+def test_infinite_scales(torch, drf):  # noqa: F811
+    """x A^T is infinite, and so is what finite and infinite weights of its sign make of it."""
+    x, w, a = torch.ones(1, 20, 8, device="cuda"), torch.zeros(8, 8, device="cuda"), torch.ones(1, 8, 8, device="cuda")
+    b = torch.full((1, 8, 8), 2.0, device="cuda")
+    b[0, 3, 1] = float("inf")
+    b[0, 5] = -1.0
+    i, s = torch.zeros(1, dtype=torch.int32, device="cuda"), torch.full((1,), float("inf"), device="cuda")
+    want = torch.full((1, 20, 8), float("inf"), device="cuda")
+    want[..., 5] = float("-inf")
+    for t in (torch.float32, torch.bfloat16):
+        assert torch.equal(drf.linear_adapters(x.to(t), w.to(t), a.to(t), b.to(t), i, None, s).float(), want)
+
+
+# ---- every tile and form, by name -------------------------------------------------------------------------------
 
 SHAPES = [(3, 70, 64, 136, 264), (5, 130, 200, 272, 300), (40, 9, 448, 152, 65), (1, 300, 72, 80, 72)]
 LENS = lambda S, N: [(N, 0, 1, N // 2, N - 1)[j % 5] for j in range(S)]  # noqa: E731
