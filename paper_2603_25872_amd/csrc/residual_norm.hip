@@ -353,13 +353,14 @@ extern "C" drf_status drf_residual_norm(const drf_residual_config* cfg, const dr
     if (rc != DRF_OK) return rc;
     if (c.width < 1) DRF_FAIL(DRF_EINVAL, "width must be >= 1");
     if (c.width > kMaxWidth) DRF_FAIL(DRF_ESHAPE, "width must be <= %d (got %d)", kMaxWidth, c.width);
-    if (!std::isfinite(c.x_scale) || !std::isfinite(c.y_scale)) DRF_FAIL(DRF_EINVAL, "x_scale and y_scale must be finite");
+    if (!std::isfinite(c.x_scale) || (y && !std::isfinite(c.y_scale))) DRF_FAIL(DRF_EINVAL, "x_scale and y_scale must be finite");
     ResidualArgs a{};
-    if ((rc = fill_norm("after", c.after, &a.after)) != DRF_OK || (rc = fill_norm("before", c.before, &a.before)) != DRF_OK) return rc;
+    if (y && (rc = fill_norm("after", c.after, &a.after)) != DRF_OK) return rc;
+    if ((rc = fill_norm("before", c.before, &a.before)) != DRF_OK) return rc;
     if (c.slots == 0 || c.tokens == 0) return DRF_OK;
     auto take = [&](const drf_rows* t) { return t ? used_rows(*t, c.slots, c.tokens) : drf_rows{}; };
     a.x = take(x); a.y = take(y); a.out = take(out); a.h = take(h);
-    a.gate = take(&c.gate); a.shift = take(&c.shift); a.scale = take(&c.scale);
+    a.gate = take(y ? &c.gate : nullptr); a.shift = take(&c.shift); a.scale = take(&c.scale);
     if (!a.x.data || (y && !y->data) || (out && !out->data) || (h && !h->data)) DRF_FAIL(DRF_EINVAL, "NULL tensor");
     if (!a.out.data && !a.h.data) DRF_FAIL(DRF_EINVAL, "neither the stream nor its norm is asked for");
     if (!a.y.data && a.out.data) DRF_FAIL(DRF_EINVAL, "a stream is stored where a branch is added to it");

@@ -64,6 +64,13 @@ def test_rows_without_a_norm_of_their_own(torch, drf):  # noqa: F811
             assert (got[0, 1] == 0).all() and torch.isnan(got[0, 9]).all() and torch.isnan(got[0, 4, 3]) and (got[0, 4, :3] == 0).all() and (got[0, 4, 4:] == 0).all()
 
 
+def test_without_a_branch_its_arguments_are_not_looked_at(torch, drf):  # noqa: F811
+    x, g = torch.randn(2, 5, 64, device="cuda"), torch.randn(64, device="cuda")
+    want = drf.residual_norm(x)[1]
+    assert torch.equal(drf.residual_norm(x, after="none", after_gain=g, y_scale=float("nan"), gate=torch.full((2, 64), float("nan"), device="cuda"))[1], want)
+    assert torch.equal(drf.residual_norm(x, after="rms", after_bias=g)[1], want)
+
+
 # ---- infinite weights of an adapter ---------------------------------------------------------------------------
 
 # tiles of bf16, forms for few rows (8 to 13), the tile of fp32 (14): those that a product can take.  Gate and value need pairs of pieces in a wave (not 7, 13); ranks of B whose

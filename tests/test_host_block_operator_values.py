@@ -3,6 +3,9 @@ import numpy as np
 import pytest
 
 from test_gpu_block_operator_values import close
+from test_host_block_operators import EINVAL, norm, residual
+
+from paper_2603_25872_amd import drf
 
 
 def test_results_that_are_no_numbers_are_refused():
@@ -21,3 +24,10 @@ def test_results_that_are_no_numbers_are_refused():
             close(got, want, "f32", 1.0)
     with pytest.raises(AssertionError):
         close(want[:1], want, "f32", 0.0)
+
+
+def test_a_residual_update_without_a_branch_has_no_look_at_its_arguments():
+    for over in (dict(y_scale=float("nan")), dict(y_scale=float("inf")), dict(after=norm(3)), dict(after=norm(eps=-1.0)), dict(after=norm(drf.QK_NONE, 0.0, 0x10000)),
+                 dict(after=norm(drf.QK_RMS, 0.0, None, 0x10000))):
+        assert residual(y=None, out=None, slots=0, **over) == 0
+        assert residual(slots=0, **over) == EINVAL
