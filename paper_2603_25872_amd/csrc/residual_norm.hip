@@ -7,6 +7,7 @@
 #include <algorithm>
 #include <type_traits>
 
+#include "gemm_device.h"
 #include "rows.h"
 
 namespace drf {
@@ -18,7 +19,8 @@ constexpr int kMaxWidth = 16384;
 // A row's squares and their sum are taken in fp32 as they are where that holds them: the sum is finite, and either above kFewSquares (what its smallest terms lose to
 // underflow, 16384 of 2^-126 at most, is 2^-29 of it) or of no account beside an eps of kMuchEps or more.  Other rows have a power of two taken out of them first.
 constexpr float kFewSquares = 1e-25f, kMuchEps = 1e-30f;
-struct RowNormArgs { int norm; float eps; double eps_given; const float *gain, *bias; };
+constexpr float kLeastEps = 1.17549435e-38f;        // (an eps that fp32 does not hold is still no zero: a row of zeros stays one)
+struct RowNormArgs { int norm; float eps, eps_part; int eps_exp; const float *gain, *bias; };     // eps_part 2^eps_exp: eps as it was given
 struct ResidualArgs {
     drf_rows x, y, out, h, gate, shift, scale;
     int rows, tokens, width;
@@ -28,8 +30,6 @@ struct ResidualArgs {
     float x_scale, y_scale, inv_width;
     RowNormArgs after, before;
 };
-
-__device__ inline int div_by(int n, uint32_t magic, int shift) { return magic ? (int)(__umulhi((uint32_t)n, magic) >> shift) : (n >> shift); }
 
 // Sum over a wave's lanes, in all of them: quads, halves of 16, 16, and the rows of 16 by swaps.  No LDS, some 6 dependent adds.
 __device__ inline float wave_total(float v)
@@ -89,7 +89,7 @@ __global__ void __launch_bounds__(512) residual_norm_kernel(const ResidualArgs a
         token = (id - slot * a.slot_tiles) * waves + wave;
     } else {
         const int row = GROUP ? a.first + blockIdx.x : (a.first + blockIdx.x) * waves + wave;
-        slot = div_by(row, a.tok_magic, a.tok_shift);
+        slot = fast_div(row, a.tok_magic, a.tok_shift);
         token = row - slot * a.tokens;
         if (row >= a.rows) return;
     }
@@ -152,14 +152,14 @@ __global__ void __launch_bounds__(512) residual_norm_kernel(const ResidualArgs a
             }
             if (most < INFINITY) {                  // (a row with an infinity: no number there, zeros beside it)
                 // x / sqrt(mean x^2 + eps) with x = 2^e t, |t| < 4: t / sqrt(mean t^2 + eps 2^-2e).  The lowest e that any fp32 row needs keeps an eps below kMuchEps finite
-                const int e = most > 0.f ? max(-110, min(126, ilogbf(most))) : -110;
-                const float f = ldexpf(1.f, -e);
+                const int e = max(-110, min(126, (int)(__builtin_bit_cast(uint32_t, most) >> 23) - 127));
+                const float f = __builtin_bit_cast(float, (uint32_t)(127 - e) << 23);
 #pragma unroll
                 for (int v = 0; v < NV; ++v)
 #pragma unroll
                     for (int j = 0; j < E; ++j) r[v][j] *= f;
                 s = total(squares(r), first + 3);
-                eps = n.eps_given > 0.0 ? fmaxf((float)ldexp(n.eps_given, -2 * e), 1.17549435e-38f) : 0.f;
+                eps = n.eps > 0.f ? fmaxf(ldexpf(n.eps_part, n.eps_exp - 2 * e), kLeastEps) : 0.f;
             }
         }
         const float inv = 1.f / sqrtf(fmaf(s, a.inv_width, eps));
@@ -331,8 +331,9 @@ drf_status fill_norm(const char* what, const drf_row_norm& n, RowNormArgs* out)
     if (!(n.eps >= 0.0) || !std::isfinite(n.eps)) DRF_FAIL(DRF_EINVAL, "%s: eps must be >= 0", what);
     if (n.norm == DRF_QK_NONE && n.gain) DRF_FAIL(DRF_EINVAL, "%s: a gain without a norm", what);
     if (n.norm != DRF_QK_LAYER && n.bias) DRF_FAIL(DRF_EINVAL, "%s: a bias belongs to DRF_QK_LAYER", what);
-    // (an eps that fp32 does not hold is still no zero: a row of zeros stays one)
-    *out = { (int)n.norm, n.eps > 0.0 ? std::max((float)n.eps, 1.17549435e-38f) : 0.f, n.eps, n.gain, n.bias };
+    int exp = 0;
+    const float part = (float)std::frexp(n.eps, &exp);
+    *out = { (int)n.norm, n.eps > 0.0 ? std::max((float)n.eps, kLeastEps) : 0.f, part, exp, n.gain, n.bias };
     return DRF_OK;
 }
 
