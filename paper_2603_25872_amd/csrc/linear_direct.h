@@ -159,13 +159,12 @@ __global__ void __launch_bounds__(NW * 64) linear_direct_kernel(const LinArgs a)
     const int tm = (int)(id / a.tiles_n), tn = (int)(id - (long long)tm * a.tiles_n), row0 = tm * LANES * MI;
     const int n0 = tn * (KIND == LIN_GLU ? LANES / 2 * NI : LANES * NI);
     const T *x[MI], *w[NI];
-    int slot[MI], token[MI];
-    bool live[MI];
 #pragma unroll
-    for (int j = 0; j < MI; ++j) {
-        live[j] = locate_row(a, 0, row0 + LANES * j + lrow, slot[j], token[j]);
-        if (row0 + LANES * j + lrow >= a.slot_rows) slot[j] = token[j] = 0;        // (any row that is there: not stored)
-        x[j] = (const T*)a.x.data + slot[j] * a.x.slot_stride + token[j] * a.x.token_stride;
+    for (int j = 0; j < MI; ++j) {                  // (rows behind a length are read and multiplied like others; what is not there is some row that is.  Neither is stored)
+        int slot, token;
+        locate_row(a, 0, row0 + LANES * j + lrow, slot, token);
+        if (row0 + LANES * j + lrow >= a.slot_rows) slot = token = 0;
+        x[j] = (const T*)a.x.data + slot * a.x.slot_stride + token * a.x.token_stride;
     }
 #pragma unroll
     for (int i = 0; i < NI; ++i) {
