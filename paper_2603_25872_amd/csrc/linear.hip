@@ -5,7 +5,8 @@
 //   adapters       t = s_i x A_i^T  [row][rank] in one launch;  then out = x W^T + t B_i^T + b: the adapter is `rank` more columns of the product's inner
 //                  axis, whose operands are a row's t and its own adapter's B
 //
-// This file has the entry points, the choice of a tile, x A^T and all of fp32; bf16 products run on the tiles of linear_tile.h.  The weights are the matrix
+// This file has the entry points, the choice of a tile or form, x A^T and the tile of fp32; bf16 products run on the tiles of linear_tile.h and linear_wide.h, few rows
+// of both types on the forms of linear_direct.h.  The weights are the matrix
 // instruction's first operand throughout: a lane ends with four consecutive columns of one row.
 #include "linear_direct.h"
 #include "../../include/drf_measure.h"
@@ -17,14 +18,16 @@ namespace {
 constexpr int kMaxTokenStride = 1 << 22;           // 256 rows within 2^31 bytes
 
 // Tiles and a time model of a launch of each: base + (per round of workgroups) round + steps * max(lat, c * thr) us, where a round is per_cu workgroups on each of 256
-// CUs and c those that share a CU in it.  Least-squares fits to 260 products (16 to 65536 rows, 64 to 9600 columns, an inner axis of 72 to 4800, weights cold);
-// the choice by it is within 1 % of the best tile on average, 11 % behind at worst.
+// CUs and c those that share a CU in it.  Least-squares fits to 260 products (16 to 65536 rows, 64 to 9600 columns, an inner axis of 72 to 4800, weights cold).
+// The whole choice, tiles and forms, on 300 other products that are drawn (60 of each type, with and without adapters): 1.4 to 3.1 % behind the best on average, a tenth of
+// them by more than 7 to 15 %, at worst 28 % (bf16), 35 % (bf16, ranks that are no multiple of 8) and 37 % (fp32), all of these products of 6 to 15 us.
 struct Tile { int bm, bn, per_cu; double base, round, lat, thr; };
 const Tile kLinTiles[] = { { 256, 256, 1, 0.00, 9.05, 1.075, 0 }, { 256, 128, 1, 0.00, 6.40, 0.723, 0 }, { 128, 128, 1, 0.43, 4.47, 0.451, 0 }, { 128, 64, 2, 1.54, 3.59, 0.324, 0.324 },
                            { 64, 128, 2, 1.60, 3.50, 0.333, 0.333 }, { 64, 64, 2, 1.75, 2.83, 0.207, 0.207 }, { 256, 256, 1, 0.00, 11.9, 0.965, 0 }, { 256, 288, 1, 0.00, 13.6, 1.067, 0 } };
 constexpr int kTiles = sizeof(kLinTiles) / sizeof(kLinTiles[0]);
 // The forms for few rows of linear_direct.h, rows and weight rows a workgroup in sixteens and its waves: fixed + turns * turn + max(0, workgroups / 256 - hidden) * (group + 128-byte
-// pieces of the inner axis * piece) us, fitted likewise (140 and 100 products of 1 to 4096 rows; the choice is within 5 % of the best on average in bf16, 3 % in fp32).
+// pieces of the inner axis * piece) us, fitted likewise (140 and 100 products of 1 to 4096 rows).  The last form's are set by hand: it is looked at up to one workgroup a CU alone,
+// where it has no shares to tell apart, and its adapters' share is the first form's.
 struct Form { int mi, ni, nw; double fixed, turn, hidden, group, piece; };
 constexpr int kForms = 6;
 const Form kFormsBf16[kForms] = { { 1, 1, 16, 1.83, 1.13, 0.27, 1.18, 0.095 }, { 1, 4, 8, 1.84, 1.75, 0.40, 0.80, 0.282 }, { 2, 2, 8, 2.18, 1.03, 0.06, 0.85, 0.196 }, { 4, 2, 8, 2.47, 1.47, 0.37, 1.71, 0.343 },
@@ -40,8 +43,8 @@ double tile_us(const Tile& m, long long tiles, int steps)
 }
 
 // What adapters add, x A^T's launch included: first + pieces of 8 of the rank * rank + workgroups / 256 * (group + pieces * group_rank) us for a form (fitted to products of
-// 1 to 800 rows of 1 to 40 slots, ranks of 8 to 128, 4 % off on average; unaligned rows of B count 1.7 times).  With it the choice is within 2 % of the best on average, 24 %
-// at worst; it matters most where every row has an adapter of its own (200 x 384 x 1152, rank 128, fp32: 31 us, the tile 220).
+// 1 to 800 rows of 1 to 40 slots, ranks of 8 to 128, 4 % off on average; unaligned rows of B count 1.7 times).  It matters most where every row is a slot (200 x 384 x 1152,
+// rank 128, fp32, four adapters among the slots: 34 us, on the tile 245; an adapter each: 65 and 352).
 struct FormAdapters { double first, rank, group, group_rank; };
 const FormAdapters kAdaptBf16[kForms] = { { 1.96, 0.232, 0, 0.246 }, { 2.36, 0.422, 0.476, 0.07 }, { 2.32, 0.401, 0.492, 0.075 }, { 2.39, 0.80, 0.69, 0.1 }, { 2.13, 0.306, 0.165, 0.219 }, { 1.96, 0.232, 0, 0.246 } };
 const FormAdapters kAdaptF32[kForms] = { { 2.65, 0.307, 0.066, 0.35 }, { 0 }, { 2.81, 0.491, 0.563, 0.072 }, { 2.78, 0.848, 0.3, 0.05 }, { 2.59, 0.359, 0.153, 0.25 }, { 0 } };
@@ -67,8 +70,8 @@ template <typename T, int KIND> int pick_form(const LinArgs& a, double* us)
     for (int f = 0; f < kForms; ++f) {
         const Form& m = forms[f];
         if (!m.mi) continue;
-        // the last form takes 8 rows by 8 and twice the pieces a turn.  Up to one workgroup a CU it is what few columns of a long inner axis want (1 x 4608 x 1152 7.5 -> 5.8 us,
-        // 1 x 9216 x 1152 12.7 -> 8.6, 8 x 4608 x 1152 9.0 -> 7.3), behind it every other is ahead (1 x 4608 x 2304 7.7, this one 10.8)
+        // the last form takes 8 rows by 8 and twice the pieces a turn.  Up to one workgroup a CU it is what few columns of a long inner axis want (weights cold, 16 by 16 and 8 by 8:
+        // 1 x 4608 x 1152 7.9 and 6.2 us, 1 x 9216 x 1152 13.5 and 9.4, 8 x 4608 x 1152 9.4 and 7.7), behind it every other is ahead (1 x 4608 x 2304 7.7 and 10.8)
         const int split = f == kForms - 1 ? 2 : 1, mr = 16 / split * m.mi, nr = 16 / split * m.ni, at_once = m.nw * split;
         const double groups = (double)((rows + mr - 1) / mr) * ((weight_rows + nr - 1) / nr);
         if (split > 1 && (KIND == LIN_GLU || groups > 256)) continue;

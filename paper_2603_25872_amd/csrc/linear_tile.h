@@ -10,9 +10,9 @@
 //  - LIN_ADAPT: where a tile keeps to a slot its adapter is more steps of the loop, 32 columns of the rank each: 64 columns of a row are the upper and
 //    the lower halves of its x A^T, those of a weight row twice the same of B.  Elsewhere the adapters are added to the finished sums (add_adapters);
 //  - the result goes out in whole rows through the idle stages, rows that are not there left out.
-// Large products are bound by the clock under the matrix unit (gate and value of 65536 rows, 1152 x 9216, on 256 x 256: 1204 to 1340 us, 1.04 to 1.16 PFLOP/s with the activation), single
+// Large products are bound by the clock under the matrix unit (gate and value of 65536 rows, 1152 x 9216, on 256 x 256: 1190 to 1300 us, 1.07 to 1.17 PFLOP/s with the activation), single
 // rounds by first copies and store (12 x 256 rows, 384 x 2 x 1536: 18 us on 144 tiles, of which the matrix unit is busy for 3).  Smaller ones are for the rounds
-// that they fill better: 19 x 77 rows, 1024 x 2304 with adapters of rank 24, 17.4 us on 216 tiles of 128 x 128.
+// that they fill better: 19 x 77 rows, 1024 x 2304 with adapters of rank 24, 18 us on 216 tiles of 128 x 128.
 #pragma once
 #include "linear_direct.h"
 #include "linear_wide.h"

@@ -1,8 +1,8 @@
 // The tiles of 256 rows by 256 or 288 rows of the weights for products that fill the chip with them: four waves, one a SIMD, each with 128 x 128 or 128 x 144 of
 // the tile and a SIMD's whole register file.  What a tile is made of is as in linear_tile.h; the loop is that of the framework's other products of this size: a
 // fixed sequence of matrix instructions with at most one LDS read or one copy beside each, both halves of a step double-buffered in registers, two barriers a step
-// (a stage is free from slot REL on, the next one is needed from slot LAND on).  65536 x 4608 x 1152: 492 to 544 us on 256 x 288, 1.28 to 1.41 PFLOP/s, bound by the clock under the matrix
-// unit; 65536 x 1152 x 3456 441 us, 1.18, and 490 to 500 with adapters of rank 32, whose step is one more of 18 and has its copies' offsets made anew.
+// (a stage is free from slot REL on, the next one is needed from slot LAND on).  65536 x 4608 x 1152: 479 to 515 us on 256 x 288, 1.35 to 1.45 PFLOP/s, bound by the clock under the matrix
+// unit; 65536 x 1152 x 3456 441 to 478 us, 1.09 to 1.18, and 455 to 494 with adapters of rank 32, whose step is one more of 18 and has its copies' offsets made anew.
 #pragma once
 #include "linear_device.h"
 

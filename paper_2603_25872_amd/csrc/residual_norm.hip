@@ -3,7 +3,9 @@
 //
 // A row's lanes hold it in registers from its load to its stores: mean, then the squares of what is left of it (two sums, so that a large mean costs nothing
 // of the variance), each over the lanes without LDS where one wave has a row.  Everything is read and written once: bound by memory.  6 x 4096 x 1152, stream in fp32, branch in
-// bf16, LayerNorm before (340 MB): 64.7 us, 5.25 TB/s;  4 x 16384 x 1536 in bf16, RMS on both sides (805 MB): 144 us, 5.6;  a large copy: 5.15.  One row: 4.5 us, a launch.
+// bf16, LayerNorm before (340 MB): 64.6 us, 5.26 TB/s;  4 x 16384 x 1536 in bf16, RMS on both sides (805 MB): 143 us, 5.6;  a large copy: 5.18.  One row: 4.4 us, a launch.
+// Modulation by token in fp32 doubles the bytes of the first of these: 679 MB, 130 us, 5.2 TB/s.  Rows on a workgroup each: 4 x 4096 of 2560 in bf16, RMS twice (336 MB) 85 us, 3.9;
+// of 4096 as the first of these (805 MB) 158, 5.1; 2 x 2048 of 8192 in fp32, LayerNorm twice (537 MB) 129, 4.2.
 #include <algorithm>
 #include <type_traits>
 

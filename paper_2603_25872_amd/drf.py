@@ -655,8 +655,8 @@ def gated_ffn(x, w_in, w_out, b_in=None, b_out=None, act="silu", lens=None, out=
 
 def linear_adapters(x, w, a, b, which, bias=None, scales=None, lens=None, out=None):
     """x W^T + bias + scales[i] (x A_i^T) B_i^T, i = which[slot], of x [slots, tokens, columns]: w [out columns, columns] for all slots, a [adapters, rank, columns]
-    and b [adapters, out columns, rank], which int32 [slots] (an index outside of the adapters: none), bias and scales fp32.  Rows behind a slot's length are left as
-    they were: zeros in an output made here.  No gradient is recorded."""
+    and b [adapters, out columns, rank], which int32 [slots] (an index outside of the adapters: none), bias and scales fp32.  In bf16 ranks that are multiples of 8 are
+    the fast ones.  Rows behind a slot's length are left as they were: zeros in an output made here.  No gradient is recorded."""
     import torch
     ops = _block_ops or _block_operators()
     n = ops.linear_adapters(x, w, a, b, which, bias, scales, lens, None, None)
